@@ -50,8 +50,10 @@ enum {
                                     outside the forest (the request is then not verified), or
                                     a second root in a tree (the node stays unreached)       */
     DSBD_DEV_TIMEOUT = 5,        /* a bounded wait gave up                                   */
-    DSBD_DEV_BAD_PARAM = 6       /* a per-request width (W_min_r, W_max_r, W_nom_r) below 1, or
+    DSBD_DEV_BAD_PARAM = 6,      /* a per-request width (W_min_r, W_max_r, W_nom_r) below 1, or
                                     W_max_r below W_min_r                                    */
+    DSBD_DEV_BAD_CHUNK = 7       /* a chunk's offset, length, page id or position that contradicts
+                                    what the call was told; what it names is left out          */
 };
 
 /* limits of this build */
@@ -443,6 +445,114 @@ int dsbd_kv_commit_paged(const dsbd_forest_t *forest, const dsbd_attn_desc_t *de
 
 size_t dsbd_kv_commit_paged_workspace(const dsbd_forest_t *forest, const dsbd_commit_params_t *params,
                                       int64_t n_pages);
+
+/* ---- From a model's projections to the forest: rotation, append, attention of a chunk -------
+ * (The paper takes the models' forward passes for granted; these are the operators between a QKV
+ * projection and the calls above.  A prompt, a piece of one, or the small model's next token goes
+ * dsbd_kv_append_paged -> dsbd_chunk_attention_paged in every layer; the nodes of a forest go
+ * dsbd_forest_positions once a step, then dsbd_rotate_qk -> dsbd_forest_attention(_paged).) */
+
+/* How the angles of a rotation grow with the position: frequency i of rot / 2 is base^(-2 i / rot),
+ * changed for contexts longer than the model was trained on by one of
+ *   LINEAR      divided by `factor`
+ *   BASE        base * factor^(rot / (rot - 2)) in place of base
+ *   WAVELENGTH  wavelengths above original / low divided by factor, those below original / high kept,
+ *               blended linearly in original / wavelength between the two
+ *   RAMP        arXiv 2309.00071: dimensions that turn more than `high` times in `original` tokens kept,
+ *               those that turn less than `low` times divided by factor, a linear ramp over the
+ *               dimensions between; cos and sin times `attention`, 0.1 ln(factor) + 1 when that is 0 */
+enum { DSBD_ROPE_PLAIN = 0, DSBD_ROPE_LINEAR = 1, DSBD_ROPE_BASE = 2, DSBD_ROPE_WAVELENGTH = 3, DSBD_ROPE_RAMP = 4 };
+
+typedef struct {
+    int32_t kind;                  /* DSBD_ROPE_*                                            */
+    double base;                   /* > 1                                                    */
+    double factor;                 /* >= 1 (ignored by PLAIN)                                */
+    double original;               /* trained context (WAVELENGTH, RAMP)                     */
+    double low, high;              /* 0 < low < high (WAVELENGTH, RAMP)                      */
+    double attention;              /* RAMP: factor on cos and sin, 0 = 0.1 ln(factor) + 1    */
+} dsbd_rope_scaling_t;
+
+/* The rot / 2 frequencies and the factor on cos and sin; host arrays, host-only.  rot: even, 2 .. 128. */
+int dsbd_rope_frequencies(const dsbd_rope_scaling_t *scaling, int32_t rot, double *frequencies, double *attention);
+
+/* table [n_positions][2][rot / 2] fp32: the cosines, then the sines of position * frequency (angles in
+ * double, rounded once).  Made once per model. */
+int dsbd_rope_table(const dsbd_rope_scaling_t *scaling, int32_t rot, int32_t n_positions, float *table,
+                    dsbd_stream_t stream);
+
+enum { DSBD_ROPE_HALF = 0, DSBD_ROPE_INTERLEAVED = 1 };
+
+/* What happens to a head's row x of d values: x * rsqrt(mean(x^2) + eps) * weight when there is a norm weight
+ * (fp32 [d]); then the first rot values are turned in pairs, (x[i], x[i + rot/2]) for HALF or
+ * (x[2i], x[2i+1]) for INTERLEAVED: (u, v) -> (u cos - v sin, v cos + u sin) with row `position` of the table; the
+ * rest of the row stays as normed.  All in fp32, rounded once to the tensors' dtype. */
+typedef struct {
+    const float *table;            /* [n_positions][2][rot / 2]; NULL with rot = 0: norms only */
+    int32_t n_positions;
+    int32_t rot;                   /* multiple of 16, at most d; 0: no rotation              */
+    int32_t layout;                /* DSBD_ROPE_HALF or DSBD_ROPE_INTERLEAVED                */
+    const float *q_norm, *k_norm;  /* [d] each, or NULL: not normed                          */
+    float eps;
+} dsbd_rope_t;
+
+/* Norm and rotation of T tokens' queries and keys in one pass.  q: row t, head h at q + t * q_stride + h * d (so a view of
+ * a fused projection's output will do), k likewise with Hkv heads; q_out, k_out with strides of their own; an
+ * output may be its input with the same stride, and overlaps it in no other way.  k (with k_out) or q (with q_out) may
+ * be NULL.  position [T] int32 in [0, n_positions): a token outside is left out and reported (DSBD_DEV_BAD_CHUNK).
+ * desc gives Hq, Hkv, d, dtype.  Errors: INVALID_ARG (null pointer, stride below heads * d, rot), UNSUPPORTED (d, dtype, a
+ * pointer or stride that is not a multiple of 16 bytes).  T = 0 launches nothing. */
+int dsbd_rotate_qk(int32_t T, const dsbd_attn_desc_t *desc, const dsbd_rope_t *rope, const int32_t *position,
+                   const void *q, int64_t q_stride, const void *k, int64_t k_stride,
+                   void *q_out, int64_t q_out_stride, void *k_out, int64_t k_out_stride,
+                   int32_t *status, dsbd_stream_t stream);
+
+/* position[n] = L_b + depth(n) for node n of beam b: the position of the node's token behind the beam's prefix.
+ * *status: DSBD_DEV_BAD_FOREST for an offset outside the forest or a parent outside the node's tree. */
+int dsbd_forest_positions(const dsbd_forest_t *forest, const int64_t *prefix_off, int32_t *position,
+                          int32_t *status, dsbd_stream_t stream);
+
+/* New tokens of B sequences, ragged: sequence b has L_b = prefix_off[b+1] - prefix_off[b] tokens in its pages already
+ * and gets the rows new_off[b] .. new_off[b+1]) of the call's tensors, token i of them at position L_b + i.  Either
+ * count may be 0.  Pages as for dsbd_forest_attention_paged; those of the new tokens are in the table already:
+ * page_off[b+1] - page_off[b] >= ceil((L_b + n_b) / DSBD_PAGE_TOKENS). */
+typedef struct {
+    int32_t B;
+    const int32_t *new_off;        /* device [B+1]                                           */
+    const int64_t *prefix_off;     /* device [B+1]                                           */
+    /* host-side facts about the arrays above */
+    int32_t total_new;             /* new_off[B]: rows of the tensors                        */
+    int32_t max_new;               /* max_b n_b (an upper bound will do)                     */
+    int64_t max_len;               /* max_b L_b + n_b (an upper bound will do)               */
+} dsbd_chunk_t;
+
+/* Appends a chunk to the paged cache: k normed and rotated on the way (rope NULL: as it is), v as it is, at the tokens'
+ * places in the pools; q (may be NULL) normed and rotated into q_out in the same pass.  A page whose first row the call
+ * writes is written whole, zeros behind the last token; of other pages the rows of the new tokens alone.  Strides as in
+ * dsbd_rotate_qk, for v as for k.  No two sequences may share a page that gets a row.  *status: DSBD_DEV_CAPACITY for a
+ * page table that is too short, DSBD_DEV_BAD_CHUNK for an offset, page id or position out of range (the rows concerned
+ * are left out).  pages->n_layers is not looked at: one layer's pools a call. */
+int dsbd_kv_append_paged(const dsbd_chunk_t *chunk, const dsbd_attn_desc_t *desc, const dsbd_rope_t *rope,
+                         const void *q, int64_t q_stride, const void *k, int64_t k_stride,
+                         const void *v, int64_t v_stride, void *q_out, int64_t q_out_stride,
+                         void *k_pool, void *v_pool, const dsbd_kv_pages_t *pages, int32_t *status,
+                         dsbd_stream_t stream);
+
+/* Attention of a chunk over the paged cache that holds it: token i of sequence b, head h,
+ *   out = sum_j softmax_j(scale * q . K_j) V_j  over the positions j = 0 .. L_b + i of its sequence.
+ * q, out [total_new, Hq, d] contiguous (out is not q).  One token a sequence or whole prompts, mixed as they come.  Rows
+ * of the pools behind a sequence's last token are not used, whatever they hold; values at positions that a row does not
+ * see, in the same stretch of 128 tokens as ones that it or a neighbouring row sees, must be finite.  bf16, d 64 or 128,
+ * Hq / Hkv <= 128, scale > 0; otherwise UNSUPPORTED (scale: INVALID_ARG).  *status as in dsbd_kv_append_paged, with rows of
+ * a sequence that is left out not written and missing pages read as zeros, and DSBD_DEV_TIMEOUT. */
+int dsbd_chunk_attention_paged(const dsbd_chunk_t *chunk, const dsbd_attn_desc_t *desc, const void *q,
+                               const void *k_pool, const void *v_pool, const dsbd_kv_pages_t *pages, void *out,
+                               void *workspace, size_t workspace_bytes, int32_t *status, dsbd_stream_t stream);
+
+/* Bytes of its workspace (256-byte aligned); 0 for arguments that the call would refuse. */
+size_t dsbd_chunk_attention_paged_workspace(const dsbd_chunk_t *chunk, const dsbd_attn_desc_t *desc);
+
+/* Kernels that a call launches (1, or 2 with the merge of sequences that are cut); 0 for invalid arguments. */
+int dsbd_chunk_attention_paged_launches(const dsbd_chunk_t *chunk, const dsbd_attn_desc_t *desc);
 
 const char *dsbd_status_string(int code);
 

@@ -25,7 +25,9 @@ EXPORTS = ["dsbd_forest_attention", "dsbd_forest_attention_workspace", "dsbd_for
            "dsbd_verify_workspace", "dsbd_verify_cluster_ctas", "dsbd_select_width", "dsbd_node_stats", "dsbd_node_stats_static",
            "dsbd_kv_commit", "dsbd_kv_commit_workspace", "dsbd_draft_layer", "dsbd_draft_workspace",
            "dsbd_forest_attention_paged", "dsbd_forest_attention_paged_workspace", "dsbd_kv_commit_paged", "dsbd_kv_commit_paged_workspace",
-           "dsbd_forest_build",
+           "dsbd_forest_build", "dsbd_rope_frequencies", "dsbd_rope_table", "dsbd_rotate_qk", "dsbd_forest_positions",
+           "dsbd_kv_append_paged", "dsbd_chunk_attention_paged", "dsbd_chunk_attention_paged_workspace",
+           "dsbd_chunk_attention_paged_launches",
            "dsbd_status_string"]
 
 _vp = C.c_void_p
@@ -129,6 +131,23 @@ def _declare(lib):
     lib.dsbd_draft_layer.restype = C.c_int
     lib.dsbd_draft_layer.argtypes = [C.c_int32, C.c_int32, _vp, _vp, _vp, C.c_int64, _vp, _vp, _vp, _vp, _vp, _vp,
                                      _vp, C.c_size_t, _vp, _vp]
+    i64 = C.c_int64
+    lib.dsbd_rope_frequencies.restype = C.c_int
+    lib.dsbd_rope_frequencies.argtypes = [_vp, C.c_int32, _vp, _vp]
+    lib.dsbd_rope_table.restype = C.c_int
+    lib.dsbd_rope_table.argtypes = [_vp, C.c_int32, C.c_int32, _vp, _vp]
+    lib.dsbd_rotate_qk.restype = C.c_int
+    lib.dsbd_rotate_qk.argtypes = [C.c_int32, _vp, _vp, _vp, _vp, i64, _vp, i64, _vp, i64, _vp, i64, _vp, _vp]
+    lib.dsbd_forest_positions.restype = C.c_int
+    lib.dsbd_forest_positions.argtypes = [_vp] * 5
+    lib.dsbd_kv_append_paged.restype = C.c_int
+    lib.dsbd_kv_append_paged.argtypes = [_vp, _vp, _vp, _vp, i64, _vp, i64, _vp, i64, _vp, i64, _vp, _vp, _vp, _vp, _vp]
+    lib.dsbd_chunk_attention_paged.restype = C.c_int
+    lib.dsbd_chunk_attention_paged.argtypes = [_vp] * 8 + [C.c_size_t, _vp, _vp]
+    lib.dsbd_chunk_attention_paged_workspace.restype = C.c_size_t
+    lib.dsbd_chunk_attention_paged_workspace.argtypes = [_vp, _vp]
+    lib.dsbd_chunk_attention_paged_launches.restype = C.c_int
+    lib.dsbd_chunk_attention_paged_launches.argtypes = [_vp, _vp]
     return lib
 
 
@@ -647,3 +666,212 @@ def select_width(forest, params, logits_p, logits_q, node_logp, node_logq, live_
     if rc != OK:
         raise DsbdError("dsbd_select_width", rc)
     return width, alpha, tail, status
+
+
+# ---------------------------------------------------------------- rotation, append, attention of a chunk
+ROPE_KINDS = {"plain": 0, "linear": 1, "base": 2, "wavelength": 3, "ramp": 4}
+ROPE_LAYOUTS = {"half": 0, "interleaved": 1}
+
+
+class RopeScalingT(C.Structure):
+    _fields_ = [("kind", C.c_int32), ("base", C.c_double), ("factor", C.c_double), ("original", C.c_double),
+                ("low", C.c_double), ("high", C.c_double), ("attention", C.c_double)]
+
+
+class RopeT(C.Structure):
+    _fields_ = [("table", _vp), ("n_positions", C.c_int32), ("rot", C.c_int32), ("layout", C.c_int32),
+                ("q_norm", _vp), ("k_norm", _vp), ("eps", C.c_float)]
+
+
+class ChunkT(C.Structure):
+    _fields_ = [("B", C.c_int32), ("new_off", _vp), ("prefix_off", _vp), ("total_new", C.c_int32),
+                ("max_new", C.c_int32), ("max_len", C.c_int64)]
+
+
+def _scaling(base, scaling):
+    s = dict(scaling or {})
+    kind = s.pop("kind", "plain")
+    if kind not in ROPE_KINDS or set(s) - {"factor", "original", "low", "high", "attention"}:
+        raise ValueError("dsbd: rope scaling %r" % (scaling,))
+    return RopeScalingT(ROPE_KINDS[kind], float(base), float(s.get("factor", 1.0)), float(s.get("original", 0.0)),
+                        float(s.get("low", 0.0)), float(s.get("high", 0.0)), float(s.get("attention", 0.0)))
+
+
+def rope_frequencies(rot, base=10000.0, scaling=None):
+    """dsbd_rope_frequencies; scaling: None or dict(kind="linear" | "base" | "wavelength" | "ramp", factor, original, low,
+    high, attention).  Returns (float64 array [rot / 2], factor on cos and sin); host-only."""
+    s, f, att = _scaling(base, scaling), np.empty(max(int(rot) // 2, 1), dtype=np.float64), C.c_double(0.0)
+    rc = load().dsbd_rope_frequencies(C.addressof(s), int(rot), f.ctypes.data, C.addressof(att))
+    if rc != OK:
+        raise DsbdError("dsbd_rope_frequencies", rc)
+    return f, att.value
+
+
+def rope_table(n_positions, rot, base=10000.0, scaling=None, device="cuda", table=None, stream=None):
+    """dsbd_rope_table: fp32 [n_positions, 2, rot / 2], cosines and sines.  Made once per model."""
+    s = _scaling(base, scaling)
+    if table is None:
+        table = torch.empty(int(n_positions), 2, int(rot) // 2, dtype=torch.float32, device=device)
+    _require_cuda(table)
+    assert table.dtype == torch.float32 and tuple(table.shape) == (int(n_positions), 2, int(rot) // 2)
+    rc = load().dsbd_rope_table(C.addressof(s), int(rot), int(n_positions), _ptr(table), _stream(stream))
+    if rc != OK:
+        raise DsbdError("dsbd_rope_table", rc)
+    return table
+
+
+class Rope:
+    """What is done to the heads of a model's queries and keys: rotation by the rows of `table` (fp32 [positions, 2, rot / 2],
+    see rope_table; None: norms only) and per-head norms (fp32 [d] weights, or None)."""
+
+    def __init__(self, table, layout="half", q_norm=None, k_norm=None, eps=1e-6):
+        _require_cuda(table, q_norm, k_norm)
+        assert table is None or (table.dtype == torch.float32 and table.dim() == 3 and table.shape[1] == 2)
+        assert all(w is None or w.dtype == torch.float32 for w in (q_norm, k_norm))
+        self.tensors = (table, q_norm, k_norm)                # (the struct holds their addresses)
+        self.d = {int(w.numel()) for w in (q_norm, k_norm) if w is not None}
+        n, rot = (int(table.shape[0]), 2 * int(table.shape[2])) if table is not None else (0, 0)
+        self._struct = RopeT(_ptr(table), n, rot, ROPE_LAYOUTS[layout], _ptr(q_norm), _ptr(k_norm), float(eps))
+        self.address = C.addressof(self._struct)
+
+    def check(self, d):
+        assert self.d <= {d}, "norm weights have the length of a head"
+
+
+class Chunk:
+    """New tokens of B sequences and the pages that they go to: rows new_off[b] .. new_off[b+1]) of a call's tensors are
+    sequence b's, behind its prefix_off[b+1] - prefix_off[b] cached tokens; pages page_table[page_off[b] .. page_off[b+1]).
+    Device tensors, plus host copies of the offsets, which size the launches.  One object serves all layers of a step."""
+
+    def __init__(self, new_off, new_off_host, prefix_off, prefix_off_host, page_table, page_off):
+        _require_cuda(new_off, prefix_off, page_table, page_off)
+        assert new_off.dtype == torch.int32 and prefix_off.dtype == torch.int64
+        assert page_table.dtype == torch.int32 and page_off.dtype == torch.int64
+        new, old = np.asarray(new_off_host, dtype=np.int64), np.asarray(prefix_off_host, dtype=np.int64)
+        assert len(new) == len(old) == new_off.numel() == prefix_off.numel() == page_off.numel() and len(new) > 1
+        self.tensors = (new_off, prefix_off, page_table, page_off)
+        self.B, self.total_new = len(new) - 1, int(new[-1])
+        n = new[1:] - new[:-1]
+        self.max_new, self.max_len = int(n.max()), int((n + old[1:] - old[:-1]).max())
+        self._struct = ChunkT(self.B, _ptr(new_off), _ptr(prefix_off), self.total_new, self.max_new, self.max_len)
+        self.address = C.addressof(self._struct)
+        self._table, self._page_off = _ptr(page_table), _ptr(page_off)
+
+    def pages(self, k_pool, v_pool):
+        assert k_pool.dim() == 4 and k_pool.shape == v_pool.shape and k_pool.shape[2] == 64
+        assert k_pool.dtype == v_pool.dtype and k_pool.is_contiguous() and v_pool.is_contiguous()
+        return KvPagesT(self._table, self._page_off, int(k_pool.shape[0]))
+
+
+def _heads(t):
+    """Pointer and row stride of a [T, H, d] tensor whose heads lie side by side (a view of a projection's output)."""
+    if t is None:
+        return None, 0
+    T, H, d = t.shape
+    s = t.stride()
+    assert (s[2] == 1 or d == 1) and (s[1] == d or H == 1), "rows of heads side by side"
+    return t.data_ptr(), s[0] if T > 1 else max(s[0], H * d)
+
+
+_DTYPES = {torch.bfloat16: DTYPE_BF16, torch.float32: DTYPE_F32}
+
+
+def _status(status, device):
+    return torch.zeros(1, dtype=torch.int32, device=device) if status is None else status
+
+
+def forest_positions(forest, prefix_off, position=None, status=None, stream=None):
+    """dsbd_forest_positions: position[n] = prefix length of node n's beam + its depth, int32 [N]; returns (position, status)."""
+    _require_cuda(prefix_off)
+    f = forest.struct()
+    if position is None:
+        position = torch.empty(forest.N, dtype=torch.int32, device=prefix_off.device)
+    status = _status(status, prefix_off.device)
+    rc = load().dsbd_forest_positions(C.addressof(f), _ptr(prefix_off), _ptr(position), _ptr(status), _stream(stream))
+    if rc != OK:
+        raise DsbdError("dsbd_forest_positions", rc)
+    return position, status
+
+
+def rotate_qk(q, k, position, rope, q_out=None, k_out=None, status=None, stream=None):
+    """dsbd_rotate_qk.  q [T, Hq, d], k [T, Hkv, d] (views of a fused projection will do; either may be None), position int32 [T].
+    q_out = q and k_out = k work in place.  Returns (q_out, k_out, status)."""
+    x = q if q is not None else k
+    _require_cuda(x, k, position)
+    T, H, d = x.shape
+    assert k is None or (k.dtype == x.dtype and k.shape[0] == T and k.shape[2] == d)
+    assert position is None or (position.dtype == torch.int32 and position.numel() == T)
+    rope.check(d)
+    if q is not None and q_out is None:
+        q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+    if k is not None and k_out is None:
+        k_out = torch.empty(k.shape, dtype=k.dtype, device=k.device)
+    status = _status(status, x.device)
+    for a, b in ((q, q_out), (k, k_out)):
+        assert a is None or (b.shape == a.shape and b.dtype == a.dtype)
+    Hkv = k.shape[1] if k is not None else H
+    desc = AttnDescT(H if q is not None else Hkv, Hkv, d, _DTYPES[x.dtype], 1.0, 0, 0)
+    rc = load().dsbd_rotate_qk(T, C.addressof(desc), rope.address, _ptr(position), *_heads(q), *_heads(k), *_heads(q_out),
+                               *_heads(k_out), _ptr(status), _stream(stream))
+    if rc != OK:
+        raise DsbdError("dsbd_rotate_qk", rc)
+    return q_out, k_out, status
+
+
+def kv_append_paged(chunk, k, v, k_pool, v_pool, rope=None, q=None, q_out=None, status=None, stream=None):
+    """dsbd_kv_append_paged.  k, v [total_new, Hkv, d], q (optional) [total_new, Hq, d], views of a fused projection will
+    do; pools [n_pages, Hkv, 64, d] of one layer, updated in place.  rope None: no norm, no rotation.  Returns (q_out, status)."""
+    _require_cuda(k, v, q, k_pool, v_pool)
+    T, Hkv, d = k.shape
+    assert T == chunk.total_new and v.shape == k.shape and k.dtype == v.dtype == k_pool.dtype
+    assert k_pool.shape[1] == Hkv and k_pool.shape[3] == d
+    pages = chunk.pages(k_pool, v_pool)
+    if rope is not None:
+        rope.check(d)
+    Hq = Hkv
+    if q is not None:
+        assert q.shape[0] == T and q.shape[2] == d and q.dtype == k.dtype
+        Hq = q.shape[1]
+        if q_out is None:
+            q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        assert q_out.shape == q.shape and q_out.dtype == q.dtype
+    status = _status(status, k.device)
+    desc = AttnDescT(Hq, Hkv, d, _DTYPES[k.dtype], 1.0, 0, 0)
+    rc = load().dsbd_kv_append_paged(chunk.address, C.addressof(desc), rope.address if rope is not None else None, *_heads(q),
+                                     *_heads(k), *_heads(v), *_heads(q_out if q is not None else None), k_pool.data_ptr(),
+                                     v_pool.data_ptr(), C.addressof(pages), _ptr(status), _stream(stream))
+    if rc != OK:
+        raise DsbdError("dsbd_kv_append_paged", rc)
+    return (q_out if q is not None else None), status
+
+
+def chunk_attention_workspace(chunk, Hq, Hkv, d, dtype, scale):
+    desc = AttnDescT(Hq, Hkv, d, _DTYPES[dtype], float(scale), 0, 0)
+    return int(load().dsbd_chunk_attention_paged_workspace(chunk.address, C.addressof(desc)))
+
+
+def chunk_attention_launches(chunk, Hq, Hkv, d, dtype, scale):
+    desc = AttnDescT(Hq, Hkv, d, _DTYPES[dtype], float(scale), 0, 0)
+    return int(load().dsbd_chunk_attention_paged_launches(chunk.address, C.addressof(desc)))
+
+
+def chunk_attention_paged(chunk, Hq, Hkv, d, scale, q, k_pool, v_pool, out=None, workspace=None, status=None, stream=None):
+    """dsbd_chunk_attention_paged; q [total_new, Hq, d], pools [n_pages, Hkv, 64, d] that hold the chunk already (see
+    kv_append_paged); returns (out, status)."""
+    _require_cuda(q, k_pool, v_pool)
+    assert q.shape == (chunk.total_new, Hq, d) and k_pool.shape[1] == Hkv and k_pool.shape[3] == d
+    assert q.dtype == k_pool.dtype
+    pages = chunk.pages(k_pool, v_pool)
+    desc = AttnDescT(Hq, Hkv, d, _DTYPES[q.dtype], float(scale), 0, 0)
+    if out is None:
+        out = torch.empty_like(q)
+    if workspace is None:
+        workspace = _workspace(load().dsbd_chunk_attention_paged_workspace(chunk.address, C.addressof(desc)), q.device)
+    status = _status(status, q.device)
+    assert out.shape == q.shape and out.dtype == q.dtype
+    rc = load().dsbd_chunk_attention_paged(chunk.address, C.addressof(desc), _ptr(q), k_pool.data_ptr(), v_pool.data_ptr(),
+                                           C.addressof(pages), _ptr(out), workspace.data_ptr(), workspace.numel(),
+                                           _ptr(status), _stream(stream))
+    if rc != OK:
+        raise DsbdError("dsbd_chunk_attention_paged", rc)
+    return out, status
