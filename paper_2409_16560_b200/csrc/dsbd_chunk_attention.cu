@@ -45,8 +45,8 @@ constexpr int kWarpTma = 8, kWarpMma = 9;
 constexpr uint32_t kHalf = kTile * 128;              // bytes of 64 columns of a tile
 constexpr uint32_t kTmemCols = 512, kColS = 0, kColO = 256;
 constexpr float kMoveRef = 8.f;
-// Registers: launched with 168 a thread (64512); 256 softmax threads of 208 and 128 others of 88 are as many.
-constexpr int kSoftmaxRegs = 208, kOtherRegs = 88;
+// Registers: launched with 168 a thread (64512); 256 softmax threads of 232 and 128 others of 40 are as many.
+constexpr int kSoftmaxRegs = 232, kOtherRegs = 40;
 static_assert(kSoftmaxRegs * 256 + kOtherRegs * 128 <= 168 * kThreads, "no more than at launch");
 #ifdef DSBD_TEST_WAIT_TIMEOUT
 constexpr uint32_t kWaitTries = 250;                 // test build: see dsbd_attention_tr.cu
