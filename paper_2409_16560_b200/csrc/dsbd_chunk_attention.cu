@@ -40,14 +40,15 @@ namespace {
 
 constexpr int kTile = 128;                           // tokens of a tile, rows of a row tile
 constexpr int kPages = kTile / kBN;                  // pages of a tile
-constexpr int kThreads = 384;                        // two softmax warpgroups, one with producer and issuer
-constexpr int kWarpTma = 8, kWarpMma = 9;
+constexpr int kPartRows = 2 * kTile;                 // rows of a unit
+constexpr int kThreads = 512;                        // two softmax warpgroups, the output's, one with producer and issuer
+constexpr int kWarpOut = 8, kWarpTma = 12, kWarpMma = 13;      // kWarpMma + X issues the products of row tile X
 constexpr uint32_t kHalf = kTile * 128;              // bytes of 64 columns of a tile
 constexpr uint32_t kTmemCols = 512, kColS = 0, kColO = 256;
 constexpr float kMoveRef = 8.f;
-// Registers: launched with 168 a thread (64512); 256 softmax threads of 232 and 128 others of 40 are as many.
-constexpr int kSoftmaxRegs = 232, kOtherRegs = 40;
-static_assert(kSoftmaxRegs * 256 + kOtherRegs * 128 <= 168 * kThreads, "no more than at launch");
+// Registers: launched with 128 a thread; the softmax warpgroups take what the others leave.
+constexpr int kSoftmaxRegs = 192, kOutRegs = 72, kOtherRegs = 56;
+static_assert(kSoftmaxRegs * 256 + kOutRegs * 128 + kOtherRegs * 128 <= 128 * kThreads, "no more than at launch");
 #ifdef DSBD_TEST_WAIT_TIMEOUT
 constexpr uint32_t kWaitTries = 250;                 // test build: see dsbd_attention_tr.cu
 #else
@@ -59,7 +60,7 @@ struct Shape {
     static constexpr int kHalves = D / 64;
     static constexpr uint32_t kSlot = kHalves * kHalf;          // a K or V tile; the rows of a row tile
     static constexpr int kSlots = D == 128 ? 5 : 8;
-    static constexpr uint32_t kSmem = 1024 + 2 * kSlot + kSlots * kSlot;
+    static constexpr uint32_t kSmem = 2 * kSlot + kSlots * kSlot;
 };
 
 struct ChunkArgs {
@@ -73,9 +74,11 @@ struct ChunkArgs {
     const int32_t *new_off, *page_table;
     const int64_t *prefix_off, *page_off;
     __nv_bfloat16 *out;
+    int out32;                                       // out is 32-byte aligned
     int32_t *status;
     struct CutRec *recs;                             // [grid]
-    float *partial;                                  // [2 * grid][256][D + 2]: reference, row sum, O
+    // what parts of units leave, run i's in slot 2 i (a unit that an earlier run began) and 2 i + 1 (one that it began):
+    float *part_ml, *part_o;                         // [2 * grid][kPartRows][2] reference and row sum, [..][D] O
 };
 
 // A place in the work: unit (b, g, q) and a tile of it.
@@ -171,13 +174,13 @@ __device__ __forceinline__ uint32_t seq_v(int i, int nt, int ahead) {
 }
 
 struct Shared {
-    unsigned long long full[8], empty[8], s_full[2], p_full[2], o_full[2], q_full, q_empty, b_done, b_free, drain;
+    unsigned long long full[2][8], empty[8], s_full[2], p_full[2][2], ml_full[2], o_full[2], o_free[2], turn[2], q_full, q_empty, drain[2];
     uint32_t tmem_base;
     int abort;
     Pos start, end;
     int64_t scan[kThreads / 32], mine[2];
     int found_b[2];
-    float ml[2][kTile];                              // reference and row sum of the narrow units' second half
+    float2 ml[2][kTile];                             // [X] reference and row sum of the rows
 };
 
 __device__ __forceinline__ bool warp_wait(void *bar, uint32_t parity, Shared *sh) {
@@ -191,6 +194,38 @@ __device__ __forceinline__ bool warp_wait(void *bar, uint32_t parity, Shared *sh
         }
     return __all_sync(kFull, ok);
 }
+
+__device__ __forceinline__ void tmem_ld16(uint32_t taddr, uint32_t (&v)[16]) {
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
+        : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7]),
+          "=r"(v[8]), "=r"(v[9]), "=r"(v[10]), "=r"(v[11]), "=r"(v[12]), "=r"(v[13]), "=r"(v[14]), "=r"(v[15])
+        : "r"(taddr) : "memory");
+}
+__device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&v)[16]) {
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};"
+        ::"r"(taddr), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]),
+          "r"(v[8]), "r"(v[9]), "r"(v[10]), "r"(v[11]), "r"(v[12]), "r"(v[13]), "r"(v[14]), "r"(v[15])
+        : "memory");
+}
+// 32 bytes a lane (32-byte aligned): a warp's rows lie far apart, so a store instruction costs a line per lane.
+__device__ __forceinline__ void st_32b(void *p, const uint32_t (&v)[8]) {
+    asm volatile("st.global.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};"
+                 ::"l"(p), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]) : "memory");
+}
+
+// The tile with number `seq` of the ring: its slot, the barrier that its copies complete, the phase of that one.  A slot has two such
+// barriers, for its fillings in turn: a warp that does not use every tile (narrow units) may wait for a filling while the
+// one before it, the other row tile's, is still on its way (copies land in any order), and the parity of one barrier could
+// not tell the two apart.  The filling before that one has landed and been used by then: the slot was filled again.
+template <int SLOTS>
+struct Tile {
+    uint32_t slot, filling;
+    __device__ __forceinline__ explicit Tile(uint32_t seq) : slot(seq % SLOTS), filling(seq / SLOTS) {}
+    __device__ __forceinline__ void *full(Shared *sh) const { return &sh->full[filling & 1][slot]; }
+    __device__ __forceinline__ uint32_t parity() const { return (filling >> 1) & 1; }
+};
 
 struct F2 { float x, y; };
 __device__ __forceinline__ F2 fma2(F2 a, F2 b, F2 c) {
@@ -212,6 +247,25 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
     asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
     return d;
 }
+
+// 2^z for z <= 120 on the FMA and integer pipes, which are idle while ex2 (a quarter of a warp's lanes a cycle) sets the pace:
+// z = n + f with n the nearest integer (what 1.5 * 2^23 leaves in the low bits), 2^f by a cubic fitted to the smallest relative
+// error on [-1/2, 1/2] with 1 at f = 0 (1.0e-4; the weights are rounded to bf16, 3.9e-3), n into the exponent.
+// From -127 down, -infinity included, the result is 0.
+__device__ __forceinline__ F2 exp2_poly(F2 z) {
+    const F2 big = {12582912.f, 12582912.f};
+    z.x = fmaxf(z.x, -127.f);
+    z.y = fmaxf(z.y, -127.f);
+    const F2 r = add2(z, big);
+    const F2 n = add2(r, F2{-12582912.f, -12582912.f});
+    const F2 f = fma2(n, F2{-1.f, -1.f}, z);
+    F2 p = fma2(f, F2{0.05500893294811249f, 0.05500893294811249f}, F2{0.2422109693288803f, 0.2422109693288803f});
+    p = fma2(p, f, F2{0.6932829022407532f, 0.6932829022407532f});
+    p = fma2(p, f, F2{1.f, 1.f});
+    return F2{__uint_as_float(__float_as_uint(p.x) + (__float_as_uint(r.x) << 23)),
+              __uint_as_float(__float_as_uint(p.y) + (__float_as_uint(r.y) << 23))};
+}
+constexpr int kPolyOf8 = 2;                          // of eight pairs of weights, those taken by exp2_poly
 
 // The CTA's run: all threads.  Returns through sh.start, sh.end; the sequences' facts are checked here, once a launch.
 __device__ void find_run(const ChunkArgs &a, Shared &sh) {
@@ -288,20 +342,26 @@ __global__ void __launch_bounds__(kThreads, 1)
 k_chunk_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v,
              const __grid_constant__ CUtensorMap map_q, ChunkArgs a) {
     using S = Shape<D>;
-    extern __shared__ unsigned char smem_raw[];
-    unsigned char *smem = smem_raw + ((1024 - (smem_u32(smem_raw) & 1023)) & 1023);    // swizzled operands
+    extern __shared__ __align__(1024) unsigned char smem[];
     unsigned char *q_s = smem, *ring = smem + 2 * S::kSlot;
     __shared__ Shared sh;
     const int warp = __shfl_sync(kFull, (int)(threadIdx.x >> 5), 0), lane = threadIdx.x & 31;
+    if ((smem_u32(smem) & 1023u) != 0u) {                    // the swizzled operands need 1024-byte alignment
+        if (threadIdx.x == 0) report(a.status, DSBD_DEV_BAD_CHUNK);
+        if (threadIdx.x == 0 && a.recs) a.recs[blockIdx.x] = CutRec{};
+        return;
+    }
+    static_assert(sizeof(Shared) <= 3072 && 3072 + S::kSmem <= 227 * 1024, "both in the shared memory of a block");
 
     if (threadIdx.x == 0) {
-        for (int s = 0; s < S::kSlots; ++s) { mbar_init(&sh.full[s], 1); mbar_init(&sh.empty[s], 1); }
-        for (int x = 0; x < 2; ++x) { mbar_init(&sh.s_full[x], 1); mbar_init(&sh.p_full[x], 4); mbar_init(&sh.o_full[x], 1); }
+        for (int s = 0; s < S::kSlots; ++s) { mbar_init(&sh.full[0][s], 1); mbar_init(&sh.full[1][s], 1); mbar_init(&sh.empty[s], 2); }
+        for (int x = 0; x < 2; ++x) {
+            mbar_init(&sh.s_full[x], 1); mbar_init(&sh.p_full[x][0], 4); mbar_init(&sh.p_full[x][1], 4);
+            mbar_init(&sh.drain[x], 1); mbar_init(&sh.turn[x], 1);
+            mbar_init(&sh.ml_full[x], 4); mbar_init(&sh.o_full[x], 1); mbar_init(&sh.o_free[x], 4);
+        }
         mbar_init(&sh.q_full, 1);
-        mbar_init(&sh.q_empty, 1);
-        mbar_init(&sh.b_done, 4);
-        mbar_init(&sh.b_free, 4);
-        mbar_init(&sh.drain, 1);
+        mbar_init(&sh.q_empty, 2);
         sh.abort = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
@@ -311,6 +371,7 @@ k_chunk_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
     }
     asm volatile("griddepcontrol.wait;" ::: "memory");
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     find_run(a, sh);
     tc_fence_before();
     __syncthreads();
@@ -327,9 +388,11 @@ k_chunk_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
         a.recs[blockIdx.x] = r;
     }
 
-    if (warp >= 8) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
     Walk w;
-    w.start(a, sh.start, sh.end);
+    if (warp >= kWarpTma) {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
+        w.start(a, sh.start, sh.end);
+    }
     if (warp == kWarpTma) {
         // ------------------------------------------------------------ copies
         uint32_t seq = 0, part = 0;
@@ -339,17 +402,7 @@ k_chunk_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
             const int t0 = w.at.t, nt = w.last_tile(u) - t0, g = w.at.g;
             if (nt <= 0) continue;
             const int ahead = u.wide ? 1 : 2;
-            if (part > 0) ok = warp_wait(&sh.q_empty, (part - 1) & 1, &sh);
-            if (!ok) break;
-            ++part;
             const bool on = lane == 0;
-            const int tiles = u.wide ? 2 : 1;
-            mbar_expect_tx_if(on, &sh.q_full, (uint32_t)(tiles * a.box_tokens * a.group * D * 2));
-            for (int x = 0; x < tiles; ++x)
-#pragma unroll
-                for (int h = 0; h < S::kHalves; ++h)
-                    tma_load_3d(on, smem_u32(q_s + x * S::kSlot + h * kHalf), &map_q, h * 64, g * a.group,
-                                u.first + u.i0 + x * a.tile_tokens, &sh.q_full);
             // K and V of a sequence with one block of rows pass once
             uint64_t policy;
             if (w.nq == 1) asm volatile("createpolicy.fractional.L2::evict_first.b64 %0, 1.0;" : "=l"(policy));
@@ -375,11 +428,11 @@ k_chunk_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
             auto copy = [&](const CUtensorMap *map, int tile, int &ids, int &at) {
                 const int p = (t0 + tile) * kPages;
                 if (p >= at + 32) { at = p; ids = fetch(p); }
-                const int s = seq % S::kSlots;
-                if (!warp_wait(&sh.empty[s], ((seq / S::kSlots) & 1) ^ 1, &sh)) { ok = false; return; }
+                const Tile<S::kSlots> to(seq);
+                if (!warp_wait(&sh.empty[to.slot], (to.filling & 1) ^ 1, &sh)) { ok = false; return; }
                 const int boxes = min(kPages, p_end - p);
-                mbar_expect_tx_if(on, &sh.full[s], (uint32_t)boxes * kBN * D * 2);
-                const uint32_t dst = smem_u32(ring + s * S::kSlot);
+                mbar_expect_tx_if(on, to.full(&sh), (uint32_t)boxes * kBN * D * 2);
+                const uint32_t dst = smem_u32(ring + to.slot * S::kSlot);
 #ifdef DSBD_TEST_WAIT_TIMEOUT
                 const bool there = !(seq == 1 && blockIdx.x == 0);       // the bytes this barrier expects never come
 #else
@@ -390,124 +443,195 @@ k_chunk_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
                     const int y = id < 0 ? INT32_MAX - 2 * kBN : (id * a.Hkv + g) * kBN;      // (past the pool: zeros)
 #pragma unroll
                     for (int h = 0; h < S::kHalves; ++h)
-                        tma_load_2d_hint(on && there, dst + h * kHalf + k * (kBN * 128), map, h * 64, y, &sh.full[s], policy);
+                        tma_load_2d_hint(on && there, dst + h * kHalf + k * (kBN * 128), map, h * 64, y, to.full(&sh), policy);
                 }
                 ++seq;
             };
+            // the first tiles do not wait for the query rows of the part before to be done with
             for (int i = 0; i < min(ahead, nt) && ok; ++i) copy(&map_k, i, ids_k, base_k);
+            if (ok) copy(&map_v, 0, ids_v, base_v);
+            if (ok && part > 0) ok = warp_wait(&sh.q_empty, (part - 1) & 1, &sh);
+            if (!ok) break;
+            ++part;
+            const int tiles = u.wide ? 2 : 1;
+            mbar_expect_tx_if(on, &sh.q_full, (uint32_t)(tiles * a.box_tokens * a.group * D * 2));
+            for (int x = 0; x < tiles; ++x)
+#pragma unroll
+                for (int h = 0; h < S::kHalves; ++h)
+                    tma_load_3d(on, smem_u32(q_s + x * S::kSlot + h * kHalf), &map_q, h * 64, g * a.group,
+                                u.first + u.i0 + x * a.tile_tokens, &sh.q_full);
             for (int i = 0; i < nt && ok; ++i) {
-                copy(&map_v, i, ids_v, base_v);
+                if (i > 0) copy(&map_v, i, ids_v, base_v);
                 if (ok && i + ahead < nt) copy(&map_k, i + ahead, ids_k, base_k);
             }
         }
         if (!ok) {
             // let the copies already issued land before the CTA goes away
             for (uint32_t k = 0; k < (uint32_t)S::kSlots && k < seq; ++k) {
-                const uint32_t t = seq - 1 - k;
-                for (uint32_t i = 0; i < kWaitTries && !mbar_try(&sh.full[t % S::kSlots], (t / S::kSlots) & 1); ++i) {}
+                const Tile<S::kSlots> t(seq - 1 - k);
+                for (uint32_t i = 0; i < kWaitTries && !mbar_try(t.full(&sh), t.parity()); ++i) {}
             }
             if (part > 0)
                 for (uint32_t i = 0; i < kWaitTries && !mbar_try(&sh.q_full, (part - 1) & 1); ++i) {}
         }
-    } else if (warp == kWarpMma) {
+    } else if (warp == kWarpMma || warp == kWarpMma + 1) {
         // ------------------------------------------------------------ products
+        const int x = warp - kWarpMma;
         const bool on = lane == 0;
         constexpr uint32_t idesc_s = instr_desc(kTile, kTile, 0, 0);
         constexpr uint32_t idesc_o = instr_desc(kTile, D, 0, 1);
-        uint32_t base = 0, part = 0, np[2] = {0, 0};
+        const uint32_t s_col = tmem + kColS + x * kTile, o_col = tmem + kColO + x * D;
+        uint32_t base = 0, part = 0, np = 0, turns = 0;
         bool ok = true;
         auto slot_wait = [&](uint32_t seq) -> uint32_t {
-            const uint32_t s = seq % S::kSlots;
-            ok = warp_wait(&sh.full[s], (seq / S::kSlots) & 1, &sh);
-            return s;
+            const Tile<S::kSlots> t(seq);
+            ok = warp_wait(t.full(&sh), t.parity(), &sh);
+            return t.slot;
+        };
+        // a slot is free when both warps have told so: in narrow units the one that uses it tells for both
+        auto release = [&](void *bar, bool twice) {
+            tc_commit(on, bar);
+            if (twice) tc_commit(on, bar);
         };
         for (; ok && w.more(); w.next(a, a.Hkv)) {
             const Unit u = unit_of(a, w.s, w.at.q);
             const int nt = w.last_tile(u) - w.at.t;
             if (nt <= 0) continue;
-            const int ahead = u.wide ? 1 : 2, steps = u.wide ? 2 * nt : nt;
-            int left = steps;                        // S products to come
+            const int ahead = u.wide ? 1 : 2, step = ahead;
             ok = warp_wait(&sh.q_full, part & 1, &sh);
-            auto product_s = [&](int x, int i) {
-                const uint32_t s = slot_wait(base + seq_k(i, ahead));
-                if (!ok) return;
-                tc_fence_after();
-                const uint64_t qd = desc_k_major(smem_u32(q_s + (u.wide ? x : 0) * S::kSlot));
+            const uint64_t qd = desc_k_major(smem_u32(q_s + (u.wide ? x : 0) * S::kSlot));
+            // Wide units: the row tiles take turns, so that one's products run while the other's softmax does (left alone they fall
+            // into step, and the tensor cores idle while both work on their rows).
+            auto take_turn = [&] {
+                if (u.wide && ok && (x == 1 || turns > 0)) ok = warp_wait(&sh.turn[x], (x == 1 ? turns : turns - 1) & 1, &sh);
+            };
+            auto pass_turn = [&] {
+                if (!u.wide) return;
+                if (on) mbar_arrive(&sh.turn[x ^ 1]);
+                ++turns;
+            };
+            auto product_s = [&](uint32_t s, int i) {
                 const uint64_t kd = desc_k_major(smem_u32(ring + s * S::kSlot));
 #pragma unroll
                 for (int ks = 0; ks < D / 16; ++ks) {
                     const uint64_t at = (uint64_t)((ks / 4) * (kHalf >> 4) + (ks % 4) * 2);
-                    mma_ss(on, tmem + kColS + x * kTile, qd + at, kd + at, idesc_s, ks > 0);
+                    mma_ss(on, s_col, qd + at, kd + at, idesc_s, ks > 0);
                 }
                 tc_commit(on, &sh.s_full[x]);
-                if (!u.wide || x == 1) tc_commit(on, &sh.empty[s]);
-                if (--left == 0) tc_commit(on, &sh.q_empty);
+                pass_turn();
+                release(&sh.empty[s], !u.wide);
+                if (i + step >= nt) tc_commit(on, &sh.q_empty);          // the row tile's last S
             };
-            for (int x = 0; x < min(2, steps) && ok; ++x) product_s(x, u.wide ? 0 : x);
-            for (int st = 0; st < steps && ok; ++st) {
-                const int x = st & 1, i = u.wide ? st >> 1 : st;
-                const uint32_t s = slot_wait(base + seq_v(i, nt, ahead));
-                if (!ok) break;
-                ok = warp_wait(&sh.p_full[x], np[x] & 1, &sh);
-                if (!ok) break;
-                ++np[x];
+            int i = u.wide ? 0 : x;
+            if (ok && i < nt) {
+                const uint32_t s = slot_wait(base + seq_k(i, ahead));
                 tc_fence_after();
-                const uint64_t vd = desc_mn_major(smem_u32(ring + s * S::kSlot), kHalf);
-                const bool fresh = u.wide ? i == 0 : i < 2;
+                take_turn();
+                if (ok) product_s(s, i);
+            }
+            // (the accumulators of the part before have been read; every part waits, so that no phase is missed)
+            if (ok && part > 0) ok = warp_wait(&sh.o_free[x], (part - 1) & 1, &sh);
+            if (ok && i >= nt) {                                         // no tile of this parity
+                if (on) { mbar_arrive(&sh.q_empty); mbar_arrive(&sh.o_full[x]); }
+                __syncwarp();
+            }
+            for (; i < nt && ok; i += step) {
+                const uint32_t sv = slot_wait(base + seq_v(i, nt, ahead));
+                // wide: K is there before P, so that nothing holds the next S up; narrow: K comes when it comes
+                uint32_t sk = 0;
+                const bool more = i + step < nt;
+                if (ok && u.wide && more) sk = slot_wait(base + seq_k(i + step, ahead));
+                const bool fresh = i < step;
+                if (!ok) break;
+                const uint64_t vd = desc_mn_major(smem_u32(ring + sv * S::kSlot), kHalf);
 #pragma unroll
-                for (int ks = 0; ks < kTile / 16; ++ks)
-                    mma_ts(on, tmem + kColO + x * D, tmem + kColS + x * kTile + ks * 8, vd + (uint64_t)(ks * ((16 * 128) >> 4)),
-                           idesc_o, (!fresh || ks > 0) ? 1u : 0u);
-                if (!u.wide || x == 1) tc_commit(on, &sh.empty[s]);
-                if (i + ahead < nt) product_s(x, i + ahead);
-                else tc_commit(on, &sh.o_full[x]);
+                for (int h = 0; h < 2; ++h) {                // the first half of P may come while the second is worked out
+                    if (ok) ok = warp_wait(&sh.p_full[x][h], np & 1, &sh);
+                    if (h == 1) take_turn();
+                    if (!ok) break;
+                    tc_fence_after();
+#pragma unroll
+                    for (int ks = h * kTile / 32; ks < (h + 1) * kTile / 32; ++ks)
+                        mma_ts(on, o_col, s_col + ks * 8, vd + (uint64_t)(ks * ((16 * 128) >> 4)), idesc_o, (!fresh || ks > 0) ? 1u : 0u);
+                }
+                if (!ok) break;
+                ++np;
+                release(&sh.empty[sv], !u.wide);
+                if (!more) {
+                    tc_commit(on, &sh.o_full[x]);
+                    pass_turn();
+                    continue;
+                }
+                if (!u.wide) {
+                    sk = slot_wait(base + seq_k(i + step, ahead));
+                    if (!ok) break;
+                    tc_fence_after();
+                }
+                product_s(sk, i + step);
             }
             base += 2 * nt;
             ++part;
         }
-        if (!ok) {
-            tc_commit(on, &sh.drain);
-            uint32_t i = 0;
-            while (!__all_sync(kFull, mbar_try(&sh.drain, 0)) && i < kWaitTries) ++i;
-        }
-    } else if (warp < 8) {
+        // the block's shared memory outlives every arrival that the products have yet to make
+        tc_commit(on, &sh.drain[x]);
+        uint32_t i = 0;
+        while (!__all_sync(kFull, mbar_try(&sh.drain[x], 0)) && i < kWaitTries) ++i;
+    } else if (warp < kWarpOut) {
         // ------------------------------------------------------------ softmax
         asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kSoftmaxRegs));
+        w.start(a, sh.start, sh.end);
         const int x = warp >> 2, row = (warp & 3) * 32 + lane;
         const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
         const uint32_t s_addr = tmem + lanes + kColS + x * kTile, o_addr = tmem + lanes + kColO + x * D;
-        const int token = row / a.group, head = row - token * a.group;
-        uint32_t base = 0, ns = 0, no = 0, narrow = 0;
+        const int token = row / a.group;
+        uint32_t base = 0, ns = 0, part = 0;
         bool ok = true;
         for (; ok && w.more(); w.next(a, a.Hkv)) {
             const Unit u = unit_of(a, w.s, w.at.q);
             const int t0 = w.at.t, nt = w.last_tile(u) - t0;
             if (nt <= 0) continue;
-            const int ahead = u.wide ? 1 : 2;
             const int i0 = u.i0 + (u.wide ? x * a.tile_tokens : 0);          // the row tile's first token
             const int left = min(a.tile_tokens, u.n - i0);                   // its tokens
-            const bool active = token < left;
             const bool work = (warp & 3) * 32 < left * a.group;              // some row of the warp
-            const int64_t sees = u.L + i0 + token + 1;                       // tokens the row sees
-            const int64_t all_see = u.L + i0 + 1;                            // every row of the tile
-            const int step = u.wide ? 1 : 2, mine = u.wide ? nt : (nt - x + 1) / 2;
+            // in tokens of the part: what this row sees, what every row of the tile sees, the block's end
+            const int all_see = (int)(u.L - (int64_t)t0 * kTile) + i0 + 1, sees = all_see + token;
+            const int end = (int)(u.end - (int64_t)t0 * kTile);
+            const int step = u.wide ? 1 : 2;
             float m_ref = -INFINITY, l = 0.f;
             for (int i = u.wide ? 0 : x; i < nt; i += step) {
                 ok = warp_wait(&sh.s_full[x], ns & 1, &sh);
                 if (!ok) break;
                 ++ns;
                 tc_fence_after();
-                const int64_t tok0 = (int64_t)(t0 + i) * kTile;
+                // what lies behind the block's last token has weight zero: its values become zeros
+                if ((i + 1) * kTile > end && (x == 0 || !u.wide)) {
+                    const Tile<S::kSlots> v(base + seq_v(i, nt, u.wide ? 1 : 2));
+                    ok = warp_wait(v.full(&sh), v.parity(), &sh);
+                    if (!ok) break;
+                    if (row >= end - i * kTile) {
+#pragma unroll
+                        for (int h = 0; h < S::kHalves; ++h) {
+                            uint4 *line = reinterpret_cast<uint4 *>(ring + v.slot * S::kSlot + h * kHalf + row * 128);
+#pragma unroll
+                            for (int e = 0; e < 8; ++e) line[e] = make_uint4(0, 0, 0, 0);
+                        }
+                    }
+                    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                }
                 if (work) {
                     uint32_t sv[4][32];
 #pragma unroll
                     for (int c = 0; c < 4; ++c) tmem_ld32(s_addr + c * 32, sv[c]);
                     tmem_wait_ld();
-                    if (tok0 + kTile > all_see) {
-                        const int lim = (int)min((int64_t)kTile, max((int64_t)0, sees - tok0));
+                    if ((i + 1) * kTile > all_see) {
 #pragma unroll
-                        for (int c = 0; c < kTile; ++c)
-                            if (c >= lim) sv[c >> 5][c & 31] = 0xff800000u;      // -inf: weight 0
+                        for (int c = 0; c < 4; ++c) {
+                            const int lim = min(max(sees - i * kTile - c * 32, 0), 32);
+                            const uint32_t vis = lim == 32 ? ~0u : (1u << lim) - 1;
+#pragma unroll
+                            for (int e = 0; e < 32; ++e)
+                                if (!((vis >> e) & 1u)) sv[c][e] = 0xff800000u;      // -inf: weight 0
+                        }
                     }
                     float m4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
@@ -522,13 +646,13 @@ k_chunk_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
                         l *= f;
                         if (i >= step) {
 #pragma unroll 1
-                            for (int c = 0; c < D; c += 32) {
-                                uint32_t ov[32];
-                                tmem_ld32(o_addr + c, ov);
+                            for (int c = 0; c < D; c += 16) {
+                                uint32_t ov[16];
+                                tmem_ld16(o_addr + c, ov);
                                 tmem_wait_ld();
 #pragma unroll
-                                for (int e = 0; e < 32; ++e) ov[e] = __float_as_uint(__uint_as_float(ov[e]) * f);
-                                tmem_st32(o_addr + c, ov);
+                                for (int e = 0; e < 16; ++e) ov[e] = __float_as_uint(__uint_as_float(ov[e]) * f);
+                                tmem_st16(o_addr + c, ov);
                             }
                         }
                         m_ref = m_new;
@@ -536,124 +660,125 @@ k_chunk_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
                     const float neg = m_ref == -INFINITY ? 0.f : -m_ref;
                     F2 l2[2] = {{0.f, 0.f}, {0.f, 0.f}};
 #pragma unroll
-                    for (int c = 0; c < 2; ++c) {
-                        uint32_t pv[32];
+                    for (int c = 0; c < 4; ++c) {
+                        uint32_t pv[16];
 #pragma unroll
-                        for (int e = 0; e < 32; ++e) {
-                            const int at = c * 64 + 2 * e;
-                            const F2 z = fma2(F2{__uint_as_float(sv[at >> 5][at & 31]), __uint_as_float(sv[at >> 5][(at & 31) + 1])},
+                        for (int e = 0; e < 16; ++e) {
+                            const F2 z = fma2(F2{__uint_as_float(sv[c][2 * e]), __uint_as_float(sv[c][2 * e + 1])},
                                               F2{a.scale_log2, a.scale_log2}, F2{neg, neg});
-                            pv[e] = pack_bf16(ex2_ftz(z.x), ex2_ftz(z.y));
-                            l2[e & 1] = add2(l2[e & 1], F2{bf16_lo(pv[e]), bf16_hi(pv[e])});
+                            const F2 w2 = e % 8 < kPolyOf8 ? exp2_poly(z) : F2{ex2_ftz(z.x), ex2_ftz(z.y)};
+                            pv[e] = pack_bf16(w2.x, w2.y);
+                            l2[e & 1] = add2(l2[e & 1], w2);
                         }
-                        tmem_st32(s_addr + c * 32, pv);
+                        tmem_st16(s_addr + c * 16, pv);
+                        if (c & 1) {
+                            tmem_wait_st();
+                            tc_fence_before();
+                            __syncwarp();
+                            if (lane == 0) mbar_arrive(&sh.p_full[x][c >> 1]);
+                        }
                     }
                     l += (l2[0].x + l2[0].y) + (l2[1].x + l2[1].y);
-                    tmem_wait_st();
+                } else {
+                    tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) { mbar_arrive(&sh.p_full[x][0]); mbar_arrive(&sh.p_full[x][1]); }
                 }
-                // what lies behind the block's last token has weight zero: its values become zeros
-                if (tok0 + kTile > u.end && (x == 0 || !u.wide)) {
-                    const uint32_t sv = base + seq_v(i, nt, ahead), s = sv % S::kSlots;
-                    ok = warp_wait(&sh.full[s], (sv / S::kSlots) & 1, &sh);
-                    if (!ok) break;
-                    const int valid = (int)(u.end - tok0);
-                    if (row >= valid) {
-#pragma unroll
-                        for (int h = 0; h < S::kHalves; ++h) {
-                            uint4 *line = reinterpret_cast<uint4 *>(ring + s * S::kSlot + h * kHalf + row * 128);
-#pragma unroll
-                            for (int e = 0; e < 8; ++e) line[e] = make_uint4(0, 0, 0, 0);
-                        }
-                    }
-                    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-                }
-                // (the accumulators of a narrow unit's second half are free once the first group has read them)
-                if (x == 1 && i < step && narrow > 0) {
-                    ok = warp_wait(&sh.b_free, (narrow - 1) & 1, &sh);
-                    if (!ok) break;
-                }
-                tc_fence_before();
-                __syncwarp();
-                if (lane == 0) mbar_arrive(&sh.p_full[x]);
             }
             if (!ok) break;
             base += 2 * nt;
-            if (mine > 0) {
-                ok = warp_wait(&sh.o_full[x], no & 1, &sh);
-                if (!ok) break;
-                ++no;
-                tc_fence_after();
-            }
-            // ---- the end of the unit, or of its part
-            float fo = 1.f, fb = 0.f;                        // factors of this tile's O and of the second half's
-            bool second = false;
-            if (!u.wide) {
-                if (x == 1) {
-                    // (the first group has read those of the narrow unit before)
-                    if (narrow > 0) ok = warp_wait(&sh.b_free, (narrow - 1) & 1, &sh);
-                    if (!ok) break;
-                    sh.ml[0][row] = m_ref;
-                    sh.ml[1][row] = l;
-                    tc_fence_before();
-                    __syncwarp();
-                    if (lane == 0) mbar_arrive(&sh.b_done);
-                    ++narrow;
-                    continue;
-                }
-                ok = warp_wait(&sh.b_done, narrow & 1, &sh);
-                if (!ok) break;
-                tc_fence_after();
-                second = nt > 1;
-                const float mb = sh.ml[0][row], lb = sh.ml[1][row];
-                const float m = fmaxf(m_ref, mb);
-                fo = m_ref == -INFINITY ? 0.f : exp2f(m_ref - m);
-                fb = mb == -INFINITY ? 0.f : exp2f(mb - m);
-                l = l * fo + lb * fb;
-                m_ref = m;
-            }
+            // the row's reference and sum for the output warps, which have read those of the part before
+            if (part > 0) ok = warp_wait(&sh.o_free[x], (part - 1) & 1, &sh);
+            if (!ok) break;
+            ++part;
+            sh.ml[x][row] = make_float2(m_ref, l);
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&sh.ml_full[x]);
+        }
+    } else if (warp < kWarpTma) {
+        // ------------------------------------------------------------ output
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOutRegs));
+        w.start(a, sh.start, sh.end);
+        const int row = (warp & 3) * 32 + lane;
+        const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16, o_addr = tmem + lanes + kColO;
+        const int token = row / a.group, head = row - token * a.group;
+        uint32_t part = 0;
+        bool ok = true;
+        for (; ok && w.more(); w.next(a, a.Hkv)) {
+            const Unit u = unit_of(a, w.s, w.at.q);
+            const int t0 = w.at.t, nt = w.last_tile(u) - t0;
+            if (nt <= 0) continue;
             const bool is_whole = t0 == 0 && nt == u.nt;
-            if (work) {
-                const int r = (u.wide ? x * a.tile_tokens * a.group : 0) + row;
-                float *part = nullptr;
+#pragma unroll 1
+            for (int x = 0; x < (u.wide ? 2 : 1) && ok; ++x) {
+                const int i0 = u.i0 + x * a.tile_tokens;
+                const bool active = token < min(a.tile_tokens, u.n - i0);
+                const bool second = !u.wide && nt > 1;
+                ok = warp_wait(&sh.ml_full[x], part & 1, &sh) && warp_wait(&sh.o_full[x], part & 1, &sh);
+                if (ok && !u.wide) ok = warp_wait(&sh.ml_full[1], part & 1, &sh) && warp_wait(&sh.o_full[1], part & 1, &sh);
+                if (!ok) break;
+                tc_fence_after();
+                float2 ml = sh.ml[x][row];
+                float fo = 1.f, fb = 0.f;                    // factors of this tile's O and of the narrow unit's other one
+                if (!u.wide) {
+                    const float2 mb = sh.ml[1][row];
+                    const float m = fmaxf(ml.x, mb.x);
+                    fo = ml.x == -INFINITY ? 0.f : exp2f(ml.x - m);
+                    fb = mb.x == -INFINITY ? 0.f : exp2f(mb.x - m);
+                    ml = make_float2(m, ml.y * fo + mb.y * fb);
+                }
+                const int64_t at = (2 * (int64_t)blockIdx.x + (t0 == 0 ? 1 : 0)) * kPartRows + x * a.tile_tokens * a.group + row;
+                float *part_o = a.part_o + at * D;
                 __nv_bfloat16 *dst = a.out + ((int64_t)(u.first + i0 + token) * a.Hq + w.at.g * a.group + head) * D;
                 if (is_whole) {
-                    const float inv = 1.f / l;
+                    const float inv = 1.f / ml.y;
                     fo *= inv; fb *= inv;
-                } else {
-                    part = a.partial + ((2 * (int64_t)blockIdx.x + (t0 == 0 ? 1 : 0)) * 256 + r) * (D + 2);
-                    if (active) { part[0] = m_ref; part[1] = l; }
+                } else if (active) {
+                    *reinterpret_cast<float2 *>(a.part_ml + at * 2) = ml;
                 }
 #pragma unroll 1
-                for (int c = 0; c < D; c += 32) {
-                    uint32_t ov[32], ow[32];
-                    tmem_ld32(o_addr + c, ov);
-                    if (second) tmem_ld32(o_addr + D + c, ow);
+                for (int c = 0; c < D; c += 16) {
+                    uint32_t ov[16], ow[16];
+                    tmem_ld16(o_addr + x * D + c, ov);
+                    if (second) tmem_ld16(o_addr + D + c, ow);
                     tmem_wait_ld();
-                    float o[32];
+                    if (c + 16 == D) {                       // all read
+                        tc_fence_before();
+                        __syncwarp();
+                        if (lane == 0) {
+                            mbar_arrive(&sh.o_free[x]);
+                            if (!u.wide) mbar_arrive(&sh.o_free[1]);
+                        }
+                    }
+                    float o[16];
 #pragma unroll
-                    for (int e = 0; e < 32; ++e) {
+                    for (int e = 0; e < 16; ++e) {
                         o[e] = __uint_as_float(ov[e]) * fo;
                         if (second) o[e] = fmaf(__uint_as_float(ow[e]), fb, o[e]);
                     }
                     if (active && is_whole) {
+                        uint32_t w8[8];
 #pragma unroll
-                        for (int e = 0; e < 32; e += 8)
-                            *reinterpret_cast<uint4 *>(dst + c + e) =
-                                make_uint4(pack_bf16(o[e], o[e + 1]), pack_bf16(o[e + 2], o[e + 3]),
-                                           pack_bf16(o[e + 4], o[e + 5]), pack_bf16(o[e + 6], o[e + 7]));
+                        for (int e = 0; e < 8; ++e) w8[e] = pack_bf16(o[2 * e], o[2 * e + 1]);
+                        if (a.out32) {
+                            st_32b(dst + c, w8);
+                        } else {
+                            *reinterpret_cast<uint4 *>(dst + c) = make_uint4(w8[0], w8[1], w8[2], w8[3]);
+                            *reinterpret_cast<uint4 *>(dst + c + 8) = make_uint4(w8[4], w8[5], w8[6], w8[7]);
+                        }
                     } else if (active) {
 #pragma unroll
-                        for (int e = 0; e < 32; e += 2) *reinterpret_cast<float2 *>(part + 2 + c + e) = make_float2(o[e], o[e + 1]);
+                        for (int e = 0; e < 16; e += 8) {
+                            uint32_t w8[8];
+#pragma unroll
+                            for (int k = 0; k < 8; ++k) w8[k] = __float_as_uint(o[e + k]);
+                            st_32b(part_o + c + e, w8);
+                        }
                     }
                     __syncwarp();
                 }
             }
-            tc_fence_before();
-            if (!u.wide) {
-                __syncwarp();
-                if (lane == 0) mbar_arrive(&sh.b_free);
-                ++narrow;
-            }
+            ++part;
         }
     }
     tc_fence_before();
@@ -665,50 +790,76 @@ k_chunk_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
     }
 }
 
-// Joins the parts of cut units: block (i, y) takes the unit that run i began and did not end, a warp to a row;
-// out = sum_p O_p 2^(m_p - m) / sum_p l_p 2^(m_p - m), the parts in the order of their runs.
-constexpr int kMergeThreads = 256, kMergeRows = 4;                       // rows of a warp
+// Joins the parts of cut units: block (i, y) takes rows of the unit that run i began and did not end, a warp to a row;
+// out = sum_p O_p 2^(m_p - m) / sum_p l_p 2^(m_p - m), the parts in the order of their runs.  A call's time here is the chain of
+// dependent loads, so the runs' records and the parts' references are read by a lane each, and the rows of O four at a time.
+constexpr int kMergeThreads = 256, kMergeRows = kMergeThreads / 32;
 template <int D>
 __global__ void __launch_bounds__(kMergeThreads)
 k_chunk_merge(ChunkArgs a, int runs) {
     asm volatile("griddepcontrol.wait;" ::: "memory");
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     const int i0 = blockIdx.x, lane = threadIdx.x & 31;
+    const int row = blockIdx.y * kMergeRows + (threadIdx.x >> 5);
     const CutRec rec = a.recs[i0];
+    int next = i0 + 1 + lane < runs ? a.recs[i0 + 1 + lane].head : 2;
     if (!rec.tail) return;
     const Seq s = seq_of(a, rec.b, false);
     const Unit u = unit_of(a, s, rec.q);
-    const int rows = u.tokens * a.group;
-    if ((int)blockIdx.y * (kMergeThreads / 32 * kMergeRows) >= rows) return;
-    int last = i0;
-    for (int h = 1; h == 1 && last + 1 < runs;) h = a.recs[++last].head;
-    constexpr int kPer = D / 32;
-    for (int k = 0; k < kMergeRows; ++k) {
-        const int row = (blockIdx.y * kMergeRows + k) * (kMergeThreads / 32) + (threadIdx.x >> 5);
-        if (row >= rows) return;
-        auto part = [&](int i) { return a.partial + ((2 * (int64_t)i + (i == i0 ? 1 : 0)) * 256 + row) * (D + 2); };
-        float m = -INFINITY;
-        for (int i = i0; i <= last; ++i)
-            if (i == i0 || a.recs[i].head) m = fmaxf(m, part(i)[0]);
-        float l = 0.f, o[kPer] = {};
-        for (int i = i0; i <= last; ++i) {
-            if (i != i0 && !a.recs[i].head) continue;
-            const float *src = part(i);
-            if (src[0] == -INFINITY) continue;
-            const float f = exp2f(src[0] - m);
-            l += src[1] * f;
-#pragma unroll
-            for (int e = 0; e < kPer; e += 2) {
-                const float2 v = *reinterpret_cast<const float2 *>(src + 2 + lane * kPer + e);
-                o[e] += v.x * f; o[e + 1] += v.y * f;
-            }
+    if (row >= u.tokens * a.group) return;
+    // the runs behind i0 that hold parts of the unit: those up to the first that ends it
+    int parts = 1;
+    for (;;) {
+        const unsigned ends = __ballot_sync(kFull, next != 1);
+        if (ends) {
+            const int k = __ffs(ends) - 1;
+            parts += k + (__shfl_sync(kFull, next, k) == 2 && i0 + parts + k < runs ? 1 : 0);
+            break;
         }
-        const float inv = 1.f / l;
-        const int token = row / a.group, head = row - token * a.group;
-        uint32_t *dst = reinterpret_cast<uint32_t *>(
-            a.out + ((int64_t)(u.first + u.i0 + token) * a.Hq + rec.g * a.group + head) * D + lane * kPer);
-#pragma unroll
-        for (int e = 0; e < kPer; e += 2) dst[e / 2] = pack_bf16(o[e] * inv, o[e + 1] * inv);
+        parts += 32;
+        next = i0 + parts + lane < runs ? a.recs[i0 + parts + lane].head : 2;
     }
+    constexpr int kPer = D / 32;
+    float m = -INFINITY, l = 0.f, o[kPer] = {};
+    for (int p0 = 0; p0 < parts; p0 += 32) {
+        const int n = min(32, parts - p0);
+        auto slot = [&](int p) { return 2 * (int64_t)(i0 + p0 + p) + (p0 + p == 0 ? 1 : 0); };
+        float2 ml = {-INFINITY, 0.f};
+        if (lane < n) ml = *reinterpret_cast<const float2 *>(a.part_ml + (slot(lane) * kPartRows + row) * 2);
+        const float m_new = fmaxf(m, warp_max(ml.x));
+        const float old = m == -INFINITY ? 0.f : exp2f(m - m_new);
+        const float f = ml.x == -INFINITY ? 0.f : exp2f(ml.x - m_new);
+        l = l * old + warp_sum(ml.y * f);
+#pragma unroll
+        for (int e = 0; e < kPer; ++e) o[e] *= old;
+        m = m_new;
+        for (int p = 0; p < n; p += 4) {
+            float v[4][kPer], w[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                w[k] = __shfl_sync(kFull, f, min(p + k, 31));
+                const float *src = a.part_o + (slot(min(p + k, n - 1)) * kPartRows + row) * D + lane * kPer;
+                if constexpr (kPer == 4) {
+                    const float4 t = *reinterpret_cast<const float4 *>(src);
+                    v[k][0] = t.x; v[k][1] = t.y; v[k][2] = t.z; v[k][3] = t.w;
+                } else {
+                    const float2 t = *reinterpret_cast<const float2 *>(src);
+                    v[k][0] = t.x; v[k][1] = t.y;
+                }
+            }
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+#pragma unroll
+                for (int e = 0; e < kPer; ++e)
+                    if (p + k < n && w[k] != 0.f) o[e] = fmaf(v[k][e], w[k], o[e]);
+        }
+    }
+    const float inv = 1.f / l;
+    const int token = row / a.group, head = row - token * a.group;
+    uint32_t *dst = reinterpret_cast<uint32_t *>(
+        a.out + ((int64_t)(u.first + u.i0 + token) * a.Hq + rec.g * a.group + head) * D + lane * kPer);
+#pragma unroll
+    for (int e = 0; e < kPer; e += 2) dst[e / 2] = pack_bf16(o[e] * inv, o[e + 1] * inv);
 }
 
 // Launch shape shared by the workspace query and the launch.
@@ -738,9 +889,11 @@ int check(const dsbd_chunk_t *c, const dsbd_attn_desc_t *d) {
     return DSBD_OK;
 }
 
+// Workspace: records, references and sums, accumulators.
+size_t recs_bytes(const Plan &p) { return align_up(sizeof(CutRec) * (size_t)p.grid, 256); }
+size_t ml_bytes(const Plan &p) { return sizeof(float) * 2 * 2 * (size_t)p.grid * kPartRows; }
 size_t workspace_of(const Plan &p, int d) {
-    if (p.whole) return 256;
-    return align_up(sizeof(CutRec) * (size_t)p.grid, 256) + align_up(sizeof(float) * 2 * (size_t)p.grid * 256 * (d + 2), 256);
+    return p.whole ? 256 : recs_bytes(p) + ml_bytes(p) + sizeof(float) * 2 * (size_t)p.grid * kPartRows * d;
 }
 
 template <int D>
@@ -760,8 +913,7 @@ int launch(const Plan &p, const CUtensorMap (&maps)[3], const ChunkArgs &a, cuda
     cfg.numAttrs = 1;
     if (cudaLaunchKernelEx(&cfg, k_chunk_attn<D>, maps[0], maps[1], maps[2], a) != cudaSuccess) return DSBD_ERR_CUDA;
     if (p.whole) return DSBD_OK;
-    const int per = kMergeThreads / 32 * kMergeRows;
-    cfg.gridDim = dim3((unsigned)p.grid, (unsigned)((p.block_rows + per - 1) / per));
+    cfg.gridDim = dim3((unsigned)p.grid, (unsigned)((p.block_rows + kMergeRows - 1) / kMergeRows));
     cfg.blockDim = dim3(kMergeThreads);
     cfg.dynamicSmemBytes = 0;
     return cudaLaunchKernelEx(&cfg, k_chunk_merge<D>, a, p.grid) == cudaSuccess ? DSBD_OK : DSBD_ERR_CUDA;
@@ -809,10 +961,13 @@ extern "C" int dsbd_chunk_attention_paged(const dsbd_chunk_t *c, const dsbd_attn
     a.max_len = c->max_len; a.n_pages = pages->n_pages;
     a.new_off = c->new_off; a.prefix_off = c->prefix_off; a.page_table = pages->page_table; a.page_off = pages->page_off;
     a.out = static_cast<__nv_bfloat16 *>(out);
+    a.out32 = (reinterpret_cast<uintptr_t>(out) & 31) == 0;
     a.status = status;
     if (!plan.whole) {
-        a.recs = static_cast<CutRec *>(workspace);
-        a.partial = reinterpret_cast<float *>(static_cast<unsigned char *>(workspace) + align_up(sizeof(CutRec) * (size_t)plan.grid, 256));
+        unsigned char *ws = static_cast<unsigned char *>(workspace);
+        a.recs = reinterpret_cast<CutRec *>(ws);
+        a.part_ml = reinterpret_cast<float *>(ws + recs_bytes(plan));
+        a.part_o = reinterpret_cast<float *>(ws + recs_bytes(plan) + ml_bytes(plan));
     }
     CUtensorMap maps[3];
     const uint64_t D = (uint64_t)d->d;

@@ -15,7 +15,12 @@ namespace {
 constexpr int kMaxRot = 128;
 constexpr int kThreads = 256;
 
-__device__ __forceinline__ void pdl_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+// Launched while the kernel before it may still run: wait for that one's results, then let the next one come (which waits
+// for these in turn).
+__device__ __forceinline__ void pdl_wait() {
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+}
 
 // ------------------------------------------------------------------------------------------ table
 struct Frequencies { double f[kMaxRot / 2]; };
