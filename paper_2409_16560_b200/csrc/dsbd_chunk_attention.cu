@@ -38,17 +38,14 @@ using namespace dsbd;
 
 namespace {
 
-constexpr int kTile = 128;                           // tokens of a tile, rows of a row tile
-constexpr int kPages = kTile / kBN;                  // pages of a tile
-constexpr int kPartRows = 2 * kTile;                 // rows of a unit
-constexpr int kThreads = 512;                        // two softmax warpgroups, the output's, one with producer and issuer
+constexpr int kRows = 128;                           // rows of a row tile
+constexpr int kTile = kBN;                           // tokens of a tile: a page
+constexpr int kPartRows = 2 * kRows;                 // rows of a unit
+constexpr int kThreads = 512;                        // two softmax warpgroups, the output's, one with producer and issuers
 constexpr int kWarpOut = 8, kWarpTma = 12, kWarpMma = 13;      // kWarpMma + X issues the products of row tile X
-constexpr uint32_t kHalf = kTile * 128;              // bytes of 64 columns of a tile
-constexpr uint32_t kTmemCols = 512, kColS = 0, kColO = 256;
+constexpr int kAhead = 2;                            // tiles that S runs ahead of O
+constexpr uint32_t kTmemCols = 512, kColS = 0, kColO = 256;    // S: [X][2 buffers][kTile]
 constexpr float kMoveRef = 8.f;
-// Registers: launched with 128 a thread; the softmax warpgroups take what the others leave.
-constexpr int kSoftmaxRegs = 192, kOutRegs = 72, kOtherRegs = 56;
-static_assert(kSoftmaxRegs * 256 + kOutRegs * 128 + kOtherRegs * 128 <= 128 * kThreads, "no more than at launch");
 #ifdef DSBD_TEST_WAIT_TIMEOUT
 constexpr uint32_t kWaitTries = 250;                 // test build: see dsbd_attention_tr.cu
 #else
@@ -58,9 +55,11 @@ constexpr uint32_t kWaitTries = 500000;              // about two seconds: a try
 template <int D>
 struct Shape {
     static constexpr int kHalves = D / 64;
-    static constexpr uint32_t kSlot = kHalves * kHalf;          // a K or V tile; the rows of a row tile
-    static constexpr int kSlots = D == 128 ? 5 : 8;
-    static constexpr uint32_t kSmem = 2 * kSlot + kSlots * kSlot;
+    static constexpr uint32_t kQHalf = kRows * 128, kQ = kHalves * kQHalf;       // 64 columns of a row tile; a row tile
+    static constexpr uint32_t kHalf = kTile * 128, kKv = kHalves * kHalf;        // 64 columns of a K or V tile; a tile
+    static constexpr uint32_t kStage = 2 * kKv;                                  // K then V
+    static constexpr int kStages = D == 128 ? 5 : 8;
+    static constexpr uint32_t kSmem = 2 * kQ + kStages * kStage;
 };
 
 struct ChunkArgs {
@@ -165,22 +164,14 @@ struct Walk {
     }
 };
 
-// Where the K and V tiles of a part of nt tiles lie in the order of the ring: `ahead` K tiles first (1 wide, 2 narrow),
-// then V tile i and K tile i + ahead in turn.
-__device__ __forceinline__ uint32_t seq_k(int i, int ahead) { return i < ahead ? i : 2 * i - ahead + 1; }
-__device__ __forceinline__ uint32_t seq_v(int i, int nt, int ahead) {
-    const int first = min(ahead, nt);
-    return first + i + min(i, nt - first);
-}
-
 struct Shared {
-    unsigned long long full[2][8], empty[8], s_full[2], p_full[2][2], ml_full[2], o_full[2], o_free[2], turn[2], q_full, q_empty, drain[2];
+    unsigned long long full[2][8], empty[8], s_full[2][2], p_full[2][2], ml_full[2], o_full[2], o_free[2], q_full, q_empty, drain[2];
     uint32_t tmem_base;
     int abort;
     Pos start, end;
     int64_t scan[kThreads / 32], mine[2];
     int found_b[2];
-    float2 ml[2][kTile];                             // [X] reference and row sum of the rows
+    float2 ml[2][kRows];                             // [X] reference and row sum of the rows
 };
 
 __device__ __forceinline__ bool warp_wait(void *bar, uint32_t parity, Shared *sh) {
@@ -215,14 +206,14 @@ __device__ __forceinline__ void st_32b(void *p, const uint32_t (&v)[8]) {
                  ::"l"(p), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]) : "memory");
 }
 
-// The tile with number `seq` of the ring: its slot, the barrier that its copies complete, the phase of that one.  A slot has two such
-// barriers, for its fillings in turn: a warp that does not use every tile (narrow units) may wait for a filling while the
+// Stage number `seq` of the ring: its slot, the barrier that its copies complete, the phase of that one.  A slot has two such
+// barriers, for its fillings in turn: a warp that does not use every stage (narrow units) may wait for a filling while the
 // one before it, the other row tile's, is still on its way (copies land in any order), and the parity of one barrier could
 // not tell the two apart.  The filling before that one has landed and been used by then: the slot was filled again.
-template <int SLOTS>
-struct Tile {
+template <int STAGES>
+struct Stage {
     uint32_t slot, filling;
-    __device__ __forceinline__ explicit Tile(uint32_t seq) : slot(seq % SLOTS), filling(seq / SLOTS) {}
+    __device__ __forceinline__ explicit Stage(uint32_t seq) : slot(seq % STAGES), filling(seq / STAGES) {}
     __device__ __forceinline__ void *full(Shared *sh) const { return &sh->full[filling & 1][slot]; }
     __device__ __forceinline__ uint32_t parity() const { return (filling >> 1) & 1; }
 };
@@ -342,8 +333,9 @@ __global__ void __launch_bounds__(kThreads, 1)
 k_chunk_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v,
              const __grid_constant__ CUtensorMap map_q, ChunkArgs a) {
     using S = Shape<D>;
+    using Stg = Stage<S::kStages>;
     extern __shared__ __align__(1024) unsigned char smem[];
-    unsigned char *q_s = smem, *ring = smem + 2 * S::kSlot;
+    unsigned char *q_s = smem, *ring = smem + 2 * S::kQ;
     __shared__ Shared sh;
     const int warp = __shfl_sync(kFull, (int)(threadIdx.x >> 5), 0), lane = threadIdx.x & 31;
     if ((smem_u32(smem) & 1023u) != 0u) {                    // the swizzled operands need 1024-byte alignment
@@ -354,11 +346,11 @@ k_chunk_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
     static_assert(sizeof(Shared) <= 3072 && 3072 + S::kSmem <= 227 * 1024, "both in the shared memory of a block");
 
     if (threadIdx.x == 0) {
-        for (int s = 0; s < S::kSlots; ++s) { mbar_init(&sh.full[0][s], 1); mbar_init(&sh.full[1][s], 1); mbar_init(&sh.empty[s], 2); }
+        for (int s = 0; s < S::kStages; ++s) { mbar_init(&sh.full[0][s], 1); mbar_init(&sh.full[1][s], 1); mbar_init(&sh.empty[s], 2); }
         for (int x = 0; x < 2; ++x) {
-            mbar_init(&sh.s_full[x], 1); mbar_init(&sh.p_full[x][0], 4); mbar_init(&sh.p_full[x][1], 4);
-            mbar_init(&sh.drain[x], 1); mbar_init(&sh.turn[x], 1);
+            for (int k = 0; k < 2; ++k) { mbar_init(&sh.s_full[x][k], 1); mbar_init(&sh.p_full[x][k], 4); }
             mbar_init(&sh.ml_full[x], 4); mbar_init(&sh.o_full[x], 1); mbar_init(&sh.o_free[x], 4);
+            mbar_init(&sh.drain[x], 1);
         }
         mbar_init(&sh.q_full, 1);
         mbar_init(&sh.q_empty, 2);
@@ -389,32 +381,27 @@ k_chunk_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
     }
 
     Walk w;
-    if (warp >= kWarpTma) {
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
-        w.start(a, sh.start, sh.end);
-    }
+    w.start(a, sh.start, sh.end);
     if (warp == kWarpTma) {
         // ------------------------------------------------------------ copies
+        // A part of nt tiles takes nt + kAhead stages: stage j has V tile j - kAhead and K tile j, where there are such.
         uint32_t seq = 0, part = 0;
         bool ok = true;
         for (; ok && w.more(); w.next(a, a.Hkv)) {
             const Unit u = unit_of(a, w.s, w.at.q);
             const int t0 = w.at.t, nt = w.last_tile(u) - t0, g = w.at.g;
             if (nt <= 0) continue;
-            const int ahead = u.wide ? 1 : 2;
             const bool on = lane == 0;
             // K and V of a sequence with one block of rows pass once
             uint64_t policy;
             if (w.nq == 1) asm volatile("createpolicy.fractional.L2::evict_first.b64 %0, 1.0;" : "=l"(policy));
             else asm volatile("createpolicy.fractional.L2::evict_normal.b64 %0, 1.0;" : "=l"(policy));
-            // page ids of the part, 32 in a warp's registers
+            // page ids: 32 in a warp's registers, those of the 32 pages before for the V tiles, which come later
             const int64_t table0 = a.page_off[w.at.b], n_table = a.page_off[w.at.b + 1] - table0;
-            const int p_end = (int)((u.end + kBN - 1) / kBN);            // pages of the unit
-            int base = t0 * kPages;
             auto fetch = [&](int from) -> int {
                 const int p = from + lane;
                 int id = -1;
-                if (p < p_end && p < (t0 + nt) * kPages) {
+                if (p < t0 + nt) {
                     if (p < n_table) {
                         id = a.page_table[table0 + p];
                         if (id < 0 || id >= a.n_pages) { report(a.status, DSBD_DEV_BAD_CHUNK); id = -1; }
@@ -424,51 +411,50 @@ k_chunk_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
                 }
                 return id;
             };
-            int ids_k = fetch(base), ids_v = ids_k, base_k = base, base_v = base;
-            auto copy = [&](const CUtensorMap *map, int tile, int &ids, int &at) {
-                const int p = (t0 + tile) * kPages;
-                if (p >= at + 32) { at = p; ids = fetch(p); }
-                const Tile<S::kSlots> to(seq);
-                if (!warp_wait(&sh.empty[to.slot], (to.filling & 1) ^ 1, &sh)) { ok = false; return; }
-                const int boxes = min(kPages, p_end - p);
-                mbar_expect_tx_if(on, to.full(&sh), (uint32_t)boxes * kBN * D * 2);
-                const uint32_t dst = smem_u32(ring + to.slot * S::kSlot);
+            int ids = fetch(t0), before_ids = ids, at = 0;
+            auto row_of = [&](int tile) -> int {                 // of the pools' maps (past their ends: zeros)
+                const int id = __shfl_sync(kFull, tile >= at ? ids : before_ids, tile & 31);
+                return id < 0 ? INT32_MAX - 2 * kBN : (id * a.Hkv + g) * kBN;
+            };
+            for (int j = 0; j < nt + kAhead && ok; ++j) {
+                if (j == kAhead) {
+                    // (the first K tiles do not wait for the query rows of the part before to be done with)
+                    if (part > 0) ok = warp_wait(&sh.q_empty, (part - 1) & 1, &sh);
+                    if (!ok) break;
+                    ++part;
+                    const int tiles = u.wide ? 2 : 1;
+                    mbar_expect_tx_if(on, &sh.q_full, (uint32_t)(tiles * a.box_tokens * a.group * D * 2));
+                    for (int x = 0; x < tiles; ++x)
+#pragma unroll
+                        for (int h = 0; h < S::kHalves; ++h)
+                            tma_load_3d(on, smem_u32(q_s + x * S::kQ + h * S::kQHalf), &map_q, h * 64, g * a.group,
+                                        u.first + u.i0 + x * a.tile_tokens, &sh.q_full);
+                }
+                if (j == at + 32) { before_ids = ids; at = j; ids = fetch(t0 + j); }
+                const bool has_k = j < nt, has_v = j >= kAhead;
+                const Stg to(seq);
+                ok = warp_wait(&sh.empty[to.slot], (to.filling & 1) ^ 1, &sh);
+                if (!ok) break;
+                const int yk = row_of(j), yv = row_of(max(j - kAhead, 0));
+                mbar_expect_tx_if(on, to.full(&sh), (uint32_t)(has_k + has_v) * S::kKv);
 #ifdef DSBD_TEST_WAIT_TIMEOUT
                 const bool there = !(seq == 1 && blockIdx.x == 0);       // the bytes this barrier expects never come
 #else
                 const bool there = true;
 #endif
-                for (int k = 0; k < boxes; ++k) {
-                    const int id = __shfl_sync(kFull, ids, p + k - at);
-                    const int y = id < 0 ? INT32_MAX - 2 * kBN : (id * a.Hkv + g) * kBN;      // (past the pool: zeros)
+                const uint32_t dst = smem_u32(ring + to.slot * S::kStage);
 #pragma unroll
-                    for (int h = 0; h < S::kHalves; ++h)
-                        tma_load_2d_hint(on && there, dst + h * kHalf + k * (kBN * 128), map, h * 64, y, to.full(&sh), policy);
+                for (int h = 0; h < S::kHalves; ++h) {
+                    tma_load_2d_hint(on && there && has_v, dst + S::kKv + h * S::kHalf, &map_v, h * 64, yv, to.full(&sh), policy);
+                    tma_load_2d_hint(on && there && has_k, dst + h * S::kHalf, &map_k, h * 64, yk, to.full(&sh), policy);
                 }
                 ++seq;
-            };
-            // the first tiles do not wait for the query rows of the part before to be done with
-            for (int i = 0; i < min(ahead, nt) && ok; ++i) copy(&map_k, i, ids_k, base_k);
-            if (ok) copy(&map_v, 0, ids_v, base_v);
-            if (ok && part > 0) ok = warp_wait(&sh.q_empty, (part - 1) & 1, &sh);
-            if (!ok) break;
-            ++part;
-            const int tiles = u.wide ? 2 : 1;
-            mbar_expect_tx_if(on, &sh.q_full, (uint32_t)(tiles * a.box_tokens * a.group * D * 2));
-            for (int x = 0; x < tiles; ++x)
-#pragma unroll
-                for (int h = 0; h < S::kHalves; ++h)
-                    tma_load_3d(on, smem_u32(q_s + x * S::kSlot + h * kHalf), &map_q, h * 64, g * a.group,
-                                u.first + u.i0 + x * a.tile_tokens, &sh.q_full);
-            for (int i = 0; i < nt && ok; ++i) {
-                if (i > 0) copy(&map_v, i, ids_v, base_v);
-                if (ok && i + ahead < nt) copy(&map_k, i + ahead, ids_k, base_k);
             }
         }
         if (!ok) {
             // let the copies already issued land before the CTA goes away
-            for (uint32_t k = 0; k < (uint32_t)S::kSlots && k < seq; ++k) {
-                const Tile<S::kSlots> t(seq - 1 - k);
+            for (uint32_t k = 0; k < (uint32_t)S::kStages && k < seq; ++k) {
+                const Stg t(seq - 1 - k);
                 for (uint32_t i = 0; i < kWaitTries && !mbar_try(t.full(&sh), t.parity()); ++i) {}
             }
             if (part > 0)
@@ -478,98 +464,77 @@ k_chunk_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
         // ------------------------------------------------------------ products
         const int x = warp - kWarpMma;
         const bool on = lane == 0;
-        constexpr uint32_t idesc_s = instr_desc(kTile, kTile, 0, 0);
-        constexpr uint32_t idesc_o = instr_desc(kTile, D, 0, 1);
-        const uint32_t s_col = tmem + kColS + x * kTile, o_col = tmem + kColO + x * D;
-        uint32_t base = 0, part = 0, np = 0, turns = 0;
+        constexpr uint32_t idesc_s = instr_desc(kRows, kTile, 0, 0);
+        constexpr uint32_t idesc_o = instr_desc(kRows, D, 0, 1);
+        const uint32_t s_col = tmem + kColS + x * 2 * kTile, o_col = tmem + kColO + x * D;
+        uint32_t base = 0, part = 0, ns = 0, np = 0;             // stages before the part; S products and P's so far
         bool ok = true;
-        auto slot_wait = [&](uint32_t seq) -> uint32_t {
-            const Tile<S::kSlots> t(seq);
-            ok = warp_wait(t.full(&sh), t.parity(), &sh);
-            return t.slot;
-        };
-        // a slot is free when both warps have told so: in narrow units the one that uses it tells for both
-        auto release = [&](void *bar, bool twice) {
-            tc_commit(on, bar);
-            if (twice) tc_commit(on, bar);
-        };
         for (; ok && w.more(); w.next(a, a.Hkv)) {
             const Unit u = unit_of(a, w.s, w.at.q);
             const int nt = w.last_tile(u) - w.at.t;
             if (nt <= 0) continue;
-            const int ahead = u.wide ? 1 : 2, step = ahead;
+            // wide: this row tile takes every K and V tile, narrow: those of its parity
+            const int step = u.wide ? 1 : 2;
             ok = warp_wait(&sh.q_full, part & 1, &sh);
-            const uint64_t qd = desc_k_major(smem_u32(q_s + (u.wide ? x : 0) * S::kSlot));
-            // Wide units: the row tiles take turns, so that one's products run while the other's softmax does (left alone they fall
-            // into step, and the tensor cores idle while both work on their rows).
-            auto take_turn = [&] {
-                if (u.wide && ok && (x == 1 || turns > 0)) ok = warp_wait(&sh.turn[x], (x == 1 ? turns : turns - 1) & 1, &sh);
+            const uint64_t qd = desc_k_major(smem_u32(q_s + (u.wide ? x : 0) * S::kQ));
+            // a stage is free when both warps have told so: in narrow units the one that uses it tells for both
+            auto release = [&](const Stg &t) {
+                tc_commit(on, &sh.empty[t.slot]);
+                if (!u.wide) tc_commit(on, &sh.empty[t.slot]);
             };
-            auto pass_turn = [&] {
-                if (!u.wide) return;
-                if (on) mbar_arrive(&sh.turn[x ^ 1]);
-                ++turns;
-            };
-            auto product_s = [&](uint32_t s, int i) {
-                const uint64_t kd = desc_k_major(smem_u32(ring + s * S::kSlot));
+            auto product_s = [&](const Stg &t) {
+                const uint64_t kd = desc_k_major(smem_u32(ring + t.slot * S::kStage));
 #pragma unroll
-                for (int ks = 0; ks < D / 16; ++ks) {
-                    const uint64_t at = (uint64_t)((ks / 4) * (kHalf >> 4) + (ks % 4) * 2);
-                    mma_ss(on, s_col, qd + at, kd + at, idesc_s, ks > 0);
-                }
-                tc_commit(on, &sh.s_full[x]);
-                pass_turn();
-                release(&sh.empty[s], !u.wide);
-                if (i + step >= nt) tc_commit(on, &sh.q_empty);          // the row tile's last S
+                for (int ks = 0; ks < D / 16; ++ks)
+                    mma_ss(on, s_col + (ns & 1) * kTile, qd + (uint64_t)((ks / 4) * (S::kQHalf >> 4) + (ks % 4) * 2),
+                           kd + (uint64_t)((ks / 4) * (S::kHalf >> 4) + (ks % 4) * 2), idesc_s, ks > 0);
+                tc_commit(on, &sh.s_full[x][ns & 1]);
+                ++ns;
             };
-            int i = u.wide ? 0 : x;
-            if (ok && i < nt) {
-                const uint32_t s = slot_wait(base + seq_k(i, ahead));
-                tc_fence_after();
-                take_turn();
-                if (ok) product_s(s, i);
+            // the stages of the first K tiles
+            int left = u.wide ? nt : (nt - x + 1) / 2;                   // S products to come
+            const bool none = left == 0;
+            for (int j = u.wide ? 0 : x; j < kAhead && ok; j += step) {
+                const Stg t(base + j);
+                if (j < nt) {
+                    ok = warp_wait(t.full(&sh), t.parity(), &sh);
+                    if (!ok) break;
+                    tc_fence_after();
+                    product_s(t);
+                    if (--left == 0) tc_commit(on, &sh.q_empty);
+                    release(t);
+                } else {
+                    ok = warp_wait(t.full(&sh), t.parity(), &sh);        // an empty stage
+                    if (!ok) break;
+                    if (on) { mbar_arrive(&sh.empty[t.slot]); if (!u.wide) mbar_arrive(&sh.empty[t.slot]); }
+                    __syncwarp();
+                }
             }
             // (the accumulators of the part before have been read; every part waits, so that no phase is missed)
             if (ok && part > 0) ok = warp_wait(&sh.o_free[x], (part - 1) & 1, &sh);
-            if (ok && i >= nt) {                                         // no tile of this parity
+            if (ok && none) {                                            // no tile of this parity
                 if (on) { mbar_arrive(&sh.q_empty); mbar_arrive(&sh.o_full[x]); }
                 __syncwarp();
             }
-            for (; i < nt && ok; i += step) {
-                const uint32_t sv = slot_wait(base + seq_v(i, nt, ahead));
-                // wide: K is there before P, so that nothing holds the next S up; narrow: K comes when it comes
-                uint32_t sk = 0;
-                const bool more = i + step < nt;
-                if (ok && u.wide && more) sk = slot_wait(base + seq_k(i + step, ahead));
-                const bool fresh = i < step;
+            for (int i = u.wide ? 0 : x; i < nt && ok; i += step) {
+                const Stg t(base + kAhead + i);
+                ok = warp_wait(t.full(&sh), t.parity(), &sh) && warp_wait(&sh.p_full[x][np & 1], (np >> 1) & 1, &sh);
                 if (!ok) break;
-                const uint64_t vd = desc_mn_major(smem_u32(ring + sv * S::kSlot), kHalf);
+                tc_fence_after();
+                const uint64_t vd = desc_mn_major(smem_u32(ring + t.slot * S::kStage) + S::kKv, S::kHalf);
 #pragma unroll
-                for (int h = 0; h < 2; ++h) {                // the first half of P may come while the second is worked out
-                    if (ok) ok = warp_wait(&sh.p_full[x][h], np & 1, &sh);
-                    if (h == 1) take_turn();
-                    if (!ok) break;
-                    tc_fence_after();
-#pragma unroll
-                    for (int ks = h * kTile / 32; ks < (h + 1) * kTile / 32; ++ks)
-                        mma_ts(on, o_col, s_col + ks * 8, vd + (uint64_t)(ks * ((16 * 128) >> 4)), idesc_o, (!fresh || ks > 0) ? 1u : 0u);
-                }
-                if (!ok) break;
+                for (int ks = 0; ks < kTile / 16; ++ks)
+                    mma_ts(on, o_col, s_col + (np & 1) * kTile + ks * 8, vd + (uint64_t)(ks * ((16 * 128) >> 4)), idesc_o,
+                           (i >= step || ks > 0) ? 1u : 0u);
                 ++np;
-                release(&sh.empty[sv], !u.wide);
-                if (!more) {
-                    tc_commit(on, &sh.o_full[x]);
-                    pass_turn();
-                    continue;
+                if (i + kAhead < nt) {
+                    product_s(t);
+                    if (--left == 0) tc_commit(on, &sh.q_empty);
                 }
-                if (!u.wide) {
-                    sk = slot_wait(base + seq_k(i + step, ahead));
-                    if (!ok) break;
-                    tc_fence_after();
-                }
-                product_s(sk, i + step);
+                release(t);
+                if (i + step >= nt) tc_commit(on, &sh.o_full[x]);
             }
-            base += 2 * nt;
+            base += nt + kAhead;
             ++part;
         }
         // the block's shared memory outlives every arrival that the products have yet to make
@@ -578,11 +543,9 @@ k_chunk_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
         while (!__all_sync(kFull, mbar_try(&sh.drain[x], 0)) && i < kWaitTries) ++i;
     } else if (warp < kWarpOut) {
         // ------------------------------------------------------------ softmax
-        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kSoftmaxRegs));
-        w.start(a, sh.start, sh.end);
         const int x = warp >> 2, row = (warp & 3) * 32 + lane;
         const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
-        const uint32_t s_addr = tmem + lanes + kColS + x * kTile, o_addr = tmem + lanes + kColO + x * D;
+        const uint32_t s_base = tmem + lanes + kColS + x * 2 * kTile, o_addr = tmem + lanes + kColO + x * D;
         const int token = row / a.group;
         uint32_t base = 0, ns = 0, part = 0;
         bool ok = true;
@@ -598,20 +561,20 @@ k_chunk_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
             const int end = (int)(u.end - (int64_t)t0 * kTile);
             const int step = u.wide ? 1 : 2;
             float m_ref = -INFINITY, l = 0.f;
-            for (int i = u.wide ? 0 : x; i < nt; i += step) {
-                ok = warp_wait(&sh.s_full[x], ns & 1, &sh);
+            for (int i = u.wide ? 0 : x; i < nt; i += step, ++ns) {
+                const uint32_t s_addr = s_base + (ns & 1) * kTile;
+                ok = warp_wait(&sh.s_full[x][ns & 1], (ns >> 1) & 1, &sh);
                 if (!ok) break;
-                ++ns;
                 tc_fence_after();
                 // what lies behind the block's last token has weight zero: its values become zeros
                 if ((i + 1) * kTile > end && (x == 0 || !u.wide)) {
-                    const Tile<S::kSlots> v(base + seq_v(i, nt, u.wide ? 1 : 2));
-                    ok = warp_wait(v.full(&sh), v.parity(), &sh);
+                    const Stg t(base + kAhead + i);
+                    ok = warp_wait(t.full(&sh), t.parity(), &sh);
                     if (!ok) break;
-                    if (row >= end - i * kTile) {
+                    if (row < kTile && row >= end - i * kTile) {
 #pragma unroll
                         for (int h = 0; h < S::kHalves; ++h) {
-                            uint4 *line = reinterpret_cast<uint4 *>(ring + v.slot * S::kSlot + h * kHalf + row * 128);
+                            uint4 *line = reinterpret_cast<uint4 *>(ring + t.slot * S::kStage + S::kKv + h * S::kHalf + row * 128);
 #pragma unroll
                             for (int e = 0; e < 8; ++e) line[e] = make_uint4(0, 0, 0, 0);
                         }
@@ -619,13 +582,13 @@ k_chunk_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
                     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                 }
                 if (work) {
-                    uint32_t sv[4][32];
+                    uint32_t sv[2][32];
 #pragma unroll
-                    for (int c = 0; c < 4; ++c) tmem_ld32(s_addr + c * 32, sv[c]);
+                    for (int c = 0; c < 2; ++c) tmem_ld32(s_addr + c * 32, sv[c]);
                     tmem_wait_ld();
                     if ((i + 1) * kTile > all_see) {
 #pragma unroll
-                        for (int c = 0; c < 4; ++c) {
+                        for (int c = 0; c < 2; ++c) {
                             const int lim = min(max(sees - i * kTile - c * 32, 0), 32);
                             const uint32_t vis = lim == 32 ? ~0u : (1u << lim) - 1;
 #pragma unroll
@@ -640,11 +603,18 @@ k_chunk_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
                     const float mx = fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3])) * a.scale_log2;    // scale > 0
                     const bool need = mx > m_ref + kMoveRef;
                     if (__any_sync(kFull, need)) {
-                        // (the tile's S product was issued behind the previous O product, so that one has landed)
                         const float m_new = need ? mx : m_ref;
                         const float f = m_ref == -INFINITY ? 0.f : exp2f(m_ref - m_new);
                         l *= f;
                         if (i >= step) {
+                            // the O product of the tile before must have landed: narrow, this tile's S was issued behind it; wide,
+                            // its stage is free then
+                            if (u.wide) {
+                                const Stg t(base + kAhead + i - 1);
+                                ok = warp_wait(&sh.empty[t.slot], t.filling & 1, &sh);
+                                if (!ok) break;
+                                tc_fence_after();
+                            }
 #pragma unroll 1
                             for (int c = 0; c < D; c += 16) {
                                 uint32_t ov[16];
@@ -660,7 +630,7 @@ k_chunk_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
                     const float neg = m_ref == -INFINITY ? 0.f : -m_ref;
                     F2 l2[2] = {{0.f, 0.f}, {0.f, 0.f}};
 #pragma unroll
-                    for (int c = 0; c < 4; ++c) {
+                    for (int c = 0; c < 2; ++c) {
                         uint32_t pv[16];
 #pragma unroll
                         for (int e = 0; e < 16; ++e) {
@@ -671,22 +641,16 @@ k_chunk_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
                             l2[e & 1] = add2(l2[e & 1], w2);
                         }
                         tmem_st16(s_addr + c * 16, pv);
-                        if (c & 1) {
-                            tmem_wait_st();
-                            tc_fence_before();
-                            __syncwarp();
-                            if (lane == 0) mbar_arrive(&sh.p_full[x][c >> 1]);
-                        }
                     }
                     l += (l2[0].x + l2[0].y) + (l2[1].x + l2[1].y);
-                } else {
-                    tc_fence_before();
-                    __syncwarp();
-                    if (lane == 0) { mbar_arrive(&sh.p_full[x][0]); mbar_arrive(&sh.p_full[x][1]); }
+                    tmem_wait_st();
                 }
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&sh.p_full[x][ns & 1]);
             }
             if (!ok) break;
-            base += 2 * nt;
+            base += nt + kAhead;
             // the row's reference and sum for the output warps, which have read those of the part before
             if (part > 0) ok = warp_wait(&sh.o_free[x], (part - 1) & 1, &sh);
             if (!ok) break;
@@ -697,8 +661,6 @@ k_chunk_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
         }
     } else if (warp < kWarpTma) {
         // ------------------------------------------------------------ output
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOutRegs));
-        w.start(a, sh.start, sh.end);
         const int row = (warp & 3) * 32 + lane;
         const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16, o_addr = tmem + lanes + kColO;
         const int token = row / a.group, head = row - token * a.group;
@@ -864,18 +826,18 @@ k_chunk_merge(ChunkArgs a, int runs) {
 
 // Launch shape shared by the workspace query and the launch.
 struct Plan { int grid, whole, block_rows; };
-constexpr int64_t kWholeTiles = 12;                  // longest units that are taken whole
-constexpr int64_t kMinRun = 4 * kTile;               // smallest run, in tokens
+constexpr int64_t kWholeTokens = 1536;               // longest units that are taken whole
+constexpr int64_t kMinRun = 512;               // smallest run, in tokens
 
 Plan make_plan(const dsbd_chunk_t *c, const dsbd_attn_desc_t *d) {
     Plan p = {};
     int dev = 0, sms = 148;
     if (cudaGetDevice(&dev) == cudaSuccess) cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
-    const int group = d->Hq / d->Hkv, block = 2 * (kTile / group);
+    const int group = d->Hq / d->Hkv, block = 2 * (kRows / group);
     p.block_rows = (int)std::min<int64_t>(block, c->max_new) * group;
     // an upper bound of the units
     const int64_t units = (int64_t)d->Hkv * std::min<int64_t>(c->total_new, c->max_new <= block ? c->B : (int64_t)c->B + c->total_new / block);
-    p.whole = units <= sms && c->max_len <= kWholeTiles * kTile;
+    p.whole = units <= sms && c->max_len <= kWholeTokens;
     p.grid = p.whole ? (int)units : sms;
     return p;
 }
@@ -884,7 +846,7 @@ int check(const dsbd_chunk_t *c, const dsbd_attn_desc_t *d) {
     if (!c || !d || c->B <= 0 || !c->new_off || !c->prefix_off || c->total_new < 0 || c->max_new < 0 || c->max_len < 0)
         return DSBD_ERR_INVALID_ARG;
     if (d->Hq <= 0 || d->Hkv <= 0 || d->Hq % d->Hkv || !(d->scale > 0.f) || !std::isfinite(d->scale)) return DSBD_ERR_INVALID_ARG;
-    if (d->dtype != DSBD_DTYPE_BF16 || (d->d != 64 && d->d != 128) || d->Hq / d->Hkv > kTile) return DSBD_ERR_UNSUPPORTED;
+    if (d->dtype != DSBD_DTYPE_BF16 || (d->d != 64 && d->d != 128) || d->Hq / d->Hkv > kRows) return DSBD_ERR_UNSUPPORTED;
     if (c->max_len > (int64_t)1 << 30) return DSBD_ERR_UNSUPPORTED;
     return DSBD_OK;
 }
@@ -951,11 +913,11 @@ extern "C" int dsbd_chunk_attention_paged(const dsbd_chunk_t *c, const dsbd_attn
     if (!plan.whole && (reinterpret_cast<uintptr_t>(workspace) & 255)) return DSBD_ERR_INVALID_ARG;
     ChunkArgs a = {};
     a.B = c->B; a.Hq = d->Hq; a.Hkv = d->Hkv; a.group = d->Hq / d->Hkv; a.T = c->total_new;
-    a.tile_tokens = kTile / a.group;
+    a.tile_tokens = kRows / a.group;
     a.block_tokens = 2 * a.tile_tokens;
     a.box_tokens = std::min(a.tile_tokens, c->total_new);
     a.whole = plan.whole;
-    a.unit_cost = kTile;
+    a.unit_cost = 256;
     a.min_run = kMinRun;
     a.scale_log2 = d->scale * 1.4426950408889634f;
     a.max_len = c->max_len; a.n_pages = pages->n_pages;
