@@ -200,6 +200,29 @@ __device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&v)[16
           "r"(v[8]), "r"(v[9]), "r"(v[10]), "r"(v[11]), "r"(v[12]), "r"(v[13]), "r"(v[14]), "r"(v[15])
         : "memory");
 }
+// Products and commits are issued by one lane that elect.sync names (the same one for the same warp): its operands are uniform
+// for the compiler.  An MMA takes 36 cycles to issue so, 62 with one lane's predicate on a converged warp's instruction
+// (M = 128, N = 16, K = 16; at N = 64 and 128 43 and 59 cycles, what it takes to run).
+__device__ __forceinline__ bool elect_one() {
+    uint32_t p;
+    asm volatile("{\n\t.reg .pred q;\n\telect.sync _|q, 0xffffffff;\n\tselp.u32 %0, 1, 0, q;\n\t}" : "=r"(p));
+    return p != 0;
+}
+__device__ __forceinline__ void mma_ss_one(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc, uint32_t acc) {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
+        ::"r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(acc) : "memory");
+}
+__device__ __forceinline__ void mma_ts_one(uint32_t d_tmem, uint32_t a_tmem, uint64_t b_desc, uint32_t idesc, uint32_t acc) {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
+        ::"r"(d_tmem), "r"(a_tmem), "l"(b_desc), "r"(idesc), "r"(acc) : "memory");
+}
+__device__ __forceinline__ void commit_one(void *bar) {
+    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_u32(bar)) : "memory");
+}
 // 32 bytes a lane (32-byte aligned): a warp's rows lie far apart, so a store instruction costs a line per lane.
 __device__ __forceinline__ void st_32b(void *p, const uint32_t (&v)[8]) {
     asm volatile("st.global.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};"
@@ -463,7 +486,6 @@ k_chunk_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
     } else if (warp == kWarpMma || warp == kWarpMma + 1) {
         // ------------------------------------------------------------ products
         const int x = warp - kWarpMma;
-        const bool on = lane == 0;
         constexpr uint32_t idesc_s = instr_desc(kRows, kTile, 0, 0);
         constexpr uint32_t idesc_o = instr_desc(kRows, D, 0, 1);
         const uint32_t s_col = tmem + kColS + x * 2 * kTile, o_col = tmem + kColO + x * D;
@@ -477,43 +499,46 @@ k_chunk_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
             const int step = u.wide ? 1 : 2;
             ok = warp_wait(&sh.q_full, part & 1, &sh);
             const uint64_t qd = desc_k_major(smem_u32(q_s + (u.wide ? x : 0) * S::kQ));
-            // a stage is free when both warps have told so: in narrow units the one that uses it tells for both
-            auto release = [&](const Stg &t) {
-                tc_commit(on, &sh.empty[t.slot]);
-                if (!u.wide) tc_commit(on, &sh.empty[t.slot]);
-            };
+            // (the elected lane's)
             auto product_s = [&](const Stg &t) {
                 const uint64_t kd = desc_k_major(smem_u32(ring + t.slot * S::kStage));
 #pragma unroll
                 for (int ks = 0; ks < D / 16; ++ks)
-                    mma_ss(on, s_col + (ns & 1) * kTile, qd + (uint64_t)((ks / 4) * (S::kQHalf >> 4) + (ks % 4) * 2),
-                           kd + (uint64_t)((ks / 4) * (S::kHalf >> 4) + (ks % 4) * 2), idesc_s, ks > 0);
-                tc_commit(on, &sh.s_full[x][ns & 1]);
-                ++ns;
+                    mma_ss_one(s_col + (ns & 1) * kTile, qd + (uint64_t)((ks / 4) * (S::kQHalf >> 4) + (ks % 4) * 2),
+                               kd + (uint64_t)((ks / 4) * (S::kHalf >> 4) + (ks % 4) * 2), idesc_s, ks > 0);
+                commit_one(&sh.s_full[x][ns & 1]);
             };
-            // the stages of the first K tiles
+            // a stage is free when both warps have told so: in narrow units the one that uses it tells for both
+            auto release = [&](const Stg &t) {
+                commit_one(&sh.empty[t.slot]);
+                if (!u.wide) commit_one(&sh.empty[t.slot]);
+            };
             int left = u.wide ? nt : (nt - x + 1) / 2;                   // S products to come
             const bool none = left == 0;
+            // the stages of the first K tiles
             for (int j = u.wide ? 0 : x; j < kAhead && ok; j += step) {
                 const Stg t(base + j);
-                if (j < nt) {
-                    ok = warp_wait(t.full(&sh), t.parity(), &sh);
-                    if (!ok) break;
-                    tc_fence_after();
-                    product_s(t);
-                    if (--left == 0) tc_commit(on, &sh.q_empty);
-                    release(t);
-                } else {
-                    ok = warp_wait(t.full(&sh), t.parity(), &sh);        // an empty stage
-                    if (!ok) break;
-                    if (on) { mbar_arrive(&sh.empty[t.slot]); if (!u.wide) mbar_arrive(&sh.empty[t.slot]); }
-                    __syncwarp();
+                ok = warp_wait(t.full(&sh), t.parity(), &sh);
+                if (!ok) break;
+                tc_fence_after();
+                if (j < nt) --left;
+                if (elect_one()) {
+                    if (j < nt) {
+                        product_s(t);
+                        if (left == 0) commit_one(&sh.q_empty);
+                        release(t);
+                    } else {                                             // an empty stage
+                        mbar_arrive(&sh.empty[t.slot]);
+                        if (!u.wide) mbar_arrive(&sh.empty[t.slot]);
+                    }
                 }
+                __syncwarp();
+                if (j < nt) ++ns;
             }
             // (the accumulators of the part before have been read; every part waits, so that no phase is missed)
             if (ok && part > 0) ok = warp_wait(&sh.o_free[x], (part - 1) & 1, &sh);
             if (ok && none) {                                            // no tile of this parity
-                if (on) { mbar_arrive(&sh.q_empty); mbar_arrive(&sh.o_full[x]); }
+                if (elect_one()) { mbar_arrive(&sh.q_empty); mbar_arrive(&sh.o_full[x]); }
                 __syncwarp();
             }
             for (int i = u.wide ? 0 : x; i < nt && ok; i += step) {
@@ -521,24 +546,31 @@ k_chunk_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
                 ok = warp_wait(t.full(&sh), t.parity(), &sh) && warp_wait(&sh.p_full[x][np & 1], (np >> 1) & 1, &sh);
                 if (!ok) break;
                 tc_fence_after();
-                const uint64_t vd = desc_mn_major(smem_u32(ring + t.slot * S::kStage) + S::kKv, S::kHalf);
+                const bool more = i + kAhead < nt;
+                left -= more;
+                if (elect_one()) {
+                    const uint64_t vd = desc_mn_major(smem_u32(ring + t.slot * S::kStage) + S::kKv, S::kHalf);
 #pragma unroll
-                for (int ks = 0; ks < kTile / 16; ++ks)
-                    mma_ts(on, o_col, s_col + (np & 1) * kTile + ks * 8, vd + (uint64_t)(ks * ((16 * 128) >> 4)), idesc_o,
-                           (i >= step || ks > 0) ? 1u : 0u);
-                ++np;
-                if (i + kAhead < nt) {
-                    product_s(t);
-                    if (--left == 0) tc_commit(on, &sh.q_empty);
+                    for (int ks = 0; ks < kTile / 16; ++ks)
+                        mma_ts_one(o_col, s_col + (np & 1) * kTile + ks * 8, vd + (uint64_t)(ks * ((16 * 128) >> 4)), idesc_o,
+                                   (i >= step || ks > 0) ? 1u : 0u);
+                    if (more) {
+                        product_s(t);
+                        if (left == 0) commit_one(&sh.q_empty);
+                    }
+                    release(t);
+                    if (i + step >= nt) commit_one(&sh.o_full[x]);
                 }
-                release(t);
-                if (i + step >= nt) tc_commit(on, &sh.o_full[x]);
+                __syncwarp();
+                ++np;
+                ns += more;
             }
             base += nt + kAhead;
             ++part;
         }
         // the block's shared memory outlives every arrival that the products have yet to make
-        tc_commit(on, &sh.drain[x]);
+        if (elect_one()) commit_one(&sh.drain[x]);
+        __syncwarp();
         uint32_t i = 0;
         while (!__all_sync(kFull, mbar_try(&sh.drain[x], 0)) && i < kWaitTries) ++i;
     } else if (warp < kWarpOut) {
