@@ -43,7 +43,6 @@ constexpr int kTile = kBN;                           // tokens of a tile: a page
 constexpr int kPartRows = 2 * kRows;                 // rows of a unit
 constexpr int kThreads = 512;                        // two softmax warpgroups, the output's, one with producer and issuers
 constexpr int kWarpOut = 8, kWarpTma = 12, kWarpMma = 13;      // kWarpMma + X issues the products of row tile X
-constexpr int kAhead = 2;                            // tiles that S runs ahead of O
 constexpr uint32_t kTmemCols = 512, kColS = 0, kColO = 256;    // S: [X][2 buffers][kTile]
 constexpr float kMoveRef = 8.f;
 #ifdef DSBD_TEST_WAIT_TIMEOUT
@@ -124,6 +123,7 @@ struct Unit {
     int64_t end;                                     // tokens that the block's last one sees
     int nt;
     bool wide;
+    int step, ahead;                                 // tiles from one of a row tile to its next; tiles that S runs ahead of O (two of a row tile)
 };
 __device__ __forceinline__ Unit unit_of(const ChunkArgs &a, const Seq &s, int q) {
     Unit u;
@@ -133,6 +133,8 @@ __device__ __forceinline__ Unit unit_of(const ChunkArgs &a, const Seq &s, int q)
     u.end = s.L + u.i0 + u.tokens;
     u.nt = (int)((u.end + kTile - 1) / kTile);
     u.wide = u.tokens > a.tile_tokens;
+    u.step = u.wide ? 1 : 2;
+    u.ahead = 2 * u.step;
     return u;
 }
 
@@ -165,7 +167,7 @@ struct Walk {
 };
 
 struct Shared {
-    unsigned long long full[2][8], empty[8], s_full[2][2], p_full[2][2], ml_full[2], o_full[2], o_free[2], q_full, q_empty, drain[2];
+    unsigned long long full[2][8], empty[2][8], s_full[2][2], p_full[2][2], ml_full[2], o_full[2], o_free[2], q_full, q_empty, drain[2];
     uint32_t tmem_base;
     int abort;
     Pos start, end;
@@ -229,15 +231,18 @@ __device__ __forceinline__ void st_32b(void *p, const uint32_t (&v)[8]) {
                  ::"l"(p), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]) : "memory");
 }
 
-// Stage number `seq` of the ring: its slot, the barrier that its copies complete, the phase of that one.  A slot has two such
+// Stage number `seq` of the ring: its slot, the barriers of its landing and of its release, their phase.  A slot has two pairs of
 // barriers, for its fillings in turn: a warp that does not use every stage (narrow units) may wait for a filling while the
-// one before it, the other row tile's, is still on its way (copies land in any order), and the parity of one barrier could
-// not tell the two apart.  The filling before that one has landed and been used by then: the slot was filled again.
+// one before it, the other row tile's, is still on its way (copies land in any order), or ask for a release when the next
+// filling is done with already, and the parity of one barrier could not tell neighbours apart.  Fillings two apart it need not:
+// stage n - 2 STAGES had been released when n - STAGES was filled, and who waits for n has seen one later than that (a stage
+// of its own or the part's query rows); and nobody gets past stage n + STAGES while a row tile still works on n.
 template <int STAGES>
 struct Stage {
     uint32_t slot, filling;
     __device__ __forceinline__ explicit Stage(uint32_t seq) : slot(seq % STAGES), filling(seq / STAGES) {}
     __device__ __forceinline__ void *full(Shared *sh) const { return &sh->full[filling & 1][slot]; }
+    __device__ __forceinline__ void *empty(Shared *sh) const { return &sh->empty[filling & 1][slot]; }
     __device__ __forceinline__ uint32_t parity() const { return (filling >> 1) & 1; }
 };
 
@@ -369,7 +374,7 @@ k_chunk_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
     static_assert(sizeof(Shared) <= 3072 && 3072 + S::kSmem <= 227 * 1024, "both in the shared memory of a block");
 
     if (threadIdx.x == 0) {
-        for (int s = 0; s < S::kStages; ++s) { mbar_init(&sh.full[0][s], 1); mbar_init(&sh.full[1][s], 1); mbar_init(&sh.empty[s], 2); }
+        for (int s = 0; s < S::kStages; ++s) { mbar_init(&sh.full[0][s], 1); mbar_init(&sh.full[1][s], 1); mbar_init(&sh.empty[0][s], 2); mbar_init(&sh.empty[1][s], 2); }
         for (int x = 0; x < 2; ++x) {
             for (int k = 0; k < 2; ++k) { mbar_init(&sh.s_full[x][k], 1); mbar_init(&sh.p_full[x][k], 4); }
             mbar_init(&sh.ml_full[x], 4); mbar_init(&sh.o_full[x], 1); mbar_init(&sh.o_free[x], 4);
@@ -407,7 +412,7 @@ k_chunk_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
     w.start(a, sh.start, sh.end);
     if (warp == kWarpTma) {
         // ------------------------------------------------------------ copies
-        // A part of nt tiles takes nt + kAhead stages: stage j has V tile j - kAhead and K tile j, where there are such.
+        // A part of nt tiles takes nt + ahead stages: stage j has V tile j - ahead and K tile j, where there are such.
         uint32_t seq = 0, part = 0;
         bool ok = true;
         for (; ok && w.more(); w.next(a, a.Hkv)) {
@@ -439,8 +444,8 @@ k_chunk_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
                 const int id = __shfl_sync(kFull, tile >= at ? ids : before_ids, tile & 31);
                 return id < 0 ? INT32_MAX - 2 * kBN : (id * a.Hkv + g) * kBN;
             };
-            for (int j = 0; j < nt + kAhead && ok; ++j) {
-                if (j == kAhead) {
+            for (int j = 0; j < nt + u.ahead && ok; ++j) {
+                if (j == u.ahead) {
                     // (the first K tiles do not wait for the query rows of the part before to be done with)
                     if (part > 0) ok = warp_wait(&sh.q_empty, (part - 1) & 1, &sh);
                     if (!ok) break;
@@ -454,11 +459,14 @@ k_chunk_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
                                         u.first + u.i0 + x * a.tile_tokens, &sh.q_full);
                 }
                 if (j == at + 32) { before_ids = ids; at = j; ids = fetch(t0 + j); }
-                const bool has_k = j < nt, has_v = j >= kAhead;
+                const bool has_k = j < nt, has_v = j >= u.ahead;
                 const Stg to(seq);
-                ok = warp_wait(&sh.empty[to.slot], (to.filling & 1) ^ 1, &sh);
-                if (!ok) break;
-                const int yk = row_of(j), yv = row_of(max(j - kAhead, 0));
+                if (to.filling > 0) {
+                    const Stg from(seq - S::kStages);
+                    ok = warp_wait(from.empty(&sh), from.parity(), &sh);
+                    if (!ok) break;
+                }
+                const int yk = row_of(j), yv = row_of(max(j - u.ahead, 0));
                 mbar_expect_tx_if(on, to.full(&sh), (uint32_t)(has_k + has_v) * S::kKv);
 #ifdef DSBD_TEST_WAIT_TIMEOUT
                 const bool there = !(seq == 1 && blockIdx.x == 0);       // the bytes this barrier expects never come
@@ -496,7 +504,7 @@ k_chunk_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
             const int nt = w.last_tile(u) - w.at.t;
             if (nt <= 0) continue;
             // wide: this row tile takes every K and V tile, narrow: those of its parity
-            const int step = u.wide ? 1 : 2;
+            const int step = u.step;
             ok = warp_wait(&sh.q_full, part & 1, &sh);
             const uint64_t qd = desc_k_major(smem_u32(q_s + (u.wide ? x : 0) * S::kQ));
             // (the elected lane's)
@@ -510,13 +518,13 @@ k_chunk_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
             };
             // a stage is free when both warps have told so: in narrow units the one that uses it tells for both
             auto release = [&](const Stg &t) {
-                commit_one(&sh.empty[t.slot]);
-                if (!u.wide) commit_one(&sh.empty[t.slot]);
+                commit_one(t.empty(&sh));
+                if (!u.wide) commit_one(t.empty(&sh));
             };
             int left = u.wide ? nt : (nt - x + 1) / 2;                   // S products to come
             const bool none = left == 0;
             // the stages of the first K tiles
-            for (int j = u.wide ? 0 : x; j < kAhead && ok; j += step) {
+            for (int j = u.wide ? 0 : x; j < u.ahead && ok; j += step) {
                 const Stg t(base + j);
                 ok = warp_wait(t.full(&sh), t.parity(), &sh);
                 if (!ok) break;
@@ -528,8 +536,8 @@ k_chunk_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
                         if (left == 0) commit_one(&sh.q_empty);
                         release(t);
                     } else {                                             // an empty stage
-                        mbar_arrive(&sh.empty[t.slot]);
-                        if (!u.wide) mbar_arrive(&sh.empty[t.slot]);
+                        mbar_arrive(t.empty(&sh));
+                        if (!u.wide) mbar_arrive(t.empty(&sh));
                     }
                 }
                 __syncwarp();
@@ -542,11 +550,11 @@ k_chunk_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
                 __syncwarp();
             }
             for (int i = u.wide ? 0 : x; i < nt && ok; i += step) {
-                const Stg t(base + kAhead + i);
+                const Stg t(base + u.ahead + i);
                 ok = warp_wait(t.full(&sh), t.parity(), &sh) && warp_wait(&sh.p_full[x][np & 1], (np >> 1) & 1, &sh);
                 if (!ok) break;
                 tc_fence_after();
-                const bool more = i + kAhead < nt;
+                const bool more = i + u.ahead < nt;
                 left -= more;
                 if (elect_one()) {
                     const uint64_t vd = desc_mn_major(smem_u32(ring + t.slot * S::kStage) + S::kKv, S::kHalf);
@@ -565,7 +573,7 @@ k_chunk_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
                 ++np;
                 ns += more;
             }
-            base += nt + kAhead;
+            base += nt + u.ahead;
             ++part;
         }
         // the block's shared memory outlives every arrival that the products have yet to make
@@ -591,7 +599,7 @@ k_chunk_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
             // in tokens of the part: what this row sees, what every row of the tile sees, the block's end
             const int all_see = (int)(u.L - (int64_t)t0 * kTile) + i0 + 1, sees = all_see + token;
             const int end = (int)(u.end - (int64_t)t0 * kTile);
-            const int step = u.wide ? 1 : 2;
+            const int step = u.step;
             float m_ref = -INFINITY, l = 0.f;
             for (int i = u.wide ? 0 : x; i < nt; i += step, ++ns) {
                 const uint32_t s_addr = s_base + (ns & 1) * kTile;
@@ -600,7 +608,7 @@ k_chunk_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
                 tc_fence_after();
                 // what lies behind the block's last token has weight zero: its values become zeros
                 if ((i + 1) * kTile > end && (x == 0 || !u.wide)) {
-                    const Stg t(base + kAhead + i);
+                    const Stg t(base + u.ahead + i);
                     ok = warp_wait(t.full(&sh), t.parity(), &sh);
                     if (!ok) break;
                     if (row < kTile && row >= end - i * kTile) {
@@ -639,14 +647,11 @@ k_chunk_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
                         const float f = m_ref == -INFINITY ? 0.f : exp2f(m_ref - m_new);
                         l *= f;
                         if (i >= step) {
-                            // the O product of the tile before must have landed: narrow, this tile's S was issued behind it; wide,
-                            // its stage is free then
-                            if (u.wide) {
-                                const Stg t(base + kAhead + i - 1);
-                                ok = warp_wait(&sh.empty[t.slot], t.filling & 1, &sh);
-                                if (!ok) break;
-                                tc_fence_after();
-                            }
+                            // the O product of the tile before has landed when that one's stage is free
+                            const Stg t(base + u.ahead + i - step);
+                            ok = warp_wait(t.empty(&sh), t.parity(), &sh);
+                            if (!ok) break;
+                            tc_fence_after();
 #pragma unroll 1
                             for (int c = 0; c < D; c += 16) {
                                 uint32_t ov[16];
@@ -682,7 +687,7 @@ k_chunk_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
                 if (lane == 0) mbar_arrive(&sh.p_full[x][ns & 1]);
             }
             if (!ok) break;
-            base += nt + kAhead;
+            base += nt + u.ahead;
             // the row's reference and sum for the output warps, which have read those of the part before
             if (part > 0) ok = warp_wait(&sh.o_free[x], (part - 1) & 1, &sh);
             if (!ok) break;
