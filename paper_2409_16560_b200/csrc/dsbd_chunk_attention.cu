@@ -61,14 +61,19 @@ struct Shape {
     static constexpr uint32_t kSmem = 2 * kQ + kStages * kStage;
 };
 
+// Costs are counted in tokens that a block's rows see: a tile takes 1500 to 1600 cycles in wide units and as long in narrow ones
+// while all SMs read their caches, a unit's beginning and end 4500 and 9000.
+constexpr int kWideCost = 192, kNarrowCost = 384;
+constexpr int kMinRun = 512;                         // smallest run
+
 struct ChunkArgs {
     int B, Hq, Hkv, group, T;
     int tile_tokens, block_tokens;                   // tokens of a row tile (128 / group) and of a block (two)
     int box_tokens;                                  // of a query box
     int whole;                                       // a unit a CTA, nothing is cut
-    int unit_cost;                                   // what a unit costs beside its tokens, in tokens
+    double per_block;                                // 1 / block_tokens
     float scale_log2;
-    int64_t max_len, n_pages, min_run;               // min_run: smallest run, in cost
+    int64_t max_len, n_pages;
     const int32_t *new_off, *page_table;
     const int64_t *prefix_off, *page_off;
     __nv_bfloat16 *out;
@@ -88,9 +93,9 @@ __device__ __forceinline__ bool before(const Pos &x, const Pos &y) {
     return x.t < y.t;
 }
 
-// What a run left for the merge.  tail: a unit that it began and did not end; head: how it went on with one that an earlier
-// run began (0 not at all, 1 not to its end, 2 to its end).
-struct CutRec { int tail, head, b, g, q, pad[3]; };
+// What a run left for the merge.  tail: a unit that it began and did not end, of `tokens` rows of the tensors from `first` on and KV head g;
+// head: how it went on with one that an earlier run began (0 not at all, 1 not to its end, 2 to its end).
+struct CutRec { int tail, head, first, tokens, g, pad[3]; };
 
 struct Seq { int n, first; int64_t L; };
 __device__ __forceinline__ Seq seq_of(const ChunkArgs &a, int b, bool tell) {
@@ -105,15 +110,21 @@ __device__ __forceinline__ Seq seq_of(const ChunkArgs &a, int b, bool tell) {
     }
     return s;
 }
-__device__ __forceinline__ int blocks_of(const ChunkArgs &a, int n) { return (n + a.block_tokens - 1) / a.block_tokens; }
-// Cost of the first q blocks of one head of a sequence.
-__device__ __forceinline__ int64_t cost_before(const ChunkArgs &a, const Seq &s, int q) {
-    const int64_t full = (int64_t)q * (s.L + a.unit_cost) + (int64_t)a.block_tokens * ((int64_t)q * (q + 1) / 2);
-    return q < blocks_of(a, s.n) || q == 0 ? full : full - ((int64_t)q * a.block_tokens - s.n);
+// ceil(n / block_tokens): half a token more keeps the product off the whole numbers, from which its error is far smaller.
+__device__ __forceinline__ int blocks_of(const ChunkArgs &a, int n) {
+    return n == 0 ? 0 : (int)(((double)(n - 1) + 0.5) * a.per_block) + 1;
 }
-__device__ __forceinline__ int64_t head_cost(const ChunkArgs &a, const Seq &s) {
+// Cost of the first q < blocks_of(n) blocks of one head of a sequence, and of all: the tokens that their last rows see, kWideCost or
+// kNarrowCost more each (a last block of at most tile_tokens is narrow).  Whole numbers in doubles, whose sums and products are
+// one instruction each.
+__device__ __forceinline__ double cost_before(const ChunkArgs &a, const Seq &s, int q) {
+    return (double)q * ((double)(s.L + kWideCost) + (double)a.block_tokens * 0.5 * (double)(q + 1));
+}
+__device__ __forceinline__ double head_cost(const ChunkArgs &a, const Seq &s) {
     const int nq = blocks_of(a, s.n);
-    return a.whole ? nq : cost_before(a, s, nq);
+    if (a.whole || nq == 0) return nq;
+    const int tail = s.n - (nq - 1) * a.block_tokens;
+    return cost_before(a, s, nq) + (double)(tail - a.block_tokens + (tail <= a.tile_tokens ? kNarrowCost - kWideCost : 0));
 }
 
 struct Unit {
@@ -143,9 +154,9 @@ struct Walk {
     Pos at, end;
     Seq s;
     int nq;
-    __device__ __forceinline__ void start(const ChunkArgs &a, const Pos &p0, const Pos &p1) {
+    __device__ __forceinline__ void start(const ChunkArgs &a, const Pos &p0, const Pos &p1, const Seq &s0) {
         at = p0; end = p1;
-        if (before(at, end)) { s = seq_of(a, at.b, false); nq = blocks_of(a, s.n); }
+        if (before(at, end)) { s = s0; nq = blocks_of(a, s.n); }
     }
     __device__ __forceinline__ bool more() const { return before(at, end); }
     __device__ __forceinline__ int last_tile(const Unit &u) const {
@@ -171,8 +182,8 @@ struct Shared {
     uint32_t tmem_base;
     int abort;
     Pos start, end;
-    int64_t scan[kThreads / 32], mine[2];
-    int found_b[2];
+    Seq seq;                                         // of start.b, and its pages
+    int64_t table0, n_table;
     float2 ml[2][kRows];                             // [X] reference and row sum of the rows
 };
 
@@ -286,74 +297,77 @@ __device__ __forceinline__ F2 exp2_poly(F2 z) {
 }
 constexpr int kPolyOf8 = 2;                          // of eight pairs of weights, those taken by exp2_poly
 
-// The CTA's run: all threads.  Returns through sh.start, sh.end; the sequences' facts are checked here, once a launch.
+// The CTA's run, by one warp.  Returns through sh.start, sh.end, sh.seq and the pages' range; the sequences' facts are checked here, once
+// a launch.  This stands before everything else of a call, and most of its time is that of fetching its instructions: one round
+// of loads, doubles in place of 64-bit integers, quotients by floats that steps put right (8500 cycles without that).
 __device__ void find_run(const ChunkArgs &a, Shared &sh) {
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    const int per = (a.B + kThreads - 1) / kThreads, b0 = min(tid * per, a.B), b1 = min(b0 + per, a.B);
-    int64_t sum = 0;
-    for (int b = b0; b < b1; ++b) sum += head_cost(a, seq_of(a, b, blockIdx.x == 0)) * a.Hkv;
-    int64_t incl = sum;
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-        const int64_t x = __shfl_up_sync(kFull, incl, o);
-        if (lane >= o) incl += x;
+    const int lane = threadIdx.x & 31;
+    const int per = (a.B + 31) / 32, b0 = min(lane * per, a.B), b1 = min(b0 + per, a.B);
+    // (a lane's first sequence stays in registers: the only one up to 32)
+    Seq s0 = {};
+    int64_t table0 = 0, table1 = 0;
+    double hc0 = 0.0;
+    if (b0 < b1) {
+        table0 = a.page_off[b0];
+        table1 = a.page_off[b0 + 1];
+        s0 = seq_of(a, b0, blockIdx.x == 0);
+        hc0 = head_cost(a, s0);
     }
-    if (lane == 31) sh.scan[warp] = incl;
-    if (tid < 2) sh.found_b[tid] = -1;
-    __syncthreads();
-    int64_t base = 0, total = 0;
-#pragma unroll
-    for (int w = 0; w < kThreads / 32; ++w) {
-        if (w < warp) base += sh.scan[w];
-        total += sh.scan[w];
-    }
-    const int64_t hi = base + incl, lo = hi - sum;
-    // the cuts: equal runs of at least min_run
-    int64_t runs = a.whole ? total : total / a.min_run;
-    runs = runs < 1 ? 1 : runs > (int64_t)gridDim.x ? (int64_t)gridDim.x : runs;
-    int64_t cut[2];
-#pragma unroll
+    double sum = hc0 * a.Hkv;
+#pragma unroll 1
+    for (int b = b0 + 1; b < b1; ++b) sum += head_cost(a, seq_of(a, b, blockIdx.x == 0)) * a.Hkv;
+    const double hi = warp_scan(sum, lane), lo = hi - sum, total = __shfl_sync(kFull, hi, 31);
+    // the cuts: equal runs, not too small.  (A CTA and its neighbour work the cut between them out alike.)
+    const int runs = max(1, (int)fmin((double)gridDim.x, a.whole ? total : floor(total * (1.0 / kMinRun))));
+    const double share = total * (double)__frcp_rn((float)runs);         // (the last cut is the total itself)
+#pragma unroll 1
     for (int k = 0; k < 2; ++k) {
-        const int64_t c = (int64_t)blockIdx.x + k;
-        cut[k] = c >= runs ? total : a.whole ? c : total / runs * c + total % runs * c / runs;
-        if (cut[k] >= lo && cut[k] < hi) {
-            int64_t x = lo;
-            for (int b = b0; b < b1; ++b) {
-                const Seq s = seq_of(a, b, false);
-                const int64_t hc = head_cost(a, s), c_b = hc * a.Hkv;
-                if (cut[k] >= x + c_b) { x += c_b; continue; }
-                const int64_t rem = cut[k] - x;
-                Pos p;
-                p.b = b;
-                p.g = (int)(rem / hc);
-                int64_t in = rem - p.g * hc;
-                const int nq = blocks_of(a, s.n);
-                if (a.whole) {
-                    p.q = (int)in; p.t = 0;
-                } else {
-                    // largest q with cost_before(q) <= in: the root of a quadratic, put right by steps
-                    const double h = (double)(s.L + a.unit_cost) / a.block_tokens + 0.5;
-                    int q = (int)(sqrt(h * h + 2.0 * (double)in / a.block_tokens) - h);
-                    q = max(0, min(q, nq - 1));
-                    while (q > 0 && cost_before(a, s, q) > in) --q;
-                    while (q + 1 < nq && cost_before(a, s, q + 1) <= in) ++q;
-                    p.q = q;
-                    in -= cost_before(a, s, q) + a.unit_cost;
-                    p.t = in > 0 ? (int)(in / kTile) : 0;
-                }
-                if (k == 0) sh.start = p; else sh.end = p;
-                sh.found_b[k] = b;
-                break;
-            }
+        const int c = (int)blockIdx.x + k;
+        const double cut = c >= runs ? total : a.whole ? (double)c : floor((double)c * share);
+        if (lane == 0) {
+            const Pos over = {a.B, 0, 0, 0};
+            (k == 0 ? sh.start : sh.end) = over;
+        }
+        __syncwarp();
+        if (cut < lo || cut >= hi) continue;
+        double in = cut - lo, hc = hc0;
+        Seq s = s0;
+        int b = b0;
+#pragma unroll 1
+        while (in >= hc * a.Hkv) {                   // (cut < hi: it lies in one of the sequences)
+            in -= hc * a.Hkv;
+            s = seq_of(a, ++b, false);
+            hc = head_cost(a, s);
+        }
+        Pos p;
+        p.b = b;
+        p.g = max((int)__fdividef((float)in, (float)hc) - 1, 0);
+        while ((double)(p.g + 1) * hc <= in) ++p.g;
+        in -= (double)p.g * hc;
+        if (a.whole) {
+            p.q = (int)in; p.t = 0;
+        } else {
+            // largest q with cost_before(q) <= in: the root of a quadratic
+            const int nq = blocks_of(a, s.n);
+            const float per = (float)a.per_block, h = (float)(s.L + kWideCost) * per + 0.5f;
+            float root;
+            asm("sqrt.approx.f32 %0, %1;" : "=f"(root) : "f"(h * h + 2.f * (float)in * per));
+            p.q = max(min((int)(root - h), nq) - 2, 0);
+            while (p.q + 1 < nq && cost_before(a, s, p.q + 1) <= in) ++p.q;
+            // (what a unit costs beside its tokens lies before them)
+            in -= cost_before(a, s, p.q) + (s.n - p.q * a.block_tokens <= a.tile_tokens ? kNarrowCost : kWideCost);
+            p.t = max((int)in, 0) / kTile;
+        }
+        if (k == 0) {
+            sh.start = p;
+            sh.seq = s;
+            if (b != b0) { table0 = a.page_off[b]; table1 = a.page_off[b + 1]; }
+            sh.table0 = table0;
+            sh.n_table = table1 - table0;
+        } else {
+            sh.end = p;
         }
     }
-    __syncthreads();
-    if (tid == 0) {
-        const Pos over = {a.B, 0, 0, 0};
-        if (sh.found_b[0] < 0) sh.start = over;
-        if (sh.found_b[1] < 0) sh.end = over;
-    }
-    __syncthreads();
 }
 
 template <int D>
@@ -392,29 +406,34 @@ k_chunk_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
     }
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-    find_run(a, sh);
+    if (warp == 0) find_run(a, sh);
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
     const uint32_t tmem = *reinterpret_cast<volatile uint32_t *>(&sh.tmem_base);
 
-    if (threadIdx.x == 0 && a.recs) {
+    if (warp == kThreads / 32 - 1 && lane == 0 && a.recs) {              // (a warp without work)
         CutRec r = {};
         const Pos p0 = sh.start, p1 = sh.end;
         const bool same = p0.b == p1.b && p0.g == p1.g && p0.q == p1.q;
         r.tail = p1.t > 0 && (!same || p0.t == 0);
         r.head = p0.t == 0 ? 0 : !same ? 2 : p1.t > p0.t ? 1 : 0;
-        r.b = p1.b; r.g = p1.g; r.q = p1.q;
+        if (r.tail) {
+            const Unit u = unit_of(a, seq_of(a, p1.b, false), p1.q);
+            r.first = u.first + u.i0; r.tokens = u.tokens; r.g = p1.g;
+        }
         a.recs[blockIdx.x] = r;
     }
 
     Walk w;
-    w.start(a, sh.start, sh.end);
+    w.start(a, sh.start, sh.end, sh.seq);
     if (warp == kWarpTma) {
         // ------------------------------------------------------------ copies
         // A part of nt tiles takes nt + ahead stages: stage j has V tile j - ahead and K tile j, where there are such.
         uint32_t seq = 0, part = 0;
         bool ok = true;
+        int table_b = sh.start.b;
+        int64_t table0 = sh.table0, n_table = sh.n_table;
         for (; ok && w.more(); w.next(a, a.Hkv)) {
             const Unit u = unit_of(a, w.s, w.at.q);
             const int t0 = w.at.t, nt = w.last_tile(u) - t0, g = w.at.g;
@@ -425,7 +444,11 @@ k_chunk_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
             if (w.nq == 1) asm volatile("createpolicy.fractional.L2::evict_first.b64 %0, 1.0;" : "=l"(policy));
             else asm volatile("createpolicy.fractional.L2::evict_normal.b64 %0, 1.0;" : "=l"(policy));
             // page ids: 32 in a warp's registers, those of the 32 pages before for the V tiles, which come later
-            const int64_t table0 = a.page_off[w.at.b], n_table = a.page_off[w.at.b + 1] - table0;
+            if (w.at.b != table_b) {
+                table_b = w.at.b;
+                table0 = a.page_off[table_b];
+                n_table = a.page_off[table_b + 1] - table0;
+            }
             auto fetch = [&](int from) -> int {
                 const int p = from + lane;
                 int id = -1;
@@ -803,9 +826,7 @@ k_chunk_merge(ChunkArgs a, int runs) {
     const CutRec rec = a.recs[i0];
     int next = i0 + 1 + lane < runs ? a.recs[i0 + 1 + lane].head : 2;
     if (!rec.tail) return;
-    const Seq s = seq_of(a, rec.b, false);
-    const Unit u = unit_of(a, s, rec.q);
-    if (row >= u.tokens * a.group) return;
+    if (row >= rec.tokens * a.group) return;
     // the runs behind i0 that hold parts of the unit: those up to the first that ends it
     int parts = 1;
     for (;;) {
@@ -856,7 +877,7 @@ k_chunk_merge(ChunkArgs a, int runs) {
     const float inv = 1.f / l;
     const int token = row / a.group, head = row - token * a.group;
     uint32_t *dst = reinterpret_cast<uint32_t *>(
-        a.out + ((int64_t)(u.first + u.i0 + token) * a.Hq + rec.g * a.group + head) * D + lane * kPer);
+        a.out + ((int64_t)(rec.first + token) * a.Hq + rec.g * a.group + head) * D + lane * kPer);
 #pragma unroll
     for (int e = 0; e < kPer; e += 2) dst[e / 2] = pack_bf16(o[e] * inv, o[e + 1] * inv);
 }
@@ -864,7 +885,6 @@ k_chunk_merge(ChunkArgs a, int runs) {
 // Launch shape shared by the workspace query and the launch.
 struct Plan { int grid, whole, block_rows; };
 constexpr int64_t kWholeTokens = 1536;               // longest units that are taken whole
-constexpr int64_t kMinRun = 512;               // smallest run, in tokens
 
 Plan make_plan(const dsbd_chunk_t *c, const dsbd_attn_desc_t *d) {
     Plan p = {};
@@ -952,10 +972,9 @@ extern "C" int dsbd_chunk_attention_paged(const dsbd_chunk_t *c, const dsbd_attn
     a.B = c->B; a.Hq = d->Hq; a.Hkv = d->Hkv; a.group = d->Hq / d->Hkv; a.T = c->total_new;
     a.tile_tokens = kRows / a.group;
     a.block_tokens = 2 * a.tile_tokens;
+    a.per_block = 1.0 / a.block_tokens;
     a.box_tokens = std::min(a.tile_tokens, c->total_new);
     a.whole = plan.whole;
-    a.unit_cost = 256;
-    a.min_run = kMinRun;
     a.scale_log2 = d->scale * 1.4426950408889634f;
     a.max_len = c->max_len; a.n_pages = pages->n_pages;
     a.new_off = c->new_off; a.prefix_off = c->prefix_off; a.page_table = pages->page_table; a.page_off = pages->page_off;
