@@ -735,7 +735,8 @@ class Rope:
         self.address = C.addressof(self._struct)
 
     def check(self, d):
-        assert self.d <= {d}, "norm weights have the length of a head"
+        if self.d and self.d != {d}:
+            raise AssertionError("norm weights have the length of a head")
 
 
 class Chunk:
@@ -757,23 +758,53 @@ class Chunk:
         self.address = C.addressof(self._struct)
         self._table, self._page_off = _ptr(page_table), _ptr(page_off)
 
-    def pages(self, k_pool, v_pool):
-        assert k_pool.dim() == 4 and k_pool.shape == v_pool.shape and k_pool.shape[2] == 64
-        assert k_pool.dtype == v_pool.dtype and k_pool.is_contiguous() and v_pool.is_contiguous()
-        return KvPagesT(self._table, self._page_off, int(k_pool.shape[0]))
+        self._pages = {}
 
-
-def _heads(t):
-    """Pointer and row stride of a [T, H, d] tensor whose heads lie side by side (a view of a projection's output)."""
-    if t is None:
-        return None, 0
-    T, H, d = t.shape
-    s = t.stride()
-    assert (s[2] == 1 or d == 1) and (s[1] == d or H == 1), "rows of heads side by side"
-    return t.data_ptr(), s[0] if T > 1 else max(s[0], H * d)
+    def pages(self, n_pages):
+        """Address of the C struct of this chunk's tables for pools of n_pages."""
+        p = self._pages.get(n_pages)
+        if p is None:
+            p = self._pages[n_pages] = KvPagesT(self._table, self._page_off, n_pages)
+        return C.addressof(p)
 
 
 _DTYPES = {torch.bfloat16: DTYPE_BF16, torch.float32: DTYPE_F32}
+_descs = {}
+
+
+def _desc(Hq, Hkv, d, dtype, scale=1.0):
+    """An AttnDescT of these values (made once per shape: 0.6 us)."""
+    key = (Hq, Hkv, d, dtype, scale)
+    x = _descs.get(key)
+    if x is None:
+        if len(_descs) > 256:
+            _descs.clear()
+        x = _descs[key] = AttnDescT(Hq, Hkv, d, _DTYPES[dtype], float(scale), 0, 0)
+    return x
+
+
+def _row_stride(t, H, d):
+    """Row stride of a [T, H, d] tensor whose heads lie side by side (a view of a projection's output will do)."""
+    a, b, c = t.stride()
+    if not ((c == 1 or d == 1) and (b == d or H == 1)):
+        raise AssertionError("rows of heads side by side")
+    return a if a >= H * d or t.shape[0] > 1 else H * d
+
+
+def _alike(out, t):
+    """An output tensor like `t` in shape and type."""
+    if out is None:
+        return torch.empty(t.shape, dtype=t.dtype, device=t.device)
+    if out.shape != t.shape or out.dtype != t.dtype:
+        raise AssertionError("the output has the input's shape and type")
+    _on_device(out)
+    return out
+
+
+def _on_device(*tensors):
+    for t in tensors:
+        if not t.is_cuda:
+            _require_cuda(t)
 
 
 def _status(status, device):
@@ -782,10 +813,11 @@ def _status(status, device):
 
 def forest_positions(forest, prefix_off, position=None, status=None, stream=None):
     """dsbd_forest_positions: position[n] = prefix length of node n's beam + its depth, int32 [N]; returns (position, status)."""
-    _require_cuda(prefix_off)
-    f = forest.struct()
+    _on_device(prefix_off)
+    f = ForestT(0, forest.B, forest.N, 0, None, _ptr(forest.dev["beam_node_off"]), _ptr(forest.dev["parent"]))
     if position is None:
         position = torch.empty(forest.N, dtype=torch.int32, device=prefix_off.device)
+    assert position.dtype == torch.int32 and position.numel() >= forest.N
     status = _status(status, prefix_off.device)
     rc = load().dsbd_forest_positions(C.addressof(f), _ptr(prefix_off), _ptr(position), _ptr(status), _stream(stream))
     if rc != OK:
@@ -797,81 +829,96 @@ def rotate_qk(q, k, position, rope, q_out=None, k_out=None, status=None, stream=
     """dsbd_rotate_qk.  q [T, Hq, d], k [T, Hkv, d] (views of a fused projection will do; either may be None), position int32 [T].
     q_out = q and k_out = k work in place.  Returns (q_out, k_out, status)."""
     x = q if q is not None else k
-    _require_cuda(x, k, position)
-    T, H, d = x.shape
-    assert k is None or (k.dtype == x.dtype and k.shape[0] == T and k.shape[2] == d)
-    assert position is None or (position.dtype == torch.int32 and position.numel() == T)
+    T, Hq, d = x.shape
+    dtype, Hkv = x.dtype, Hq
+    _on_device(x)
     rope.check(d)
-    if q is not None and q_out is None:
-        q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-    if k is not None and k_out is None:
-        k_out = torch.empty(k.shape, dtype=k.dtype, device=k.device)
+    qp = kp = qo = ko = None
+    qs = ks = qos = kos = 0
+    if q is not None:
+        q_out = _alike(q_out, q)
+        qp, qs, qo, qos = q.data_ptr(), _row_stride(q, Hq, d), q_out.data_ptr(), _row_stride(q_out, Hq, d)
+    if k is not None:
+        Tk, Hkv, dk = k.shape
+        assert k.dtype == dtype and Tk == T and dk == d
+        _on_device(k)
+        k_out = _alike(k_out, k)
+        kp, ks, ko, kos = k.data_ptr(), _row_stride(k, Hkv, d), k_out.data_ptr(), _row_stride(k_out, Hkv, d)
+    if position is not None:
+        _on_device(position)
+        assert position.dtype == torch.int32 and position.numel() == T
     status = _status(status, x.device)
-    for a, b in ((q, q_out), (k, k_out)):
-        assert a is None or (b.shape == a.shape and b.dtype == a.dtype)
-    Hkv = k.shape[1] if k is not None else H
-    desc = AttnDescT(H if q is not None else Hkv, Hkv, d, _DTYPES[x.dtype], 1.0, 0, 0)
-    rc = load().dsbd_rotate_qk(T, C.addressof(desc), rope.address, _ptr(position), *_heads(q), *_heads(k), *_heads(q_out),
-                               *_heads(k_out), _ptr(status), _stream(stream))
+    desc = _desc(Hq if q is not None else Hkv, Hkv, d, dtype)
+    rc = load().dsbd_rotate_qk(T, C.addressof(desc), rope.address, _ptr(position), qp, qs, kp,
+                               ks, qo, qos, ko, kos, status.data_ptr(), _stream(stream))
     if rc != OK:
         raise DsbdError("dsbd_rotate_qk", rc)
     return q_out, k_out, status
 
 
+def _pools(k_pool, v_pool, Hkv, d, dtype):
+    n, h, t, e = k_pool.shape
+    if (h, t, e) != (Hkv, 64, d) or v_pool.shape != k_pool.shape or k_pool.dtype != dtype or v_pool.dtype != dtype:
+        raise AssertionError("pools [n_pages, Hkv, 64, d] of the tensors' type")
+    _on_device(k_pool, v_pool)
+    assert k_pool.is_contiguous() and v_pool.is_contiguous()
+    return n
+
+
 def kv_append_paged(chunk, k, v, k_pool, v_pool, rope=None, q=None, q_out=None, status=None, stream=None):
     """dsbd_kv_append_paged.  k, v [total_new, Hkv, d], q (optional) [total_new, Hq, d], views of a fused projection will
     do; pools [n_pages, Hkv, 64, d] of one layer, updated in place.  rope None: no norm, no rotation.  Returns (q_out, status)."""
-    _require_cuda(k, v, q, k_pool, v_pool)
     T, Hkv, d = k.shape
-    assert T == chunk.total_new and v.shape == k.shape and k.dtype == v.dtype == k_pool.dtype
-    assert k_pool.shape[1] == Hkv and k_pool.shape[3] == d
-    pages = chunk.pages(k_pool, v_pool)
+    dtype = k.dtype
+    _on_device(k, v)
+    assert T == chunk.total_new and v.shape == k.shape and v.dtype == dtype
+    n_pages = _pools(k_pool, v_pool, Hkv, d, dtype)
     if rope is not None:
         rope.check(d)
-    Hq = Hkv
+    Hq, qp, qs, qo, qos = Hkv, None, 0, None, 0
     if q is not None:
-        assert q.shape[0] == T and q.shape[2] == d and q.dtype == k.dtype
-        Hq = q.shape[1]
-        if q_out is None:
-            q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-        assert q_out.shape == q.shape and q_out.dtype == q.dtype
+        Tq, Hq, dq = q.shape
+        assert Tq == T and dq == d and q.dtype == dtype
+        _on_device(q)
+        q_out = _alike(q_out, q)
+        qp, qs, qo, qos = q.data_ptr(), _row_stride(q, Hq, d), q_out.data_ptr(), _row_stride(q_out, Hq, d)
     status = _status(status, k.device)
-    desc = AttnDescT(Hq, Hkv, d, _DTYPES[k.dtype], 1.0, 0, 0)
-    rc = load().dsbd_kv_append_paged(chunk.address, C.addressof(desc), rope.address if rope is not None else None, *_heads(q),
-                                     *_heads(k), *_heads(v), *_heads(q_out if q is not None else None), k_pool.data_ptr(),
-                                     v_pool.data_ptr(), C.addressof(pages), _ptr(status), _stream(stream))
+    desc = _desc(Hq, Hkv, d, dtype)
+    rc = load().dsbd_kv_append_paged(chunk.address, C.addressof(desc), rope.address if rope is not None else None, qp, qs,
+                                     k.data_ptr(), _row_stride(k, Hkv, d), v.data_ptr(), _row_stride(v, Hkv, d), qo, qos,
+                                     k_pool.data_ptr(), v_pool.data_ptr(), chunk.pages(n_pages), status.data_ptr(),
+                                     _stream(stream))
     if rc != OK:
         raise DsbdError("dsbd_kv_append_paged", rc)
     return (q_out if q is not None else None), status
 
 
 def chunk_attention_workspace(chunk, Hq, Hkv, d, dtype, scale):
-    desc = AttnDescT(Hq, Hkv, d, _DTYPES[dtype], float(scale), 0, 0)
+    desc = _desc(Hq, Hkv, d, dtype, scale)
     return int(load().dsbd_chunk_attention_paged_workspace(chunk.address, C.addressof(desc)))
 
 
 def chunk_attention_launches(chunk, Hq, Hkv, d, dtype, scale):
-    desc = AttnDescT(Hq, Hkv, d, _DTYPES[dtype], float(scale), 0, 0)
+    desc = _desc(Hq, Hkv, d, dtype, scale)
     return int(load().dsbd_chunk_attention_paged_launches(chunk.address, C.addressof(desc)))
 
 
 def chunk_attention_paged(chunk, Hq, Hkv, d, scale, q, k_pool, v_pool, out=None, workspace=None, status=None, stream=None):
     """dsbd_chunk_attention_paged; q [total_new, Hq, d], pools [n_pages, Hkv, 64, d] that hold the chunk already (see
     kv_append_paged); returns (out, status)."""
-    _require_cuda(q, k_pool, v_pool)
-    assert q.shape == (chunk.total_new, Hq, d) and k_pool.shape[1] == Hkv and k_pool.shape[3] == d
-    assert q.dtype == k_pool.dtype
-    pages = chunk.pages(k_pool, v_pool)
-    desc = AttnDescT(Hq, Hkv, d, _DTYPES[q.dtype], float(scale), 0, 0)
-    if out is None:
-        out = torch.empty_like(q)
+    _on_device(q)
+    dtype = q.dtype
+    assert q.shape == (chunk.total_new, Hq, d) and q.is_contiguous()
+    n_pages = _pools(k_pool, v_pool, Hkv, d, dtype)
+    desc = _desc(Hq, Hkv, d, dtype, scale)
+    out = _alike(out, q)
+    assert out.is_contiguous()
     if workspace is None:
         workspace = _workspace(load().dsbd_chunk_attention_paged_workspace(chunk.address, C.addressof(desc)), q.device)
     status = _status(status, q.device)
-    assert out.shape == q.shape and out.dtype == q.dtype
-    rc = load().dsbd_chunk_attention_paged(chunk.address, C.addressof(desc), _ptr(q), k_pool.data_ptr(), v_pool.data_ptr(),
-                                           C.addressof(pages), _ptr(out), workspace.data_ptr(), workspace.numel(),
-                                           _ptr(status), _stream(stream))
+    rc = load().dsbd_chunk_attention_paged(chunk.address, C.addressof(desc), q.data_ptr(), k_pool.data_ptr(), v_pool.data_ptr(),
+                                           chunk.pages(n_pages), out.data_ptr(), workspace.data_ptr(),
+                                           workspace.numel() * workspace.element_size(), status.data_ptr(), _stream(stream))
     if rc != OK:
         raise DsbdError("dsbd_chunk_attention_paged", rc)
     return out, status

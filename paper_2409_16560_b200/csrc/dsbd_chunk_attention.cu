@@ -70,7 +70,7 @@ struct ChunkArgs {
     int B, Hq, Hkv, group, T;
     int tile_tokens, block_tokens;                   // tokens of a row tile (128 / group) and of a block (two)
     int box_tokens;                                  // of a query box
-    int whole;                                       // a unit a CTA, nothing is cut
+    int whole, max_blocks;                           // a unit a CTA, nothing is cut: (sequence, KV head, one of max_blocks blocks)
     double per_block;                                // 1 / block_tokens
     float scale_log2;
     int64_t max_len, n_pages;
@@ -122,7 +122,7 @@ __device__ __forceinline__ double cost_before(const ChunkArgs &a, const Seq &s, 
 }
 __device__ __forceinline__ double head_cost(const ChunkArgs &a, const Seq &s) {
     const int nq = blocks_of(a, s.n);
-    if (a.whole || nq == 0) return nq;
+    if (nq == 0) return 0.0;
     const int tail = s.n - (nq - 1) * a.block_tokens;
     return cost_before(a, s, nq) + (double)(tail - a.block_tokens + (tail <= a.tile_tokens ? kNarrowCost - kWideCost : 0));
 }
@@ -302,6 +302,21 @@ constexpr int kPolyOf8 = 2;                          // of eight pairs of weight
 // of loads, doubles in place of 64-bit integers, quotients by floats that steps put right (8500 cycles without that).
 __device__ void find_run(const ChunkArgs &a, Shared &sh) {
     const int lane = threadIdx.x & 31;
+    if (a.whole) {
+        const int c = (int)blockIdx.x, pair = c / a.max_blocks;
+        Pos p;
+        p.b = pair / a.Hkv; p.g = pair - p.b * a.Hkv; p.q = c - pair * a.max_blocks; p.t = 0;
+        const int64_t table0 = a.page_off[p.b], table1 = a.page_off[p.b + 1];
+        const Seq s = seq_of(a, p.b, p.g == 0 && p.q == 0 && lane == 0);
+        if (lane == 0) {
+            sh.start = sh.end = p;
+            if (p.q < blocks_of(a, s.n)) ++sh.end.q;
+            sh.seq = s;
+            sh.table0 = table0;
+            sh.n_table = table1 - table0;
+        }
+        return;
+    }
     const int per = (a.B + 31) / 32, b0 = min(lane * per, a.B), b1 = min(b0 + per, a.B);
     // (a lane's first sequence stays in registers: the only one up to 32)
     Seq s0 = {};
@@ -318,12 +333,12 @@ __device__ void find_run(const ChunkArgs &a, Shared &sh) {
     for (int b = b0 + 1; b < b1; ++b) sum += head_cost(a, seq_of(a, b, blockIdx.x == 0)) * a.Hkv;
     const double hi = warp_scan(sum, lane), lo = hi - sum, total = __shfl_sync(kFull, hi, 31);
     // the cuts: equal runs, not too small.  (A CTA and its neighbour work the cut between them out alike.)
-    const int runs = max(1, (int)fmin((double)gridDim.x, a.whole ? total : floor(total * (1.0 / kMinRun))));
+    const int runs = max(1, (int)fmin((double)gridDim.x, floor(total * (1.0 / kMinRun))));
     const double share = total * (double)__frcp_rn((float)runs);         // (the last cut is the total itself)
 #pragma unroll 1
     for (int k = 0; k < 2; ++k) {
         const int c = (int)blockIdx.x + k;
-        const double cut = c >= runs ? total : a.whole ? (double)c : floor((double)c * share);
+        const double cut = c >= runs ? total : floor((double)c * share);
         if (lane == 0) {
             const Pos over = {a.B, 0, 0, 0};
             (k == 0 ? sh.start : sh.end) = over;
@@ -344,20 +359,16 @@ __device__ void find_run(const ChunkArgs &a, Shared &sh) {
         p.g = max((int)__fdividef((float)in, (float)hc) - 1, 0);
         while ((double)(p.g + 1) * hc <= in) ++p.g;
         in -= (double)p.g * hc;
-        if (a.whole) {
-            p.q = (int)in; p.t = 0;
-        } else {
-            // largest q with cost_before(q) <= in: the root of a quadratic
-            const int nq = blocks_of(a, s.n);
-            const float per = (float)a.per_block, h = (float)(s.L + kWideCost) * per + 0.5f;
-            float root;
-            asm("sqrt.approx.f32 %0, %1;" : "=f"(root) : "f"(h * h + 2.f * (float)in * per));
-            p.q = max(min((int)(root - h), nq) - 2, 0);
-            while (p.q + 1 < nq && cost_before(a, s, p.q + 1) <= in) ++p.q;
-            // (what a unit costs beside its tokens lies before them)
-            in -= cost_before(a, s, p.q) + (s.n - p.q * a.block_tokens <= a.tile_tokens ? kNarrowCost : kWideCost);
-            p.t = max((int)in, 0) / kTile;
-        }
+        // largest q with cost_before(q) <= in: the root of a quadratic
+        const int nq = blocks_of(a, s.n);
+        const float per_block = (float)a.per_block, h = (float)(s.L + kWideCost) * per_block + 0.5f;
+        float root;
+        asm("sqrt.approx.f32 %0, %1;" : "=f"(root) : "f"(h * h + 2.f * (float)in * per_block));
+        p.q = max(min((int)(root - h), nq) - 2, 0);
+        while (p.q + 1 < nq && cost_before(a, s, p.q + 1) <= in) ++p.q;
+        // (what a unit costs beside its tokens lies before them)
+        in -= cost_before(a, s, p.q) + (s.n - p.q * a.block_tokens <= a.tile_tokens ? kNarrowCost : kWideCost);
+        p.t = max((int)in, 0) / kTile;
         if (k == 0) {
             sh.start = p;
             sh.seq = s;
@@ -883,7 +894,7 @@ k_chunk_merge(ChunkArgs a, int runs) {
 }
 
 // Launch shape shared by the workspace query and the launch.
-struct Plan { int grid, whole, block_rows; };
+struct Plan { int grid, whole, max_blocks, block_rows; };
 constexpr int64_t kWholeTokens = 1536;               // longest units that are taken whole
 
 Plan make_plan(const dsbd_chunk_t *c, const dsbd_attn_desc_t *d) {
@@ -892,8 +903,8 @@ Plan make_plan(const dsbd_chunk_t *c, const dsbd_attn_desc_t *d) {
     if (cudaGetDevice(&dev) == cudaSuccess) cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
     const int group = d->Hq / d->Hkv, block = 2 * (kRows / group);
     p.block_rows = (int)std::min<int64_t>(block, c->max_new) * group;
-    // an upper bound of the units
-    const int64_t units = (int64_t)d->Hkv * std::min<int64_t>(c->total_new, c->max_new <= block ? c->B : (int64_t)c->B + c->total_new / block);
+    p.max_blocks = (int)((std::min<int64_t>(c->max_new, c->total_new) + block - 1) / block);
+    const int64_t units = (int64_t)c->B * d->Hkv * p.max_blocks;         // (or places for them)
     p.whole = units <= sms && c->max_len <= kWholeTokens;
     p.grid = p.whole ? (int)units : sms;
     return p;
@@ -975,6 +986,7 @@ extern "C" int dsbd_chunk_attention_paged(const dsbd_chunk_t *c, const dsbd_attn
     a.per_block = 1.0 / a.block_tokens;
     a.box_tokens = std::min(a.tile_tokens, c->total_new);
     a.whole = plan.whole;
+    a.max_blocks = std::max(plan.max_blocks, 1);
     a.scale_log2 = d->scale * 1.4426950408889634f;
     a.max_len = c->max_len; a.n_pages = pages->n_pages;
     a.new_off = c->new_off; a.prefix_off = c->prefix_off; a.page_table = pages->page_table; a.page_off = pages->page_off;

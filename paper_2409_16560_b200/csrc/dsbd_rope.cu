@@ -13,7 +13,7 @@ using namespace dsbd;
 namespace {
 
 constexpr int kMaxRot = 128;
-constexpr int kThreads = 256;
+constexpr int kThreads = 128;
 
 // Launched while the kernel before it may still run: wait for that one's results, then let the next one come (which waits
 // for these in turn).
@@ -115,40 +115,32 @@ k_forest_positions(int B, int N, const int32_t *__restrict__ node_off, const int
 }
 
 // ------------------------------------------------------------------------------------------ rotation and append
-template <class T> struct Vec;                       // 16 bytes of a row, widened to fp32
-template <> struct Vec<float> {
-    static constexpr int kN = 4;
-    __device__ static void widen(const uint4 &v, float *x) {
+// Four neighbouring values of a row, as they lie in memory and widened to fp32.
+template <class T> struct Four;
+template <> struct Four<float> {
+    using Raw = uint4;
+    __device__ static void widen(const Raw &v, float *x) {
         x[0] = __uint_as_float(v.x); x[1] = __uint_as_float(v.y); x[2] = __uint_as_float(v.z); x[3] = __uint_as_float(v.w);
     }
-    __device__ static uint4 narrow(const float *x) {
+    __device__ static Raw narrow(const float *x) {
         return make_uint4(__float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]), __float_as_uint(x[3]));
     }
 };
-template <> struct Vec<__nv_bfloat16> {
-    static constexpr int kN = 8;
-    __device__ static void widen(const uint4 &v, float *x) {
-        const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            x[2 * i] = __uint_as_float(w[i] << 16);
-            x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
-        }
+template <> struct Four<__nv_bfloat16> {
+    using Raw = uint2;
+    __device__ static void widen(const Raw &v, float *x) {
+        x[0] = __uint_as_float(v.x << 16); x[1] = __uint_as_float(v.x & 0xffff0000u);
+        x[2] = __uint_as_float(v.y << 16); x[3] = __uint_as_float(v.y & 0xffff0000u);
     }
-    __device__ static uint4 narrow(const float *x) {
-        uint32_t w[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const __nv_bfloat162 p = __floats2bfloat162_rn(x[2 * i], x[2 * i + 1]);
-            w[i] = *reinterpret_cast<const uint32_t *>(&p);
-        }
-        return make_uint4(w[0], w[1], w[2], w[3]);
+    __device__ static Raw narrow(const float *x) {
+        const __nv_bfloat162 a = __floats2bfloat162_rn(x[0], x[1]), b = __floats2bfloat162_rn(x[2], x[3]);
+        return make_uint2(*reinterpret_cast<const uint32_t *>(&a), *reinterpret_cast<const uint32_t *>(&b));
     }
 };
 
 struct RopeArgs {
     int T, Hq, Hkv;
-    int q_pieces, k_pieces, pieces;                  // pieces of kUnroll warp steps: of q, of k; all of a token (v's too)
+    int q_pieces, k_pieces, pieces;                  // pieces of a few warp steps: of q, of k; all of a token (v's too)
     int per_warp, parts;                             // pieces a warp takes, warps of a token
     int rot, layout, n_positions;
     float eps;
@@ -166,7 +158,8 @@ struct RopeArgs {
     int32_t *status;
 };
 
-constexpr int kUnroll = 4;                           // 16-byte loads in flight a lane
+// Steps of a piece, whose loads (64 bytes a lane) are in flight together: four of bf16, two of fp32 (at 64 registers).
+__host__ __device__ constexpr int unroll(int size) { return size == 2 ? 4 : 2; }
 
 // The sequence of row t: the largest b with new_off[b] <= t, by a warp, 32 probes at a time.
 __device__ __forceinline__ int find_sequence(const int32_t *new_off, int B, int t, int lane) {
@@ -182,26 +175,27 @@ __device__ __forceinline__ int find_sequence(const int32_t *new_off, int B, int 
     return lo;
 }
 
-// A warp takes a token and some of its heads, 32 / (d * size / 16) of them a step, a lane 16 bytes of one.  A token's
-// row of cosines and sines goes to registers once (as what a lane's values and their partners are multiplied by) and
-// serves all heads of the warp; the partners of the half layout come from another lane of the same head.  Bound by bytes:
-// every value is read and written once.
+// A warp takes a token and some of its heads, 32 / (d / 8) of them a step, a lane eight values of one: two fours that are each other's
+// partners (i and i + rot / 2 in the half layout; neighbours in the interleaved one and behind the rotated part), so that no
+// value crosses lanes but the norm's sum.  A token's row of cosines and sines goes to registers once and serves all heads of
+// the warp.  Bound by bytes: every value is read and written once.
 template <class T, int D, bool APPEND>
-__global__ void __launch_bounds__(kThreads)
+__global__ void __launch_bounds__(kThreads, 8)
 k_rotate(RopeArgs a) {
-    using V = Vec<T>;
-    constexpr int N = V::kN, kLanes = D / N, kHeads = 32 / kLanes;      // lanes of a head, heads of a step
-    constexpr int kPiece = kHeads * kUnroll;
+    using F = Four<T>;
+    using Raw = typename F::Raw;
+    constexpr int kLanes = D / 8, kHeads = 32 / kLanes;                 // lanes of a head, heads of a step
+    constexpr int kUnroll = unroll(sizeof(T)), kPiece = kHeads * kUnroll;
     pdl_wait();
-    const int lane = threadIdx.x & 31, e0 = (lane % kLanes) * N;
+    const int lane = threadIdx.x & 31, j = lane % kLanes;
     const int64_t job = (int64_t)blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5);
     const int64_t jobs = (int64_t)a.T * a.parts;
     if (job >= jobs) {
         if (!APPEND) return;
-        // what is behind the last token of a page that this call opened: a warp to a sequence and a pool
-        const int64_t z = job - jobs;
-        const int b = (int)(z >> 1);
-        if (b >= a.B) return;
+        // what is behind the last token of a page that this call opened: a warp to a sequence, a head and a pool
+        const unsigned z = (unsigned)(job - jobs), of_b = z / (2u * a.Hkv), g = (z >> 1) - of_b * a.Hkv;
+        if (of_b >= (unsigned)a.B) return;
+        const int b = (int)of_b;
         const int n = a.new_off[b + 1] - a.new_off[b];
         const int64_t L = a.prefix_off[b + 1] - a.prefix_off[b], end = L + n;
         const int from = (int)(end % DSBD_PAGE_TOKENS);
@@ -211,36 +205,41 @@ k_rotate(RopeArgs a) {
         const int page = a.page_table[a.page_off[b] + p];
         if (page < 0 || page >= a.n_pages) return;
         T *pool = static_cast<T *>((z & 1) ? a.v_pool : a.k_pool);
-        const int left = (DSBD_PAGE_TOKENS - from) * kLanes;            // 16-byte words of a head
-        for (int g = 0; g < a.Hkv; ++g) {
-            uint4 *dst = reinterpret_cast<uint4 *>(pool + (((int64_t)page * a.Hkv + g) * DSBD_PAGE_TOKENS + from) * D);
-            for (int i = lane; i < left; i += 32) dst[i] = make_uint4(0, 0, 0, 0);
-        }
+        const int left = (DSBD_PAGE_TOKENS - from) * (D * (int)sizeof(T) / 16);      // 16-byte words of a head
+        uint4 *dst = reinterpret_cast<uint4 *>(pool + (((int64_t)page * a.Hkv + g) * DSBD_PAGE_TOKENS + from) * D);
+        for (int i = lane; i < left; i += 32) dst[i] = make_uint4(0, 0, 0, 0);
         return;
     }
-    const int t = (int)(job / a.parts);
+    const int t = a.parts == 1 ? (int)job : (int)((unsigned)job / (unsigned)a.parts);
     int piece = (int)(job - (int64_t)t * a.parts) * a.per_warp;
     const int piece_end = min(piece + a.per_warp, a.pieces);
 
+    // the lane's values: e0 .. e0 + 3 and e1 .. e1 + 3
+    const bool by_half = a.layout == DSBD_ROPE_HALF, turned = 8 * j < a.rot;
+    const int half = a.rot / 2;
+    const int e0 = by_half && turned ? 4 * j : 8 * j, e1 = by_half && turned ? half + 4 * j : 8 * j + 4;
+
     // where a piece reads: kind 0 q, 1 k, 2 v
-    uint4 raw[kUnroll];
-    int kind, first, heads;
-    auto place = [&](int p) {
-        kind = p < a.q_pieces ? 0 : p < a.q_pieces + a.k_pieces ? 1 : 2;
-        first = (p - (kind == 0 ? 0 : kind == 1 ? a.q_pieces : a.q_pieces + a.k_pieces)) * kPiece + lane / kLanes;
-        heads = kind == 0 ? a.Hq : a.Hkv;
-    };
+    struct Piece { int kind, first, heads; Raw x[kUnroll], y[kUnroll]; };
     auto load = [&](int p) {
-        place(p);
-        const T *src = kind == 0 ? static_cast<const T *>(a.q) + t * a.q_stride
-                     : kind == 1 ? static_cast<const T *>(a.k) + t * a.k_stride : static_cast<const T *>(a.v) + t * a.v_stride;
+        Piece r;
+        r.kind = p < a.q_pieces ? 0 : p < a.q_pieces + a.k_pieces ? 1 : 2;
+        r.first = (p - (r.kind == 0 ? 0 : r.kind == 1 ? a.q_pieces : a.q_pieces + a.k_pieces)) * kPiece + lane / kLanes;
+        r.heads = r.kind == 0 ? a.Hq : a.Hkv;
+        const T *src = r.kind == 0 ? static_cast<const T *>(a.q) + t * a.q_stride
+                     : r.kind == 1 ? static_cast<const T *>(a.k) + t * a.k_stride : static_cast<const T *>(a.v) + t * a.v_stride;
 #pragma unroll
         for (int u = 0; u < kUnroll; ++u) {
-            const int h = first + u * kHeads;
-            raw[u] = h < heads ? *reinterpret_cast<const uint4 *>(src + (int64_t)h * D + e0) : make_uint4(0, 0, 0, 0);
+            const int h = r.first + u * kHeads;
+            r.x[u] = r.y[u] = Raw{};
+            if (h < r.heads) {
+                r.x[u] = *reinterpret_cast<const Raw *>(src + (int64_t)h * D + e0);
+                r.y[u] = *reinterpret_cast<const Raw *>(src + (int64_t)h * D + e1);
+            }
         }
+        return r;
     };
-    load(piece);
+    Piece now = load(piece);
 
     int64_t pos;
     int64_t row = 0;                                 // of the pools: (page * Hkv) * 64 + slot
@@ -272,86 +271,71 @@ k_rotate(RopeArgs a) {
         }
     }
 
-    // y = x * c + partner * s
-    float c[N], s[N];
-    const bool turned = e0 < a.rot;
-    const int half = a.rot / 2;
-    const bool by_half = a.layout == DSBD_ROPE_HALF;
-    int partner = lane;
+    // the lane's pairs: 4 j .. 4 j + 3 of the table's row, in either layout
+    float4 c = {1.f, 1.f, 1.f, 1.f}, s = {0.f, 0.f, 0.f, 0.f};
     if (turned) {
-        const float *cs = a.table + pos * a.rot;
-        if (by_half) {
-            const bool second = e0 >= half;
-            const int i = second ? e0 - half : e0;
-            partner = second ? lane - half / N : lane + half / N;
-#pragma unroll
-            for (int e = 0; e < N; e += 4) {
-                const float4 cv = *reinterpret_cast<const float4 *>(cs + i + e);
-                const float4 sv = *reinterpret_cast<const float4 *>(cs + half + i + e);
-                const float sg = second ? 1.f : -1.f;
-                c[e] = cv.x; c[e + 1] = cv.y; c[e + 2] = cv.z; c[e + 3] = cv.w;
-                s[e] = sg * sv.x; s[e + 1] = sg * sv.y; s[e + 2] = sg * sv.z; s[e + 3] = sg * sv.w;
-            }
-        } else {
-#pragma unroll
-            for (int e = 0; e < N; e += 4) {
-                const float2 cv = *reinterpret_cast<const float2 *>(cs + (e0 + e) / 2);
-                const float2 sv = *reinterpret_cast<const float2 *>(cs + half + (e0 + e) / 2);
-                c[e] = c[e + 1] = cv.x; c[e + 2] = c[e + 3] = cv.y;
-                s[e] = -sv.x; s[e + 1] = sv.x; s[e + 2] = -sv.y; s[e + 3] = sv.y;
-            }
-        }
+        const float *cs = a.table + pos * a.rot + 4 * j;
+        c = *reinterpret_cast<const float4 *>(cs);
+        s = *reinterpret_cast<const float4 *>(cs + half);
     }
 
     for (;;) {
-        if (kind == 2) {
-            T *dst = static_cast<T *>(a.v_pool) + row * D + e0;
-#pragma unroll
-            for (int u = 0; u < kUnroll; ++u) {
-                const int h = first + u * kHeads;
-                if (h < heads) *reinterpret_cast<uint4 *>(dst + (int64_t)h * DSBD_PAGE_TOKENS * D) = raw[u];
-            }
+        const int kind = now.kind;
+        const float *norm = kind == 0 ? a.q_norm : kind == 1 ? a.k_norm : nullptr;
+        T *dst;
+        int64_t pitch = D;
+        if (kind == 0) {
+            dst = static_cast<T *>(a.q_out) + t * a.q_out_stride;
+        } else if (APPEND) {
+            dst = static_cast<T *>(kind == 1 ? a.k_pool : a.v_pool) + row * D;
+            pitch = DSBD_PAGE_TOKENS * D;
         } else {
-            const float *norm = kind == 0 ? a.q_norm : a.k_norm;
-            float w[N];
-            if (norm) {
+            dst = static_cast<T *>(a.k_out) + t * a.k_out_stride;
+        }
+        float4 w0 = {}, w1 = {};
+        if (norm) {
+            w0 = *reinterpret_cast<const float4 *>(norm + e0);
+            w1 = *reinterpret_cast<const float4 *>(norm + e1);
+        }
 #pragma unroll
-                for (int e = 0; e < N; e += 4) {
-                    const float4 v = *reinterpret_cast<const float4 *>(norm + e0 + e);
-                    w[e] = v.x; w[e + 1] = v.y; w[e + 2] = v.z; w[e + 3] = v.w;
-                }
-            }
-            T *dst;
-            int64_t pitch = D;
-            if (kind == 0) dst = static_cast<T *>(a.q_out) + t * a.q_out_stride + e0;
-            else if (APPEND) { dst = static_cast<T *>(a.k_pool) + row * D + e0; pitch = DSBD_PAGE_TOKENS * D; }
-            else dst = static_cast<T *>(a.k_out) + t * a.k_out_stride + e0;
-#pragma unroll
-            for (int u = 0; u < kUnroll; ++u) {
-                const int h = first + u * kHeads;
-                float x[N];
-                V::widen(raw[u], x);
+        for (int u = 0; u < kUnroll; ++u) {
+            const int h = now.first + u * kHeads;
+            if (kind != 2 && (norm || turned)) {     // (everything else keeps its bits; a head's lanes agree where there is a norm)
+                float x[4], y[4];
+                F::widen(now.x[u], x);
+                F::widen(now.y[u], y);
                 if (norm) {
                     float ss = 0.f;
 #pragma unroll
-                    for (int e = 0; e < N; ++e) ss = fmaf(x[e], x[e], ss);
+                    for (int e = 0; e < 4; ++e) ss = fmaf(x[e], x[e], fmaf(y[e], y[e], ss));
 #pragma unroll
                     for (int o = kLanes / 2; o > 0; o >>= 1) ss += __shfl_xor_sync(kFull, ss, o);
                     const float r = rsqrtf(ss * (1.f / D) + a.eps);
-#pragma unroll
-                    for (int e = 0; e < N; ++e) x[e] = x[e] * r * w[e];
+                    x[0] *= r * w0.x; x[1] *= r * w0.y; x[2] *= r * w0.z; x[3] *= r * w0.w;
+                    y[0] *= r * w1.x; y[1] *= r * w1.y; y[2] *= r * w1.z; y[3] *= r * w1.w;
                 }
-                float y[N];
-#pragma unroll
-                for (int e = 0; e < N; ++e) {
-                    const float far = by_half ? __shfl_sync(kFull, x[e], partner) : x[e ^ 1];
-                    y[e] = turned ? fmaf(x[e], c[e], far * s[e]) : x[e];
+                if (turned) {
+                    auto turn = [](float &p, float &q, float cc, float sn) {
+                        const float v = p;
+                        p = fmaf(v, cc, -q * sn);
+                        q = fmaf(q, cc, v * sn);
+                    };
+                    if (by_half) {
+                        turn(x[0], y[0], c.x, s.x); turn(x[1], y[1], c.y, s.y); turn(x[2], y[2], c.z, s.z); turn(x[3], y[3], c.w, s.w);
+                    } else {
+                        turn(x[0], x[1], c.x, s.x); turn(x[2], x[3], c.y, s.y); turn(y[0], y[1], c.z, s.z); turn(y[2], y[3], c.w, s.w);
+                    }
                 }
-                if (h < heads) *reinterpret_cast<uint4 *>(dst + h * pitch) = norm || turned ? V::narrow(y) : raw[u];
+                now.x[u] = F::narrow(x);
+                now.y[u] = F::narrow(y);
+            }
+            if (h < now.heads) {
+                *reinterpret_cast<Raw *>(dst + h * pitch + e0) = now.x[u];
+                *reinterpret_cast<Raw *>(dst + h * pitch + e1) = now.y[u];
             }
         }
         if (++piece >= piece_end) break;
-        load(piece);
+        now = load(piece);
     }
 }
 
@@ -400,17 +384,23 @@ void set_rope(RopeArgs &a, const dsbd_rope_t *r) {
     a.table = r->table; a.q_norm = r->q_norm; a.k_norm = r->k_norm;
 }
 
+// Warps that a call is spread over at least, 24 an SM: with 48 4608 tokens x 40 heads of 128 take 18.1 us instead of 16.9, 20 tokens 2.2
+// either way.
+constexpr int64_t kMinWarps = 148 * 24;
+
 template <bool APPEND>
 int launch_rotate(RopeArgs a, const dsbd_attn_desc_t *d, cudaStream_t stream) {
-    const int lanes = d->d * (d->dtype == DSBD_DTYPE_BF16 ? 2 : 4) / 16, piece = 32 / lanes * kUnroll;
+    const int piece = 32 / (d->d / 8) * unroll(d->dtype == DSBD_DTYPE_BF16 ? 2 : 4);
     a.q_pieces = a.q ? (a.Hq + piece - 1) / piece : 0;
     a.k_pieces = a.k ? (a.Hkv + piece - 1) / piece : 0;
     a.pieces = a.q_pieces + a.k_pieces + (APPEND ? a.k_pieces : 0);
-    a.per_warp = 1;
+    // a token's heads to one warp, or to as many as it takes to have kMinWarps
+    const int want = (int)std::min<int64_t>(a.pieces, (kMinWarps + a.T - 1) / a.T);
+    a.per_warp = (a.pieces + want - 1) / want;
     a.parts = (a.pieces + a.per_warp - 1) / a.per_warp;
-    const int64_t jobs = (int64_t)a.T * a.parts + (APPEND ? 2 * (int64_t)a.B : 0);
+    const int64_t jobs = (int64_t)a.T * a.parts + (APPEND ? 2 * (int64_t)a.B * a.Hkv : 0);
     const int64_t grid = (jobs + kThreads / 32 - 1) / (kThreads / 32);
-    if (grid > INT32_MAX) return DSBD_ERR_UNSUPPORTED;
+    if (jobs > INT32_MAX) return DSBD_ERR_UNSUPPORTED;
     if (d->dtype == DSBD_DTYPE_F32)
         return d->d == 64 ? launch_pdl(k_rotate<float, 64, APPEND>, grid, kThreads, stream, a)
                           : launch_pdl(k_rotate<float, 128, APPEND>, grid, kThreads, stream, a);
