@@ -480,8 +480,8 @@ k_chunk_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
                 return id < 0 ? INT32_MAX - 2 * kBN : (id * a.Hkv + g) * kBN;
             };
             for (int j = 0; j < nt + u.ahead && ok; ++j) {
-                if (j == u.ahead) {
-                    // (the first K tiles do not wait for the query rows of the part before to be done with)
+                if (j == 2) {
+                    // (the first K tile of either row tile does not wait for the query rows of the part before to be done with)
                     if (part > 0) ok = warp_wait(&sh.q_empty, (part - 1) & 1, &sh);
                     if (!ok) break;
                     ++part;
