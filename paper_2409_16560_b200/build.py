@@ -82,9 +82,10 @@ def _build_variant(lib_path, tag, sources, define, force):
 
 
 def build_wait_test(force=False):
-    """A second library for one test: the attention kernel compiled with DSBD_TEST_WAIT_TIMEOUT
-    (short bounded waits, one tile never delivered).  Nothing but that test loads it."""
-    return _build_variant(WAIT_TEST_LIB, "waittest", ("dsbd_api.cu", "dsbd_attention.cu", "dsbd_attention_tc.cu", "dsbd_attention_tr.cu"),
+    """A second library for tests of the waits: the attention kernels compiled with DSBD_TEST_WAIT_TIMEOUT
+    (short bounded waits, one tile never delivered).  Nothing but those tests loads it."""
+    return _build_variant(WAIT_TEST_LIB, "waittest", ("dsbd_api.cu", "dsbd_attention.cu", "dsbd_attention_tc.cu", "dsbd_attention_tr.cu",
+                                           "dsbd_chunk_attention.cu"),
                           "-DDSBD_TEST_WAIT_TIMEOUT", force)
 
 

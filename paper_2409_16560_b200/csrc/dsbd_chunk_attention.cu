@@ -4,27 +4,35 @@
 //   out[i, h] = sum_j softmax_j(scale q[i, h] . K_j) V_j   over the positions j = 0 .. L_b + i of token i's sequence.
 //
 // Work unit = (sequence, KV head, block of tokens): the query rows of the block that map to this KV head (row = token *
-// group + head) against the pages from the first to the block's last token, in tiles of 128 tokens (two pages).  A CTA
-// has two row tiles of 128 rows, X = 0 and 1, each with a softmax warpgroup (a thread to a row, so maximum and sum of a row
-// are one thread's), 128 columns of S in TMEM (the weights P, bf16, overwrite their first half) and its accumulators O:
-//   S_X = Q_X K^T   (M = 128 rows, N = 128 tokens, K = d)    both operands K-major in shared memory
-//   O_X += P_X V    (M = 128 rows, N = d, K = 128 tokens)    P from TMEM, V MN-major in shared memory
-// While one group works on its S, the tensor cores work for the other: the products of X = 0 and 1 alternate.
-//   wide   more than 128 rows: the tiles hold different rows, every K and V tile serves both.
-//   narrow up to 128 rows (few tokens: single ones, ends of prompts): both tiles hold the same rows, X takes the K and V
-//          tiles of its parity, and X = 0's group joins the two results at the end.  (The time of these units is the
-//          cache's bytes; what counts is that the next copies are always on their way.)
-// One warp issues the copies (K and V tiles through one ring of slots in the order in which they are used, the query rows),
-// one the products.  Both run converged with one lane's predicate on the instructions.
+// group + head) against the pages from the first to the block's last token, in tiles of a page (64 tokens).  A CTA has two row
+// tiles of 128 rows, X = 0 and 1, each with a softmax warpgroup (a thread to a row, so maximum and sum of a row are one thread's),
+// two buffers of 64 columns for S in TMEM (the weights P, bf16, overwrite the first half of theirs) and its accumulators O:
+//   S_X = Q_X K^T   (M = 128 rows, N = 64 tokens, K = d)    both operands K-major in shared memory
+//   O_X += P_X V    (M = 128 rows, N = d, K = 64 tokens)    P from TMEM, V MN-major in shared memory
+// S runs two of a row tile's tiles ahead of O, so neither a softmax nor the tensor cores wait for the other's latency.  (Tiles of
+// 128 tokens read less of Q but leave TMEM no second buffer: the chain from a row tile's P over O and S to its next softmax then
+// took 3600 cycles for 128 tokens, two tiles of 64 take 3100.)
+//   wide   more than 128 rows: the row tiles hold different rows, every K and V tile serves both.
+//   narrow up to 128 rows (few tokens: single ones, ends of prompts): both hold the same rows, X takes the K and V tiles of its
+//          parity, and the output warps join the two results.  (The time of these units is the cache's bytes; what counts is that
+//          the next copies are always on their way.)
+// The other warps: four write the results (the softmax goes on to the next unit meanwhile), one issues the copies (K and V of a
+// stage of the ring together, the query rows), one for each row tile its products.
 //
 // Masks: a unit ends with the tile of its block's last token; in the last tiles a row sees the tokens up to its own.  V rows
 // behind the block's last token are cleared in shared memory, so that nothing in the pages behind it counts.
-// A row's reference is its running maximum, moved only when a logit exceeds it by more than 2^8; P is rounded to bf16 (the
-// operand type of V) and the row sum adds the rounded weights, so that a heavy weight's rounding cancels.
+// A row's reference is its running maximum, moved only when a logit exceeds it by more than 2^8.  P is rounded to bf16, the operand
+// type of V (3.9e-3 of a weight at most, 1.6e-3 on average over random weights, as much as the output's own rounding); the row sum
+// adds the weights before that: adding the rounded ones cost two more instructions a weight.
 //
-// Work split: the tiles of all units form one sequence (sequence, KV head, block), cut into equal runs, one per CTA; a unit
+// Work split: the tiles of all units form one sequence (sequence, KV head, block), cut into runs of equal cost, one per CTA; a unit
 // that straddles a cut leaves partial results that k_chunk_merge joins.  Few short units are taken whole, one a CTA.  Every
 // CTA finds its run with one scan over the sequences; there is no plan kernel.
+//
+// What bounds it: wide units shared memory's bandwidth (96 KB of operands of S, 32 KB of V and 32 KB of copies for 64 tokens of both row
+// tiles, 1545 cycles, where the products alone take 1100) and, in calls of a millisecond, the power limit: 16384 tokens at once, 32 / 8
+// heads of 128, 1.66 ms (1320 TFLOP/s), 1.95 ms (1120) in a loop of seconds, where the clock falls to 1.4 GHz.  Single tokens HBM:
+// 64 behind 1024 to 4096 97 us, 6.0 TB/s.  The shortest calls a chain of latencies: 4 tokens behind 512, heads of 64, 8.8 us.
 //
 // Every mbarrier wait is bounded; on a time-out the kernel records DSBD_DEV_TIMEOUT, lets its copies and products land,
 // frees its TMEM and returns.
@@ -68,7 +76,7 @@ constexpr int kWideCost = 192, kNarrowCost = 384;
 constexpr int kMinRun = 512;                         // smallest run
 
 struct ChunkArgs {
-    int B, Hq, Hkv, group, T;
+    int B, Hq, Hkv, group, T, max_new;
     int tile_tokens, block_tokens;                   // tokens of a row tile (128 / group) and of a block (two)
     int box_tokens;                                  // of a query box
     int whole, max_blocks;                           // a unit a CTA, nothing is cut: (sequence, KV head, one of max_blocks blocks)
@@ -105,7 +113,7 @@ __device__ __forceinline__ Seq seq_of(const ChunkArgs &a, int b, bool tell) {
     const int end = a.new_off[b + 1];
     s.L = a.prefix_off[b + 1] - a.prefix_off[b];
     s.n = end - s.first;
-    if (s.first < 0 || end < s.first || end > a.T || s.L < 0 || s.L > a.max_len || s.L + s.n > a.max_len) {
+    if (s.first < 0 || end < s.first || end > a.T || s.n > a.max_new || s.L < 0 || s.L > a.max_len || s.L + s.n > a.max_len) {
         s.n = 0;
         if (tell) report(a.status, DSBD_DEV_BAD_CHUNK);
     }
@@ -517,15 +525,13 @@ k_chunk_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
                 ++seq;
             }
         }
-        if (!ok) {
-            // let the copies already issued land before the CTA goes away
-            for (uint32_t k = 0; k < (uint32_t)S::kStages && k < seq; ++k) {
-                const Stg t(seq - 1 - k);
-                for (uint32_t i = 0; i < kWaitTries && !mbar_try(t.full(&sh), t.parity()); ++i) {}
-            }
-            if (part > 0)
-                for (uint32_t i = 0; i < kWaitTries && !mbar_try(&sh.q_full, (part - 1) & 1); ++i) {}
+        // the copies land before the CTA goes away, also where another warp gave up
+        for (uint32_t k = 0; k < (uint32_t)S::kStages && k < seq; ++k) {
+            const Stg t(seq - 1 - k);
+            for (uint32_t i = 0; i < kWaitTries && !mbar_try(t.full(&sh), t.parity()); ++i) {}
         }
+        if (part > 0)
+            for (uint32_t i = 0; i < kWaitTries && !mbar_try(&sh.q_full, (part - 1) & 1); ++i) {}
     } else if (warp == kWarpMma || warp == kWarpMma + 1) {
         // ------------------------------------------------------------ products
         const int x = warp - kWarpMma;
@@ -929,7 +935,7 @@ Plan make_plan(const dsbd_chunk_t *c, const dsbd_attn_desc_t *d) {
 }
 
 int check(const dsbd_chunk_t *c, const dsbd_attn_desc_t *d) {
-    if (!c || !d || c->B <= 0 || !c->new_off || !c->prefix_off || c->total_new < 0 || c->max_new < 0 || c->max_len < 0)
+    if (!c || !d || c->B <= 0 || !c->new_off || !c->prefix_off || c->total_new < 0 || c->max_new < 0 || (c->total_new > 0 && c->max_new == 0) || c->max_len < 0)
         return DSBD_ERR_INVALID_ARG;
     if (d->Hq <= 0 || d->Hkv <= 0 || d->Hq % d->Hkv || !(d->scale > 0.f) || !std::isfinite(d->scale)) return DSBD_ERR_INVALID_ARG;
     if (d->dtype != DSBD_DTYPE_BF16 || (d->d != 64 && d->d != 128) || d->Hq / d->Hkv > kRows) return DSBD_ERR_UNSUPPORTED;
@@ -998,7 +1004,7 @@ extern "C" int dsbd_chunk_attention_paged(const dsbd_chunk_t *c, const dsbd_attn
     if (!workspace || workspace_bytes < workspace_of(plan, d->d)) return DSBD_ERR_WORKSPACE_TOO_SMALL;
     if (!plan.whole && (reinterpret_cast<uintptr_t>(workspace) & 255)) return DSBD_ERR_INVALID_ARG;
     ChunkArgs a = {};
-    a.B = c->B; a.Hq = d->Hq; a.Hkv = d->Hkv; a.group = d->Hq / d->Hkv; a.T = c->total_new;
+    a.B = c->B; a.Hq = d->Hq; a.Hkv = d->Hkv; a.group = d->Hq / d->Hkv; a.T = c->total_new; a.max_new = c->max_new;
     a.tile_tokens = kRows / a.group;
     a.block_tokens = 2 * a.tile_tokens;
     a.per_block = 1.0 / a.block_tokens;

@@ -35,6 +35,8 @@ LENGTHS = {
     "mixed": ([1, 0, 200, 1, 17, 0, 300], [1000, 500, 0, 40, 2111, 0, 77]),
     "long": ([1, 5], [9000, 20000]),
     "prompt": ([1500], [0]),
+    "whole": ([0, 1, 0, 70, 3], [5, 0, 9, 100, 64]),
+    "blocks": ([0, 129, 65, 300], [64, 0, 700, 5]),
     "many": ([1, 2, 3] * 130, [17 * (i % 23) for i in range(390)]),
 }
 
@@ -79,6 +81,18 @@ def test_peaked_and_shifted_logits():
         size = float((q.float().abs().amax() * p["k_pool"].float().abs().amax()) * 128 * d ** -0.5)
         bar = attention_bar(mass) + 128 * 2.0 ** -24 * size * mass
         assert st == 0 and torch.all((out.double() - ref).abs() <= bar), what
+
+
+def test_an_output_at_16_bytes():
+    """32-byte stores are for outputs that allow them."""
+    for new, old in (([40, 1], [10, 300]), ([200], [3000])):
+        p = paged_problem(new, old, 2, 128, BF, seed=20)
+        q = p["randn"](p["T"], 8, 128)
+        want, _ = _attend(p, q, 2, 128 ** -0.5)
+        out = torch.empty(q.numel() + 8, dtype=BF, device="cuda")[8:].view(q.shape)
+        assert out.data_ptr() % 32 == 16
+        got, st = _attend(p, q, 2, 128 ** -0.5, out=out)
+        assert st == 0 and torch.equal(got, want)
 
 
 def test_scales():
@@ -248,3 +262,36 @@ def test_another_stream_and_a_graph():
         p["old"] = np.array(old)
         ref, mass = attention_reference(q, p, 128 ** -0.5)
         assert int(status.item()) == 0 and torch.all((out.double() - ref).abs() <= attention_bar(mass))
+
+
+def test_a_wait_that_runs_out_sets_the_status_and_leaves_the_context_usable():
+    """In a second library, built with short waits, CTA 0's second stage never comes: the call returns with the status set, the rows of
+    the other CTAs are right, and the product library's next launch is.  (Whole units, then units that are cut.)"""
+    import ctypes as C
+    from paper_2409_16560_b200 import build
+    lib = C.CDLL(build.build_wait_test())
+    lib.dsbd_chunk_attention_paged.argtypes = [C.c_void_p] * 8 + [C.c_size_t, C.c_void_p, C.c_void_p]
+    from paper_2409_16560_b200 import binding as bd
+    for new, old in (([5, 70, 2], [600, 300, 500]), ([40, 300, 7], [9000, 700, 6000])):
+        p = paged_problem(new, old, 2, 128, BF, seed=16)
+        q = p["randn"](p["T"], 8, 128)
+        want, st = _attend(p, q, 2, 128 ** -0.5)
+        assert st == 0
+        c = chunk_of(p)
+        desc = bd._desc(8, 2, 128, BF, 128 ** -0.5)
+        ws = torch.empty(dsbd.chunk_attention_workspace(c, 8, 2, 128, BF, 128 ** -0.5), dtype=torch.uint8, device="cuda")
+        for _ in range(2):                                    # (the first launch loads the kernel)
+            out, status = torch.zeros_like(q), torch.zeros(1, dtype=torch.int32, device="cuda")
+            begin, end = (torch.cuda.Event(enable_timing=True) for _ in range(2))
+            begin.record()
+            rc = lib.dsbd_chunk_attention_paged(c.address, C.addressof(desc), q.data_ptr(), p["k_pool"].data_ptr(), p["v_pool"].data_ptr(),
+                                                c.pages(p["k_pool"].shape[0]), out.data_ptr(), ws.data_ptr(), ws.numel(),
+                                                status.data_ptr(), torch.cuda.current_stream().cuda_stream)
+            end.record()
+            assert rc == 0
+            torch.cuda.synchronize()
+            assert int(status.item()) == 5
+        assert begin.elapsed_time(end) < 20.0                 # a millisecond a wait that runs out, and a few of them
+        assert torch.equal(out[-new[-1]:], want[-new[-1]:])   # the last sequence is other CTAs'
+        again, st = _attend(p, q, 2, 128 ** -0.5)
+        assert st == 0 and torch.equal(again, want)
