@@ -647,8 +647,9 @@ k_chunk_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
                 ok = warp_wait(&sh.s_full[x][ns & 1], (ns >> 1) & 1, &sh);
                 if (!ok) break;
                 tc_fence_after();
-                // what lies behind the block's last token has weight zero: its values become zeros
-                if ((i + 1) * kTile > end && (x == 0 || !u.wide)) {
+                // What lies behind the block's last token has weight zero: its values become zeros.  (In wide units by either group, before
+                // its own product may run: which of the two comes first is open.)
+                if ((i + 1) * kTile > end) {
                     const Stg t(base + u.ahead + i);
                     ok = warp_wait(t.full(&sh), t.parity(), &sh);
                     if (!ok) break;

@@ -121,6 +121,24 @@ def test_what_lies_behind_the_last_token_does_not_count():
             assert st == 0 and torch.equal(got, want)
 
 
+@pytest.mark.parametrize("Hq,Hkv,d", [(62, 2, 128), (8, 2, 128), (8, 8, 64)])
+def test_what_lies_behind_many_wide_blocks_does_not_count(Hq, Hkv, d):
+    """Either row tile of a wide block may be the first to come to the block's last tile."""
+    new, old = [122, 5, 300, 71, 1, 257, 130] * 6, [3, 475, 0, 65, 65, 30, 700] * 6
+    p = paged_problem(new, old, Hkv, d, BF, seed=19)
+    used = torch.zeros(p["k_pool"].shape[0], PAGE, dtype=torch.bool, device="cuda")
+    for b in range(len(new)):
+        pages = torch.as_tensor(p["table_host"][p["page_off_host"][b]:p["page_off_host"][b + 1]]).long().cuda()
+        used[pages] = (torch.arange(len(pages) * PAGE, device="cuda") < new[b] + old[b]).view(-1, PAGE)
+    for pool in (p["k_pool"], p["v_pool"]):
+        pool[~used[:, None].expand(-1, Hkv, -1)] = float("nan")
+    q = p["randn"](p["T"], Hq, d)
+    first = _check(p, q, Hkv, d ** -0.5)
+    for _ in range(20):
+        out, st = _attend(p, q, Hkv, d ** -0.5)
+        assert st == 0 and torch.equal(out, first)
+
+
 def test_rows_of_bad_numbers_stay_their_own():
     """A query row of NaN or infinities gives NaN and leaves its neighbours alone."""
     p = paged_problem([60, 1], [200, 40], 2, 128, BF, seed=10)
