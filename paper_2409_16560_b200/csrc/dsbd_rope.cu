@@ -138,6 +138,29 @@ template <> struct Four<__nv_bfloat16> {
     }
 };
 
+// Two fp32 operations an instruction (sm_100): the kernel below has 65 % of its issue slots full with single ones.
+struct F2 { float x, y; };
+__device__ __forceinline__ F2 mul2(F2 a, F2 b) {
+    F2 d;
+    asm("{\n\t.reg .b64 a, b, d;\n\tmov.b64 a, {%2, %3};\n\tmov.b64 b, {%4, %5};\n\t"
+        "mul.rn.f32x2 d, a, b;\n\tmov.b64 {%0, %1}, d;\n\t}"
+        : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+    return d;
+}
+__device__ __forceinline__ F2 fma2(F2 a, F2 b, F2 c) {
+    F2 d;
+    asm("{\n\t.reg .b64 a, b, c, d;\n\tmov.b64 a, {%2, %3};\n\tmov.b64 b, {%4, %5};\n\tmov.b64 c, {%6, %7};\n\t"
+        "fma.rn.f32x2 d, a, b, c;\n\tmov.b64 {%0, %1}, d;\n\t}"
+        : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
+    return d;
+}
+// (u, v) turned, two pairs: (u c - v s, v c + u s); ms = -s
+__device__ __forceinline__ void turn2(F2 &u, F2 &v, F2 c, F2 s, F2 ms) {
+    const F2 t = fma2(v, ms, mul2(u, c));
+    v = fma2(u, s, mul2(v, c));
+    u = t;
+}
+
 struct RopeArgs {
     int T, Hq, Hkv;
     int q_pieces, k_pieces, pieces;                  // pieces of a few warp steps: of q, of k; all of a token (v's too)
@@ -228,13 +251,13 @@ k_rotate(RopeArgs a) {
         r.heads = r.kind == 0 ? a.Hq : a.Hkv;
         const T *src = r.kind == 0 ? static_cast<const T *>(a.q) + t * a.q_stride
                      : r.kind == 1 ? static_cast<const T *>(a.k) + t * a.k_stride : static_cast<const T *>(a.v) + t * a.v_stride;
+        src += (int64_t)r.first * D;
 #pragma unroll
         for (int u = 0; u < kUnroll; ++u) {
-            const int h = r.first + u * kHeads;
             r.x[u] = r.y[u] = Raw{};
-            if (h < r.heads) {
-                r.x[u] = *reinterpret_cast<const Raw *>(src + (int64_t)h * D + e0);
-                r.y[u] = *reinterpret_cast<const Raw *>(src + (int64_t)h * D + e1);
+            if (r.first + u * kHeads < r.heads) {
+                r.x[u] = *reinterpret_cast<const Raw *>(src + u * kHeads * D + e0);
+                r.y[u] = *reinterpret_cast<const Raw *>(src + u * kHeads * D + e1);
             }
         }
         return r;
@@ -278,6 +301,7 @@ k_rotate(RopeArgs a) {
         c = *reinterpret_cast<const float4 *>(cs);
         s = *reinterpret_cast<const float4 *>(cs + half);
     }
+    const F2 c0 = {c.x, c.y}, c1 = {c.z, c.w}, s0 = {s.x, s.y}, s1 = {s.z, s.w}, m0 = {-s.x, -s.y}, m1 = {-s.z, -s.w};
 
     for (;;) {
         const int kind = now.kind;
@@ -292,48 +316,52 @@ k_rotate(RopeArgs a) {
         } else {
             dst = static_cast<T *>(a.k_out) + t * a.k_out_stride;
         }
-        float4 w0 = {}, w1 = {};
-        if (norm) {
-            w0 = *reinterpret_cast<const float4 *>(norm + e0);
-            w1 = *reinterpret_cast<const float4 *>(norm + e1);
-        }
+        dst += now.first * pitch;
+        if (kind != 2 && (norm || turned)) {         // (everything else keeps its bits; a head's lanes agree where there is a norm)
+            float4 w0 = {1.f, 1.f, 1.f, 1.f}, w1 = {1.f, 1.f, 1.f, 1.f};
+            if (norm) {
+                w0 = *reinterpret_cast<const float4 *>(norm + e0);
+                w1 = *reinterpret_cast<const float4 *>(norm + e1);
+            }
 #pragma unroll
-        for (int u = 0; u < kUnroll; ++u) {
-            const int h = now.first + u * kHeads;
-            if (kind != 2 && (norm || turned)) {     // (everything else keeps its bits; a head's lanes agree where there is a norm)
+            for (int u = 0; u < kUnroll; ++u) {
                 float x[4], y[4];
                 F::widen(now.x[u], x);
                 F::widen(now.y[u], y);
+                F2 x0 = {x[0], x[1]}, x1 = {x[2], x[3]}, y0 = {y[0], y[1]}, y1 = {y[2], y[3]};
                 if (norm) {
-                    float ss = 0.f;
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) ss = fmaf(x[e], x[e], fmaf(y[e], y[e], ss));
+                    const F2 q = fma2(x0, x0, fma2(x1, x1, fma2(y0, y0, mul2(y1, y1))));
+                    float ss = q.x + q.y;
 #pragma unroll
                     for (int o = kLanes / 2; o > 0; o >>= 1) ss += __shfl_xor_sync(kFull, ss, o);
                     const float r = rsqrtf(ss * (1.f / D) + a.eps);
-                    x[0] *= r * w0.x; x[1] *= r * w0.y; x[2] *= r * w0.z; x[3] *= r * w0.w;
-                    y[0] *= r * w1.x; y[1] *= r * w1.y; y[2] *= r * w1.z; y[3] *= r * w1.w;
+                    const F2 rr = {r, r};
+                    x0 = mul2(mul2(x0, rr), F2{w0.x, w0.y}); x1 = mul2(mul2(x1, rr), F2{w0.z, w0.w});
+                    y0 = mul2(mul2(y0, rr), F2{w1.x, w1.y}); y1 = mul2(mul2(y1, rr), F2{w1.z, w1.w});
                 }
                 if (turned) {
-                    auto turn = [](float &p, float &q, float cc, float sn) {
-                        const float v = p;
-                        p = fmaf(v, cc, -q * sn);
-                        q = fmaf(q, cc, v * sn);
-                    };
                     if (by_half) {
-                        turn(x[0], y[0], c.x, s.x); turn(x[1], y[1], c.y, s.y); turn(x[2], y[2], c.z, s.z); turn(x[3], y[3], c.w, s.w);
+                        turn2(x0, y0, c0, s0, m0);
+                        turn2(x1, y1, c1, s1, m1);
                     } else {
-                        turn(x[0], x[1], c.x, s.x); turn(x[2], x[3], c.y, s.y); turn(y[0], y[1], c.z, s.z); turn(y[2], y[3], c.w, s.w);
+                        F2 u0 = {x0.x, x1.x}, v0 = {x0.y, x1.y}, u1 = {y0.x, y1.x}, v1 = {y0.y, y1.y};
+                        turn2(u0, v0, c0, s0, m0);
+                        turn2(u1, v1, c1, s1, m1);
+                        x0 = {u0.x, v0.x}; x1 = {u0.y, v0.y}; y0 = {u1.x, v1.x}; y1 = {u1.y, v1.y};
                     }
                 }
+                x[0] = x0.x; x[1] = x0.y; x[2] = x1.x; x[3] = x1.y;
+                y[0] = y0.x; y[1] = y0.y; y[2] = y1.x; y[3] = y1.y;
                 now.x[u] = F::narrow(x);
                 now.y[u] = F::narrow(y);
             }
-            if (h < now.heads) {
-                *reinterpret_cast<Raw *>(dst + h * pitch + e0) = now.x[u];
-                *reinterpret_cast<Raw *>(dst + h * pitch + e1) = now.y[u];
-            }
         }
+#pragma unroll
+        for (int u = 0; u < kUnroll; ++u)
+            if (now.first + u * kHeads < now.heads) {
+                *reinterpret_cast<Raw *>(dst + u * kHeads * pitch + e0) = now.x[u];
+                *reinterpret_cast<Raw *>(dst + u * kHeads * pitch + e1) = now.y[u];
+            }
         if (++piece >= piece_end) break;
         now = load(piece);
     }
