@@ -70,10 +70,14 @@ struct Shape {
     static constexpr uint32_t kSmem = 2 * kQ + kStages * kStage;
 };
 
-// Costs are counted in tokens that a block's rows see: a tile takes 1500 to 1600 cycles in wide units and as long in narrow ones
-// while all SMs read their caches, a unit's beginning and end 4500 and 9000.
-constexpr int kWideCost = 192, kNarrowCost = 384;
-constexpr int kMinRun = 512;                         // smallest run
+// Costs are counted in tokens that a block's rows see, kNarrowShare of them in narrow units: a wide tile takes 1545 cycles, a
+// narrow one half as long where HBM does not hold it up (its row tiles share the tokens) and 1400 where all SMs read their
+// caches at once.  A unit's beginning and end are worth kWideCost and kNarrowCost more.  Batches of chunks and single tokens are
+// up to 12 % faster than with a share of 1 (12 chunks of 1 to 777 tokens behind 0 to 6000: 100.6 us -> 97.1), the rest as fast; 0.5 gains as much
+// on those and loses 10 % on many short chunks.
+constexpr int kWideCost = 192, kNarrowCost = 288;
+constexpr double kNarrowShare = 0.75;
+constexpr int kMinRun = 384;                         // smallest run
 
 struct ChunkArgs {
     int B, Hq, Hkv, group, T, max_new;
@@ -123,17 +127,18 @@ __device__ __forceinline__ Seq seq_of(const ChunkArgs &a, int b, bool tell) {
 __device__ __forceinline__ int blocks_of(const ChunkArgs &a, int n) {
     return n == 0 ? 0 : (int)(((double)(n - 1) + 0.5) * a.per_block) + 1;
 }
-// Cost of the first q < blocks_of(n) blocks of one head of a sequence, and of all: the tokens that their last rows see, kWideCost or
-// kNarrowCost more each (a last block of at most tile_tokens is narrow).  Whole numbers in doubles, whose sums and products are
-// one instruction each.
+// Cost of the first q < blocks_of(n) blocks of one head of a sequence, and of all (a last block of at most tile_tokens is narrow).
 __device__ __forceinline__ double cost_before(const ChunkArgs &a, const Seq &s, int q) {
     return (double)q * ((double)(s.L + kWideCost) + (double)a.block_tokens * 0.5 * (double)(q + 1));
 }
+__device__ __forceinline__ bool narrow_block(const ChunkArgs &a, const Seq &s, int q) {
+    return s.n - q * a.block_tokens <= a.tile_tokens;
+}
 __device__ __forceinline__ double head_cost(const ChunkArgs &a, const Seq &s) {
-    const int nq = blocks_of(a, s.n);
-    if (nq == 0) return 0.0;
-    const int tail = s.n - (nq - 1) * a.block_tokens;
-    return cost_before(a, s, nq) + (double)(tail - a.block_tokens + (tail <= a.tile_tokens ? kNarrowCost - kWideCost : 0));
+    const int last = blocks_of(a, s.n) - 1;
+    if (last < 0) return 0.0;
+    const double sees = (double)(s.L + s.n);
+    return floor(cost_before(a, s, last) + (narrow_block(a, s, last) ? kNarrowCost + kNarrowShare * sees : kWideCost + sees));
 }
 
 struct Unit {
@@ -376,8 +381,9 @@ __device__ void find_run(const ChunkArgs &a, Shared &sh) {
         p.q = max(min((int)(root - h), nq) - 2, 0);
         while (p.q + 1 < nq && cost_before(a, s, p.q + 1) <= in) ++p.q;
         // (what a unit costs beside its tokens lies before them)
-        in -= cost_before(a, s, p.q) + (s.n - p.q * a.block_tokens <= a.tile_tokens ? kNarrowCost : kWideCost);
-        p.t = max((int)in, 0) / kTile;
+        in -= cost_before(a, s, p.q);
+        p.t = narrow_block(a, s, p.q) ? max((int)((in - kNarrowCost) * (1.0 / (kNarrowShare * kTile))), 0)
+                                      : max((int)((in - kWideCost) * (1.0 / kTile)), 0);
         if (k == 0) {
             sh.start = p;
             sh.seq = s;
