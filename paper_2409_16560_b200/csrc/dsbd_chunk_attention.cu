@@ -286,16 +286,18 @@ __device__ __forceinline__ F2 add2(F2 a, F2 b) {
         : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
     return d;
 }
+// NaN if any of the three is.
 __device__ __forceinline__ float max3(float a, float b, float c) {
     float d;
-    asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+    asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
     return d;
 }
 
 // 2^z for z <= 120 on the FMA and integer pipes, which are idle while ex2 (a quarter of a warp's lanes a cycle) sets the pace:
 // z = n + f with n the nearest integer (what 1.5 * 2^23 leaves in the low bits), 2^f by a cubic fitted to the smallest relative
 // error on [-1/2, 1/2] with 1 at f = 0 (1.0e-4; the weights are rounded to bf16, 3.9e-3), n into the exponent.
-// From -127 down, -infinity included, the result is 0.
+// From -127 down, -infinity included, the result is 0; for a NaN it is 0 too (the integer addition would make a number of it
+// in any case), so a row's NaN is noticed by its maximum.
 __device__ __forceinline__ F2 exp2_poly(F2 z) {
     const F2 big = {12582912.f, 12582912.f};
     z.x = fmaxf(z.x, -127.f);
@@ -688,8 +690,8 @@ k_chunk_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
 #pragma unroll
                     for (int c = 0; c < kTile; c += 2)
                         m4[(c >> 1) & 3] = max3(m4[(c >> 1) & 3], __uint_as_float(sv[c >> 5][c & 31]), __uint_as_float(sv[c >> 5][(c & 31) + 1]));
-                    const float mx = fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3])) * a.scale_log2;    // scale > 0
-                    const bool need = mx > m_ref + kMoveRef;
+                    const float mx = max3(max3(m4[0], m4[1], m4[2]), m4[3], m4[3]) * a.scale_log2;      // scale > 0
+                    const bool need = mx > m_ref + kMoveRef;         // (not for a NaN: the reference stays as it is)
                     if (__any_sync(kFull, need)) {
                         const float m_new = need ? mx : m_ref;
                         const float f = m_ref == -INFINITY ? 0.f : exp2f(m_ref - m_new);
@@ -728,6 +730,7 @@ k_chunk_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
                         tmem_st16(s_addr + c * 16, pv);
                     }
                     l += (l2[0].x + l2[0].y) + (l2[1].x + l2[1].y);
+                    if (mx != mx) l = mx;                            // a logit that the row sees is NaN: so is its result, through every join
                     tmem_wait_st();
                 }
                 tc_fence_before();
