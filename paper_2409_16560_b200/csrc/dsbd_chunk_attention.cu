@@ -22,8 +22,12 @@
 // Masks: a unit ends with the tile of its block's last token; in the last tiles a row sees the tokens up to its own.  V rows
 // behind the block's last token are cleared in shared memory, so that nothing in the pages behind it counts.
 // A row's reference is its running maximum, moved only when a logit exceeds it by more than 2^8.  P is rounded to bf16, the operand
-// type of V (3.9e-3 of a weight at most, 1.6e-3 on average over random weights, as much as the output's own rounding); the row sum
-// adds the weights before that: adding the rounded ones cost two more instructions a weight.
+// type of V: a weight is off by 3.9e-3 of itself at most, a row of random weights by 1.6e-3 on average, as much as by the output's own
+// rounding.  The row sum adds the rounded weights, so that the rounding cancels where it is common to a row (one heavy
+// weight, many equal ones; a value that all positions share comes back exactly).  The sum of the weights before their rounding
+// leaves up to 3.9e-3 of such a row and is 1.5 % faster with heads of 128 (16384 tokens 1727 us instead of 1755), 3 to 5 % with
+// heads of 64.  A second term of the weights, as the forest attention has it for heads of 64, would be a second product of O and
+// more instructions for the softmax, which bound heads of 64 here already.
 //
 // Work split: the tiles of all units form one sequence (sequence, KV head, block), cut into runs of equal cost, one per CTA; a unit
 // that straddles a cut leaves partial results that k_chunk_merge joins.  Few short units are taken whole, one a CTA.  Every
@@ -725,7 +729,7 @@ k_chunk_attn(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
                                               F2{a.scale_log2, a.scale_log2}, F2{neg, neg});
                             const F2 w2 = e % 8 < kPolyOf8 ? exp2_poly(z) : F2{ex2_ftz(z.x), ex2_ftz(z.y)};
                             pv[e] = pack_bf16(w2.x, w2.y);
-                            l2[e & 1] = add2(l2[e & 1], w2);
+                            l2[e & 1] = add2(l2[e & 1], F2{bf16_lo(pv[e]), bf16_hi(pv[e])});
                         }
                         tmem_st16(s_addr + c * 16, pv);
                     }

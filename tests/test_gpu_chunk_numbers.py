@@ -82,3 +82,48 @@ def test_infinite_keys(shape, d):
         r = slice(int(p["new_off_host"][b]), int(p["new_off_host"][b + 1]))
         kinds |= {bool(x) for x in bad[r].flatten()[:: max(bad[r].numel() // 4096, 1)]}
     assert kinds == {True, False}
+
+
+def _constant_values(p, q, Hkv, scale, c):
+    p["v_pool"].fill_(c)
+    return _attend(p, q, Hkv, scale)
+
+
+# Just below 2 and 1: the neighbour above 255/128 is 2, half a step of 2^-8 = 1.96e-3 away; the one below 1 is 2^-9 away.
+CONSTANTS = (255 / 128, 1.0, -1.0, -255 / 128)
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("lengths", [([300], [0]), ([1, 40, 2], [3000, 700, 20000]), ([1] * 20, [40 + 50 * i for i in range(20)])])
+def test_values_that_are_all_alike_come_back(lengths, d):
+    """Weights that sum to one give back a value that all positions share.  The weights are rounded to bf16 for the product; when the
+    row sum adds those same rounded weights the rounding cancels, and what is left are fp32 sums of up to 20002 terms of one
+    sign, errors of a random walk: sqrt(20002) 2^-24 < 1e-5, far below the half step of 1.95e-3 to a neighbouring bf16, so
+    the result is exact.  A sum of the weights before their rounding is off by up to 3.9e-3 where a row's weights round alike."""
+    new, old = lengths
+    p = paged_problem(new, old, 2, d, BF, seed=31)
+    for peak in (1.0, 6.0):                                   # broad rows, and rows of one or two heavy weights
+        q = (p["randn"](p["T"], 8, d).float() * peak).to(BF)
+        for c in CONSTANTS:
+            out = _constant_values(p, q, 2, d ** -0.5, c)
+            assert torch.all(out == c), (peak, c, float((out.float() - c).abs().max()))
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("weight", [0.50205, 0.50185, 0.2511, 0.2508, 0.7285])
+def test_equal_weights_beside_a_heavier_one(weight, d):
+    """The first key of a sequence is the maximum, all others have the same weight just off the middle between two bf16 values (at
+    0.50205 it rounds up by 3.7e-3 of itself, at 0.50185 down by as much)."""
+    import math
+    for new, old in (([70], [300]), ([1, 1], [2000, 6000])):
+        p = paged_problem(new, old, 1, d, BF, seed=1)
+        q = torch.zeros(p["T"], 4, d, dtype=BF, device="cuda")
+        q[..., 0] = 1.0
+        p["k_pool"].zero_()
+        p["k_pool"][..., 0] = -1.0
+        for b in range(len(new)):
+            page, row = _place(p, b, 0)
+            p["k_pool"][page, :, row, 0] = 0.0
+        for c in CONSTANTS:
+            out = _constant_values(p, q, 1, -math.log(weight), c)
+            assert torch.all(out == c), (c, float((out.float() - c).abs().max()))
