@@ -808,15 +808,22 @@ def _on_device(*tensors):
 
 
 def _status(status, device):
-    return torch.zeros(1, dtype=torch.int32, device=device) if status is None else status
+    """The caller's status word, or a new one."""
+    if status is None:
+        return torch.zeros(1, dtype=torch.int32, device=device)
+    if not status.is_cuda or status.dtype != torch.int32 or status.numel() < 1:
+        raise AssertionError("the status word is an int32 on the device")
+    return status
 
 
 def forest_positions(forest, prefix_off, position=None, status=None, stream=None):
     """dsbd_forest_positions: position[n] = prefix length of node n's beam + its depth, int32 [N]; returns (position, status)."""
-    _on_device(prefix_off)
+    _on_device(prefix_off, forest.dev["beam_node_off"], forest.dev["parent"])
+    assert prefix_off.dtype == torch.int64 and prefix_off.numel() == forest.B + 1
     f = ForestT(0, forest.B, forest.N, 0, None, _ptr(forest.dev["beam_node_off"]), _ptr(forest.dev["parent"]))
     if position is None:
         position = torch.empty(forest.N, dtype=torch.int32, device=prefix_off.device)
+    _on_device(position)
     assert position.dtype == torch.int32 and position.numel() >= forest.N
     status = _status(status, prefix_off.device)
     rc = load().dsbd_forest_positions(C.addressof(f), _ptr(prefix_off), _ptr(position), _ptr(status), _stream(stream))
@@ -915,9 +922,11 @@ def chunk_attention_paged(chunk, Hq, Hkv, d, scale, q, k_pool, v_pool, out=None,
     assert out.is_contiguous()
     if workspace is None:
         workspace = _workspace(load().dsbd_chunk_attention_paged_workspace(chunk.address, C.addressof(desc)), q.device)
+    else:
+        _on_device(workspace)
     status = _status(status, q.device)
     rc = load().dsbd_chunk_attention_paged(chunk.address, C.addressof(desc), q.data_ptr(), k_pool.data_ptr(), v_pool.data_ptr(),
-                                           chunk.pages(n_pages), out.data_ptr(), workspace.data_ptr(),
+                                           chunk.pages(n_pages), out.data_ptr(), _ptr(workspace),
                                            workspace.numel() * workspace.element_size(), status.data_ptr(), _stream(stream))
     if rc != OK:
         raise DsbdError("dsbd_chunk_attention_paged", rc)
