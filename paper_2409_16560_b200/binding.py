@@ -187,8 +187,17 @@ def _widest(off):
     return max(d.tolist()) if 0 < len(d) <= 64 else int(d.max()) if len(d) else 0
 
 
-def _workspace(need, device):
-    return torch.empty(max(int(need), 256), dtype=torch.uint8, device=device)
+def _made_on(stream, make, shape, dtype, device):
+    """make(shape) on the stream that a call runs on: a tensor's filling comes before the call's kernels there, and memory that
+    the call alone holds does not go to work of another stream while they run."""
+    if stream is None:
+        return make(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(stream):
+        return make(shape, dtype=dtype, device=device)
+
+
+def _workspace(need, device, stream=None):
+    return _made_on(stream, torch.empty, max(int(need), 256), torch.uint8, device)
 
 
 def _require_cuda(*tensors):
@@ -711,7 +720,7 @@ def rope_table(n_positions, rot, base=10000.0, scaling=None, device="cuda", tabl
     """dsbd_rope_table: fp32 [n_positions, 2, rot / 2], cosines and sines.  Made once per model."""
     s = _scaling(base, scaling)
     if table is None:
-        table = torch.empty(int(n_positions), 2, int(rot) // 2, dtype=torch.float32, device=device)
+        table = _made_on(stream, torch.empty, (int(n_positions), 2, int(rot) // 2), torch.float32, device)
     _require_cuda(table)
     assert table.dtype == torch.float32 and tuple(table.shape) == (int(n_positions), 2, int(rot) // 2)
     rc = load().dsbd_rope_table(C.addressof(s), int(rot), int(n_positions), _ptr(table), _stream(stream))
@@ -791,10 +800,10 @@ def _row_stride(t, H, d):
     return a if a >= H * d or t.shape[0] > 1 else H * d
 
 
-def _alike(out, t):
+def _alike(out, t, stream):
     """An output tensor like `t` in shape and type."""
     if out is None:
-        return torch.empty(t.shape, dtype=t.dtype, device=t.device)
+        return _made_on(stream, torch.empty, t.shape, t.dtype, t.device)
     if out.shape != t.shape or out.dtype != t.dtype:
         raise AssertionError("the output has the input's shape and type")
     _on_device(out)
@@ -807,10 +816,10 @@ def _on_device(*tensors):
             _require_cuda(t)
 
 
-def _status(status, device):
+def _status(status, device, stream):
     """The caller's status word, or a new one."""
     if status is None:
-        return torch.zeros(1, dtype=torch.int32, device=device)
+        return _made_on(stream, torch.zeros, 1, torch.int32, device)
     if not status.is_cuda or status.dtype != torch.int32 or status.numel() < 1:
         raise AssertionError("the status word is an int32 on the device")
     return status
@@ -822,10 +831,10 @@ def forest_positions(forest, prefix_off, position=None, status=None, stream=None
     assert prefix_off.dtype == torch.int64 and prefix_off.numel() == forest.B + 1
     f = ForestT(0, forest.B, forest.N, 0, None, _ptr(forest.dev["beam_node_off"]), _ptr(forest.dev["parent"]))
     if position is None:
-        position = torch.empty(forest.N, dtype=torch.int32, device=prefix_off.device)
+        position = _made_on(stream, torch.empty, forest.N, torch.int32, prefix_off.device)
     _on_device(position)
     assert position.dtype == torch.int32 and position.numel() >= forest.N
-    status = _status(status, prefix_off.device)
+    status = _status(status, prefix_off.device, stream)
     rc = load().dsbd_forest_positions(C.addressof(f), _ptr(prefix_off), _ptr(position), _ptr(status), _stream(stream))
     if rc != OK:
         raise DsbdError("dsbd_forest_positions", rc)
@@ -843,18 +852,18 @@ def rotate_qk(q, k, position, rope, q_out=None, k_out=None, status=None, stream=
     qp = kp = qo = ko = None
     qs = ks = qos = kos = 0
     if q is not None:
-        q_out = _alike(q_out, q)
+        q_out = _alike(q_out, q, stream)
         qp, qs, qo, qos = q.data_ptr(), _row_stride(q, Hq, d), q_out.data_ptr(), _row_stride(q_out, Hq, d)
     if k is not None:
         Tk, Hkv, dk = k.shape
         assert k.dtype == dtype and Tk == T and dk == d
         _on_device(k)
-        k_out = _alike(k_out, k)
+        k_out = _alike(k_out, k, stream)
         kp, ks, ko, kos = k.data_ptr(), _row_stride(k, Hkv, d), k_out.data_ptr(), _row_stride(k_out, Hkv, d)
     if position is not None:
         _on_device(position)
         assert position.dtype == torch.int32 and position.numel() == T
-    status = _status(status, x.device)
+    status = _status(status, x.device, stream)
     desc = _desc(Hq if q is not None else Hkv, Hkv, d, dtype)
     rc = load().dsbd_rotate_qk(T, C.addressof(desc), rope.address, _ptr(position), qp, qs, kp,
                                ks, qo, qos, ko, kos, status.data_ptr(), _stream(stream))
@@ -887,9 +896,9 @@ def kv_append_paged(chunk, k, v, k_pool, v_pool, rope=None, q=None, q_out=None, 
         Tq, Hq, dq = q.shape
         assert Tq == T and dq == d and q.dtype == dtype
         _on_device(q)
-        q_out = _alike(q_out, q)
+        q_out = _alike(q_out, q, stream)
         qp, qs, qo, qos = q.data_ptr(), _row_stride(q, Hq, d), q_out.data_ptr(), _row_stride(q_out, Hq, d)
-    status = _status(status, k.device)
+    status = _status(status, k.device, stream)
     desc = _desc(Hq, Hkv, d, dtype)
     rc = load().dsbd_kv_append_paged(chunk.address, C.addressof(desc), rope.address if rope is not None else None, qp, qs,
                                      k.data_ptr(), _row_stride(k, Hkv, d), v.data_ptr(), _row_stride(v, Hkv, d), qo, qos,
@@ -918,13 +927,13 @@ def chunk_attention_paged(chunk, Hq, Hkv, d, scale, q, k_pool, v_pool, out=None,
     assert q.shape == (chunk.total_new, Hq, d) and q.is_contiguous()
     n_pages = _pools(k_pool, v_pool, Hkv, d, dtype)
     desc = _desc(Hq, Hkv, d, dtype, scale)
-    out = _alike(out, q)
+    out = _alike(out, q, stream)
     assert out.is_contiguous()
     if workspace is None:
-        workspace = _workspace(load().dsbd_chunk_attention_paged_workspace(chunk.address, C.addressof(desc)), q.device)
+        workspace = _workspace(load().dsbd_chunk_attention_paged_workspace(chunk.address, C.addressof(desc)), q.device, stream)
     else:
         _on_device(workspace)
-    status = _status(status, q.device)
+    status = _status(status, q.device, stream)
     rc = load().dsbd_chunk_attention_paged(chunk.address, C.addressof(desc), q.data_ptr(), k_pool.data_ptr(), v_pool.data_ptr(),
                                            chunk.pages(n_pages), out.data_ptr(), _ptr(workspace),
                                            workspace.numel() * workspace.element_size(), status.data_ptr(), _stream(stream))
