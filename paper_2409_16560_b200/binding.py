@@ -196,7 +196,11 @@ def _made_on(stream, make, shape, dtype, device):
         return make(shape, dtype=dtype, device=device)
 
 
-def _workspace(need, device, stream=None):
+def _minus_ones(n, dtype, device):
+    return torch.full((n,), -1, dtype=dtype, device=device)
+
+
+def _workspace(need, device, stream):
     return _made_on(stream, torch.empty, max(int(need), 256), torch.uint8, device)
 
 
@@ -298,11 +302,10 @@ def forest_attention(forest, Hq, Hkv, d, scale, q, k_new, v_new, k_prefix, v_pre
     f = forest.struct()
     desc = _attn_desc(Hq, Hkv, d, q.dtype, scale, prefix_off_host)
     if out is None:
-        out = torch.empty_like(q)
+        out = _alike(None, q, stream)
     if workspace is None:
-        workspace = _workspace(load().dsbd_forest_attention_workspace(C.addressof(f), C.addressof(desc)), q.device)
-    if status is None:
-        status = torch.zeros(1, dtype=torch.int32, device=q.device)
+        workspace = _workspace(load().dsbd_forest_attention_workspace(C.addressof(f), C.addressof(desc)), q.device, stream)
+    status = _status(status, q.device, stream)
     rc = load().dsbd_forest_attention(C.addressof(f), C.addressof(desc), _ptr(q), _ptr(k_new), _ptr(v_new),
                                       _ptr(k_prefix), _ptr(v_prefix), _ptr(prefix_off), _ptr(out),
                                       _ptr(workspace), workspace.numel(), _ptr(status), _stream(stream))
@@ -323,13 +326,12 @@ def forest_build(req_beam_off, req_beam_off_host, gamma, W_S, draw_parent, draw_
     rbo = np.asarray(req_beam_off_host)
     R, B = len(rbo) - 1, int(rbo[-1])
     N = B + gamma * R * W_S
-    i32 = lambda n: torch.empty(n, dtype=torch.int32, device=dev)
+    i32 = lambda shape, make=torch.empty: _made_on(stream, make, shape, torch.int32, dev)
     arrays = dict(req_beam_off=req_beam_off, beam_node_off=i32(B + 1), parent=i32(N), token=i32(N),
                   draft_rank=i32(N))
-    node_of_draw = torch.empty(gamma, R * W_S, dtype=torch.int32, device=dev)
-    if status is None:
-        status = torch.zeros(1, dtype=torch.int32, device=dev)
-    largest = torch.zeros(1, dtype=torch.int32, device=dev) if exact else None
+    node_of_draw = i32((gamma, R * W_S))
+    status = _status(status, dev, stream)
+    largest = i32(1, torch.zeros) if exact else None
     rc = load().dsbd_forest_build(R, gamma, W_S, _ptr(req_beam_off), _ptr(draw_parent), _ptr(draw_token),
                                   _ptr(arrays["beam_node_off"]), _ptr(arrays["parent"]), _ptr(arrays["token"]),
                                   _ptr(arrays["draft_rank"]), _ptr(node_of_draw),
@@ -359,7 +361,7 @@ def forest_attention_paged(forest, Hq, Hkv, d, scale, q, k_new, v_new, k_pool, v
     pages = KvPagesT()
     pages.page_table, pages.page_off, pages.n_pages = _ptr(page_table), _ptr(page_off), int(k_pool.shape[-4])
     if out is None:
-        out = torch.empty_like(q)
+        out = _alike(None, q, stream)
     if k_pool.dim() == 5:
         pages.n_layers = int(k_pool.shape[0])
         assert q.dim() == 4 and k_new.dim() == 4 and q.shape[0] == k_new.shape[0] == pages.n_layers
@@ -368,9 +370,8 @@ def forest_attention_paged(forest, Hq, Hkv, d, scale, q, k_new, v_new, k_pool, v
         pages.pool_layer_stride, pages.new_layer_stride = int(k_pool.stride(0)), int(k_new.stride(0))
         pages.q_layer_stride = int(q.stride(0))
     if workspace is None:
-        workspace = _workspace(load().dsbd_forest_attention_paged_workspace(C.addressof(f), C.addressof(desc), C.addressof(pages)), q.device)
-    if status is None:
-        status = torch.zeros(1, dtype=torch.int32, device=q.device)
+        workspace = _workspace(load().dsbd_forest_attention_paged_workspace(C.addressof(f), C.addressof(desc), C.addressof(pages)), q.device, stream)
+    status = _status(status, q.device, stream)
     rc = load().dsbd_forest_attention_paged(C.addressof(f), C.addressof(desc), _ptr(q), _ptr(k_new), _ptr(v_new),
                                             _ptr(k_pool), _ptr(v_pool), C.addressof(pages), _ptr(prefix_off),
                                             _ptr(out), _ptr(workspace), workspace.numel(), _ptr(status),
@@ -405,14 +406,12 @@ def draft_layer(req_beam_off, req_beam_off_host, params, layer, W_S, logits_q, b
                      int(params.get("seed", 0)), int(params.get("step", 0)), int(layer), int(params.get("top_k", 0)),
                      float(params.get("top_p", 1.0)), int(n_slots), _widest(rbo))
     if workspace is None:
-        workspace = _workspace(load().dsbd_draft_workspace(R, n_beams, C.addressof(p)), dev)
-    if status is None:
-        status = torch.zeros(1, dtype=torch.int32, device=dev)
+        workspace = _workspace(load().dsbd_draft_workspace(R, n_beams, C.addressof(p)), dev, stream)
+    status = _status(status, dev, stream)
+    new = lambda make, n, dtype: _made_on(stream, make, int(n), dtype, dev)
     res = out if out is not None else dict(
-        out_parent=torch.full((int(n_slots),), -1, dtype=torch.int32, device=dev),
-        out_token=torch.full((int(n_slots),), -1, dtype=torch.int32, device=dev),
-        out_logq=torch.zeros(int(n_slots), dtype=torch.float32, device=dev),
-        req_error=torch.zeros(R, dtype=torch.int32, device=dev))
+        out_parent=new(_minus_ones, n_slots, torch.int32), out_token=new(_minus_ones, n_slots, torch.int32),
+        out_logq=new(torch.zeros, n_slots, torch.float32), req_error=new(torch.zeros, R, torch.int32))
     res["status"], res["workspace"] = status, workspace
     stride = int(row_stride) if row_stride is not None else int(logits_q.stride(0))
     rc = load().dsbd_draft_layer(R, n_beams, _ptr(req_beam_off), C.addressof(p), _ptr(logits_q), stride,
@@ -440,21 +439,21 @@ def kv_commit(forest, Hkv, d, out_off, out_width, out_parent, out_root_beam, out
     desc = _attn_desc(Hkv, Hkv, d, k_new.dtype, 1.0, prefix_off_host)
     p = CommitParamsT()
     p.n_slots, p.keep_best, p.dst_capacity = int(n_slots), int(bool(keep_best)), int(dst_capacity)
+    new = lambda n, dtype: _made_on(stream, torch.empty, int(n), dtype, dev)
     if k_dst is None:
-        k_dst = torch.empty(int(dst_capacity) * Hkv * d, dtype=k_new.dtype, device=dev)
+        k_dst = new(int(dst_capacity) * Hkv * d, k_new.dtype)
     if v_dst is None:
-        v_dst = torch.empty(int(dst_capacity) * Hkv * d, dtype=k_new.dtype, device=dev)
+        v_dst = new(int(dst_capacity) * Hkv * d, k_new.dtype)
     if workspace is None:
-        workspace = _workspace(load().dsbd_kv_commit_workspace(C.addressof(f), C.addressof(p)), dev)
-    if status is None:
-        status = torch.zeros(1, dtype=torch.int32, device=dev)
+        workspace = _workspace(load().dsbd_kv_commit_workspace(C.addressof(f), C.addressof(p)), dev, stream)
+    status = _status(status, dev, stream)
     if out is not None:
         new_req_beam_off, new_prefix_off, new_beam_slot = (out[k] for k in ("new_req_beam_off", "new_prefix_off",
                                                                               "new_beam_slot"))
     else:
-        new_req_beam_off = torch.empty(forest.R + 1, dtype=torch.int32, device=dev)
-        new_prefix_off = torch.empty(int(n_slots) + 1, dtype=torch.int64, device=dev)
-        new_beam_slot = torch.empty(int(n_slots), dtype=torch.int32, device=dev)
+        new_req_beam_off = new(forest.R + 1, torch.int32)
+        new_prefix_off = new(int(n_slots) + 1, torch.int64)
+        new_beam_slot = new(n_slots, torch.int32)
     rc = load().dsbd_kv_commit(C.addressof(f), C.addressof(desc), C.addressof(p), _ptr(out_off), _ptr(out_width),
                                _ptr(out_parent), _ptr(out_root_beam), _ptr(out_logp) if out_logp is not None else None,
                                _ptr(k_new), _ptr(v_new), _ptr(k_prefix), _ptr(v_prefix), _ptr(prefix_off),
@@ -491,15 +490,15 @@ def kv_commit_paged(forest, Hkv, d, out_off, out_width, out_parent, out_root_bea
     pages.page_table, pages.page_off = _ptr(page_table), _ptr(page_off)
     pages.n_pages = int(k_pool.shape[-4])
     if workspace is None:
-        workspace = _workspace(load().dsbd_kv_commit_paged_workspace(C.addressof(f), C.addressof(p), pages.n_pages), dev)
-    if status is None:
-        status = torch.zeros(1, dtype=torch.int32, device=dev)
+        workspace = _workspace(load().dsbd_kv_commit_paged_workspace(C.addressof(f), C.addressof(p), pages.n_pages), dev, stream)
+    status = _status(status, dev, stream)
+    new = lambda n, dtype, make=torch.empty: _made_on(stream, make, int(n), dtype, dev)
     res = out if out is not None else dict(
-        new_req_beam_off=torch.empty(forest.R + 1, dtype=torch.int32, device=dev),
-        new_prefix_off=torch.empty(int(n_slots) + 1, dtype=torch.int64, device=dev),
-        new_page_off=torch.empty(int(n_slots) + 1, dtype=torch.int64, device=dev),
-        new_page_table=torch.full((int(table_capacity),), -1, dtype=torch.int32, device=dev),
-        new_beam_slot=torch.empty(int(n_slots), dtype=torch.int32, device=dev))
+        new_req_beam_off=new(forest.R + 1, torch.int32),
+        new_prefix_off=new(int(n_slots) + 1, torch.int64),
+        new_page_off=new(int(n_slots) + 1, torch.int64),
+        new_page_table=new(table_capacity, torch.int32, _minus_ones),
+        new_beam_slot=new(n_slots, torch.int32))
     res["status"], res["workspace"] = status, workspace
     rc = load().dsbd_kv_commit_paged(
         C.addressof(f), C.addressof(desc), C.addressof(p), _ptr(out_off), _ptr(out_width), _ptr(out_parent),
@@ -599,9 +598,8 @@ def verify_step(forest, params, logits_p, logits_q, root_logp, root_logq, out, w
     p = _params(params, keep)
     o = VerifyOutT(*[_ptr(out[name]) for name in _OUT_FIELDS])
     if workspace is None:
-        workspace = _workspace(load().dsbd_verify_workspace(C.addressof(f), C.addressof(p)), logits_p.device)
-    if status is None:
-        status = torch.zeros(1, dtype=torch.int32, device=logits_p.device)
+        workspace = _workspace(load().dsbd_verify_workspace(C.addressof(f), C.addressof(p)), logits_p.device, stream)
+    status = _status(status, logits_p.device, stream)
     stride = int(row_stride) if row_stride is not None else logits_p.stride(0)
     rc = load().dsbd_verify_step(C.addressof(f), C.addressof(p), _ptr(logits_p), _ptr(logits_q), stride,
                                  _ptr(root_logp), _ptr(root_logq), C.addressof(o), _ptr(workspace),
@@ -619,11 +617,11 @@ def node_stats(forest, params, logits_p, logits_q, lse_p=None, lse_q=None, works
     p = _params(params, keep)
     dev = logits_p.device
     if lse_p is None:
-        lse_p = torch.empty(forest.N, dtype=torch.float32, device=dev)
+        lse_p = _made_on(stream, torch.empty, forest.N, torch.float32, dev)
     if lse_q is None:
-        lse_q = torch.empty(forest.N, dtype=torch.float32, device=dev)
+        lse_q = _made_on(stream, torch.empty, forest.N, torch.float32, dev)
     if workspace is None:
-        workspace = _workspace(load().dsbd_verify_workspace(C.addressof(f), C.addressof(p)), dev)
+        workspace = _workspace(load().dsbd_verify_workspace(C.addressof(f), C.addressof(p)), dev, stream)
     rc = load().dsbd_node_stats(C.addressof(f), C.addressof(p), _ptr(logits_p), _ptr(logits_q),
                                 logits_p.stride(0), _ptr(lse_p), _ptr(lse_q), _ptr(workspace),
                                 workspace.numel(), _stream(stream))
@@ -660,13 +658,13 @@ def select_width(forest, params, logits_p, logits_q, node_logp, node_logq, live_
     f = forest.struct()
     p = _params(params, keep)
     dev = logits_p.device
-    width = torch.zeros(forest.R, dtype=torch.int32, device=dev)
-    alpha = torch.zeros(forest.R, out_stride, dtype=torch.float32, device=dev) if want_alpha else None
-    tail = torch.zeros(forest.R, out_stride, dtype=torch.float32, device=dev) if want_alpha else None
+    zeros = lambda shape, dtype: _made_on(stream, torch.zeros, shape, dtype, dev)
+    width = zeros(forest.R, torch.int32)
+    alpha = zeros((forest.R, out_stride), torch.float32) if want_alpha else None
+    tail = zeros((forest.R, out_stride), torch.float32) if want_alpha else None
     if workspace is None:
-        workspace = _workspace(load().dsbd_verify_workspace(C.addressof(f), C.addressof(p)), dev)
-    if status is None:
-        status = torch.zeros(1, dtype=torch.int32, device=dev)
+        workspace = _workspace(load().dsbd_verify_workspace(C.addressof(f), C.addressof(p)), dev, stream)
+    status = _status(status, dev, stream)
     rc = load().dsbd_select_width(C.addressof(f), C.addressof(p), _ptr(logits_p), _ptr(logits_q),
                                   logits_p.stride(0), _ptr(node_logp), _ptr(node_logq), _ptr(live_off),
                                   _ptr(live_nodes), _ptr(m), _ptr(width), _ptr(alpha), _ptr(tail),
