@@ -338,6 +338,8 @@ def forest_build(req_beam_off, req_beam_off_host, gamma, W_S, draw_parent, draw_
                                   _ptr(largest) if exact else None, _ptr(status), _stream(stream))
     if rc != OK:
         raise DsbdError("dsbd_forest_build", rc)
+    if exact and stream is not None:
+        stream.synchronize()
     f = Forest.from_device(R, B, N, gamma, arrays,
                            max_tree_nodes=int(largest.item()) if exact else 1 + gamma * W_S,
                            max_req_beams=_widest(rbo), max_layer_nodes=W_S)

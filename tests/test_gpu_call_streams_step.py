@@ -66,3 +66,17 @@ def test_everything_is_made_on_the_stream_of_the_call(made, name):
     made.clear()
     call(None)
     assert made and all(s == torch.cuda.current_stream() for s in made)
+
+
+def test_the_largest_tree_is_read_behind_the_build(monkeypatch):
+    """exact=True reads the size of the largest tree back: of the call's own stream, which may be busy."""
+    rbo, parent, token = _t(0, 1), _t(0, 0, 1, 1).view(2, 2), _t(1, 2, 3, 4).view(2, 2)
+    want, _, _ = dsbd.forest_build(rbo, [0, 1], 2, 2, parent, token, exact=True)
+    assert want.max_tree_nodes == 5
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        torch.cuda._sleep(100_000_000)
+    got, _, status = dsbd.forest_build(rbo, [0, 1], 2, 2, parent, token, exact=True, stream=side)
+    torch.cuda.synchronize()
+    assert int(status.item()) == 0 and got.max_tree_nodes == 5
