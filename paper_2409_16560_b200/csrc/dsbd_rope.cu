@@ -79,9 +79,11 @@ constexpr int kTreeWarps = 4, kTreeSmem = 1056;     // dsbd_forest_build makes t
 
 // A warp to a tree: its parents go to shared memory, every lane walks up from its nodes (a dependent chain of
 // shared-memory look-ups instead of one of global loads).  Parents come before their children, so a walk ends.
+// (No __restrict__: the blocks may be resident while the kernel before, dsbd_forest_build's for one, writes the forest, and
+// data that is written meanwhile must not be read by non-coherent loads.)
 __global__ void __launch_bounds__(kTreeWarps * 32)
-k_forest_positions(int B, int N, const int32_t *__restrict__ node_off, const int32_t *__restrict__ parent,
-                   const int64_t *__restrict__ prefix_off, int32_t *__restrict__ position, int32_t *status) {
+k_forest_positions(int B, int N, const int32_t *node_off, const int32_t *parent, const int64_t *prefix_off, int32_t *position,
+                   int32_t *status) {
     __shared__ int par_s[kTreeWarps][kTreeSmem];
     pdl_wait();
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, b = blockIdx.x * kTreeWarps + warp;
