@@ -78,7 +78,8 @@ int frequencies(const dsbd_rope_scaling_t *s, int rot, double *f, double *attent
 constexpr int kTreeWarps = 4, kTreeSmem = 1056;     // dsbd_forest_build makes trees of at most 1025 nodes
 
 // A warp to a tree: its parents go to shared memory, every lane walks up from its nodes (a dependent chain of
-// shared-memory look-ups instead of one of global loads).  Parents come before their children, so a walk ends.
+// shared-memory look-ups instead of one of global loads).  Parents come before their children, so a walk ends.  Walks of large
+// trees would cost their nodes times their depth; those are done 32 nodes at a time behind what is done already.
 // (No __restrict__: the blocks may be resident while the kernel before, dsbd_forest_build's for one, writes the forest, and
 // data that is written meanwhile must not be read by non-coherent loads.)
 __global__ void __launch_bounds__(kTreeWarps * 32)
@@ -96,23 +97,41 @@ k_forest_positions(int B, int N, const int32_t *node_off, const int32_t *parent,
     }
     const int n = hi - lo;
     int *par = par_s[warp];
-    const bool staged = n <= kTreeSmem;
-    if (staged) {
+    if (n <= kTreeSmem) {
         for (int i = lane; i < n; i += 32) par[i] = parent[lo + i] - lo;
         __syncwarp();
-    }
-    for (int i = lane; i < n; i += 32) {
-        int depth = 0;
-        for (int j = i; ;) {
-            const int p = staged ? par[j] : parent[lo + j] - lo;
-            if (p < 0 || p >= j) {
-                if (j == i && (i != 0 || p != -1 - lo)) report(status, DSBD_DEV_BAD_FOREST);
-                break;
+        for (int i = lane; i < n; i += 32) {
+            int depth = 0;
+            for (int j = i; ;) {
+                const int p = par[j];
+                if (p < 0 || p >= j) {
+                    if (j == i && (i != 0 || p != -1 - lo)) report(status, DSBD_DEV_BAD_FOREST);
+                    break;
+                }
+                ++depth;
+                j = p;
             }
-            ++depth;
-            j = p;
+            position[lo + i] = (int)L + depth;
         }
-        position[lo + i] = (int)L + depth;
+        return;
+    }
+    // 32 nodes at a time, whose ancestors among the 32 are found by doubling; an ancestor before them has its position already
+    for (int base = 0; base < n; base += 32) {
+        const int i = base + lane;
+        int up = -1, depth = 0;                      // an ancestor of node i, and how far above it
+        if (i < n) {
+            const int p = parent[lo + i] - lo;
+            if (p >= 0 && p < i) { up = p; depth = 1; }
+            else if (i != 0 || p != -1 - lo) report(status, DSBD_DEV_BAD_FOREST);
+        }
+#pragma unroll
+        for (int r = 0; r < 5; ++r) {
+            const int src = up >= base ? up - base : lane;
+            const int next = __shfl_sync(kFull, up, src), more = __shfl_sync(kFull, depth, src);
+            if (up >= base) { up = next; depth += more; }
+        }
+        if (i < n) position[lo + i] = (up >= 0 ? position[lo + up] : (int)L) + depth;
+        __syncwarp();
     }
 }
 
