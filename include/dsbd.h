@@ -469,7 +469,7 @@ typedef struct {
     double factor;                 /* >= 1 (ignored by PLAIN)                                */
     double original;               /* trained context (WAVELENGTH, RAMP)                     */
     double low, high;              /* 0 < low < high (WAVELENGTH, RAMP)                      */
-    double attention;              /* RAMP: factor on cos and sin, 0 = 0.1 ln(factor) + 1    */
+    double attention;              /* RAMP: factor on cos and sin, >= 0; 0 = 0.1 ln(factor) + 1 */
 } dsbd_rope_scaling_t;
 
 /* The rot / 2 frequencies and the factor on cos and sin; host arrays, host-only.  rot: even, 2 .. 128. */

@@ -46,6 +46,7 @@ int frequencies(const dsbd_rope_scaling_t *s, int rot, double *f, double *attent
     if ((kind == DSBD_ROPE_WAVELENGTH || kind == DSBD_ROPE_RAMP) &&
         !(s->original > 0.0 && s->low > 0.0 && s->high > s->low && std::isfinite(s->original) && std::isfinite(s->high)))
         return DSBD_ERR_INVALID_ARG;
+    if (kind == DSBD_ROPE_RAMP && !(s->attention >= 0.0 && std::isfinite(s->attention))) return DSBD_ERR_INVALID_ARG;
     const double kPi = 3.14159265358979323846;
     const double base = kind == DSBD_ROPE_BASE ? s->base * pow(s->factor, (double)rot / (rot - 2)) : s->base;
     // RAMP: dimension at which `turns` turns fit into the trained context
