@@ -541,8 +541,8 @@ int dsbd_kv_append_paged(const dsbd_chunk_t *chunk, const dsbd_attn_desc_t *desc
  *   out = sum_j softmax_j(scale * q . K_j) V_j  over the positions j = 0 .. L_b + i of its sequence.
  * q, out [total_new, Hq, d] contiguous (out is not q).  One token a sequence or whole prompts, mixed as they come.  Rows
  * of the pools behind a sequence's last token are not used, whatever they hold; values at positions that a row does not
- * see, in the same page as ones that it or a neighbouring row sees, must be finite.  bf16, d 64 or 128, Hq / Hkv <= 128,
- * max_len <= 2^30, n_pages * Hkv * DSBD_PAGE_TOKENS < 2^31 - 256, pointers multiples of 16 bytes; otherwise UNSUPPORTED.  INVALID_ARG for
+ * see, in the same page as ones that it or a neighbouring row sees, must be finite.  A logit that is NaN makes a row that sees it
+ * NaN.  bf16, d 64 or 128, Hq / Hkv <= 128, max_len <= 2^30, n_pages * Hkv * DSBD_PAGE_TOKENS < 2^31 - 256, pointers multiples of 16 bytes; otherwise UNSUPPORTED.  INVALID_ARG for
  * null pointers, out = q and a scale that is not positive and finite.  *status as in dsbd_kv_append_paged, with rows of
  * a sequence that is left out not written and missing pages read as zeros, and DSBD_DEV_TIMEOUT. */
 int dsbd_chunk_attention_paged(const dsbd_chunk_t *chunk, const dsbd_attn_desc_t *desc, const void *q,

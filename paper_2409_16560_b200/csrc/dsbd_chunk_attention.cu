@@ -35,8 +35,8 @@
 //
 // What bounds it: wide units shared memory's bandwidth (96 KB of operands of S, 32 KB of V and 32 KB of copies for 64 tokens of both row
 // tiles, 1545 cycles, where the products alone take 1100) and, in calls of a millisecond, the power limit: 16384 tokens at once, 32 / 8
-// heads of 128, 1.66 ms (1320 TFLOP/s), 1.95 ms (1120) in a loop of seconds, where the clock falls to 1.4 GHz.  Single tokens HBM:
-// 64 behind 1024 to 4096 97 us, 6.0 TB/s.  The shortest calls a chain of latencies: 4 tokens behind 512, heads of 64, 8.8 us.
+// heads of 128, 1.72 ms (1280 TFLOP/s), 2.00 ms (1100) in a loop of seconds, where the clock falls to 1.4 GHz.  Single tokens HBM:
+// 64 behind 1024 to 4096 97 us, 6.0 TB/s.  The shortest calls a chain of latencies: 4 tokens behind 512, heads of 64, 9.0 to 9.5 us.
 //
 // Every mbarrier wait is bounded; on a time-out the kernel records DSBD_DEV_TIMEOUT, lets its copies and products land,
 // frees its TMEM and returns.
@@ -77,7 +77,7 @@ struct Shape {
 // Costs are counted in tokens that a block's rows see, kNarrowShare of them in narrow units: a wide tile takes 1545 cycles, a
 // narrow one half as long where HBM does not hold it up (its row tiles share the tokens) and 1400 where all SMs read their
 // caches at once.  A unit's beginning and end are worth kWideCost and kNarrowCost more.  Batches of chunks and single tokens are
-// up to 12 % faster than with a share of 1 (12 chunks of 1 to 777 tokens behind 0 to 6000: 100.6 us -> 97.1), the rest as fast; 0.5 gains as much
+// up to 12 % faster than with a share of 1 (12 chunks of 1 to 777 tokens behind 0 to 6000: 100.6 us -> 97.1, 99 with the row sum of today), the rest as fast; 0.5 gains as much
 // on those and loses 10 % on many short chunks.
 constexpr int kWideCost = 192, kNarrowCost = 288;
 constexpr double kNarrowShare = 0.75;
