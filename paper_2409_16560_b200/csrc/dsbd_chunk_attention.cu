@@ -77,7 +77,7 @@ struct Shape {
 // Costs are counted in tokens that a block's rows see, kNarrowShare of them in narrow units: a wide tile takes 1545 cycles, a
 // narrow one half as long where HBM does not hold it up (its row tiles share the tokens) and 1400 where all SMs read their
 // caches at once.  A unit's beginning and end are worth kWideCost and kNarrowCost more.  Batches of chunks and single tokens are
-// up to 12 % faster than with a share of 1 (12 chunks of 1 to 777 tokens behind 0 to 6000: 100.6 us -> 97.1, 99 with the row sum of today), the rest as fast; 0.5 gains as much
+// up to 12 % faster than with a share of 1 (12 chunks of 1 to 777 tokens behind 0 to 6000: 100.6 us -> 97.1), the rest as fast; 0.5 gains as much
 // on those and loses 10 % on many short chunks.
 constexpr int kWideCost = 192, kNarrowCost = 288;
 constexpr double kNarrowShare = 0.75;
