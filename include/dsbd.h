@@ -52,8 +52,9 @@ enum {
     DSBD_DEV_TIMEOUT = 5,        /* a bounded wait gave up                                   */
     DSBD_DEV_BAD_PARAM = 6,      /* a per-request width (W_min_r, W_max_r, W_nom_r) below 1, or
                                     W_max_r below W_min_r                                    */
-    DSBD_DEV_BAD_CHUNK = 7       /* a chunk's offset, length, page id or position that contradicts
+    DSBD_DEV_BAD_CHUNK = 7,      /* a chunk's offset, length, page id or position that contradicts
                                     what the call was told; what it names is left out          */
+    DSBD_DEV_BAD_LOGIT = 8       /* a logit that is NaN or +inf; its row has no result           */
 };
 
 /* limits of this build */
@@ -554,6 +555,76 @@ size_t dsbd_chunk_attention_paged_workspace(const dsbd_chunk_t *chunk, const dsb
 
 /* Kernels that a call launches (1, or 2 with the merge of sequences that are cut); 0 for invalid arguments. */
 int dsbd_chunk_attention_paged_launches(const dsbd_chunk_t *chunk, const dsbd_attn_desc_t *desc);
+
+/* ---- Rows of next-token logits beside the decode step ------------------------------------------
+ * (Draws with each row's own settings: the first beams behind a prompt, requests that decode plainly.  The largest logits of the
+ * large model's rows, and the loss that pulls the small model's rows to them: the small model's fit decides how many of its drafts
+ * dsbd_verify_step accepts.) */
+#define DSBD_MAX_ROW_BYTES 1572864 /* V elements: 393216 in fp32, 786432 in bf16               */
+#define DSBD_MAX_TOP 1024          /* K of dsbd_top_logits and dsbd_distill                    */
+
+/* Row r: the V elements from logits + r * row_stride (elements) on, at any alignment of an element; what lies between the rows is
+ * not read.  -inf marks a token that is masked out. */
+typedef struct {
+    const void *logits;
+    int64_t row_stride;            /* >= V where there is more than one row                  */
+    int32_t rows, V;
+    int32_t dtype;                 /* DSBD_DTYPE_F32 or DSBD_DTYPE_BF16                      */
+} dsbd_rows_t;
+
+typedef struct {
+    float temperature;             /* 0: the largest logit's token (the lowest of equal ones) */
+    float top_p;                   /* > 0; from 1 on: off                                    */
+    float min_p;                   /* 0 .. 1; 0: off                                         */
+    int32_t top_k;                 /* <= 0 or >= V: off                                      */
+    /* a row's own, device [rows], or NULL: the number above for all */
+    const float *temperature_r, *top_p_r, *min_p_r;
+    const int32_t *top_k_r;
+    int32_t draws;                 /* of each row                                            */
+} dsbd_sample_params_t;
+
+/* Independent draws from each row.  A token's mass is exp((z - largest z) / temperature); the row keeps, in falling order of logits
+ * (of equal ones the lower token first), the first top_k tokens, of these the shortest prefix that has at least top_p of their mass,
+ * and of these the tokens of at least min_p of the largest one's mass.  Draw j of row r is the first kept token, in the tokens' order,
+ * whose cumulative mass exceeds uniform[r * draws + j] times the whole (a uniform of 1: the last one).  token [rows, draws];
+ * logp [rows, draws] or NULL: the logarithm of its share of the kept mass.  Masses and their sums are in 64 bits.
+ * *status: DSBD_DEV_BAD_LOGIT for a row with a NaN or +inf, DSBD_DEV_EXHAUSTED for a row of nothing but -inf, DSBD_DEV_BAD_PARAM for a
+ * row's own setting or a uniform out of range; the draws concerned are token -1 with logp NaN.
+ * Errors: INVALID_ARG (null pointer, setting, stride), UNSUPPORTED (dtype, a row longer than DSBD_MAX_ROW_BYTES, an element that is
+ * not aligned).  rows = 0 or draws = 0 launches nothing. */
+int dsbd_sample_rows(const dsbd_rows_t *rows, const dsbd_sample_params_t *params, const float *uniform, int32_t *token,
+                     float *logp, int32_t *status, dsbd_stream_t stream);
+
+/* The K largest logits of each row in falling order, of equal ones the lower token first: value [rows, K] fp32, index [rows, K];
+ * rest [rows] or NULL: log of the sum of exp(z / temperature) over the row's other tokens (-inf where there are none, or all of them
+ * are masked).  Where fewer than K tokens are above -inf the first ones at -inf follow.  1 <= K <= min(V, DSBD_MAX_TOP), temperature > 0.
+ * *status: DSBD_DEV_BAD_LOGIT, DSBD_DEV_EXHAUSTED as above; such a row gets index -1, value and rest NaN. */
+int dsbd_top_logits(const dsbd_rows_t *rows, int32_t K, float temperature, float *value, int32_t *index, float *rest,
+                    int32_t *status, dsbd_stream_t stream);
+
+/* Distillation from a teacher's entries, with the gradient.  Teacher of row r: p = softmax over value[r, k] / temperature and, where
+ * rest is given, rest[r] as one more outcome (all other tokens together, as dsbd_top_logits gives it at the same temperature).  Student:
+ * q = softmax(z / temperature) of the row's V logits, on the same outcomes (rest: the sum over the tokens that index does not name).
+ *   loss[r] = temperature^2 * sum_k p_k (log p_k - log q_k)
+ *   grad[r, v] = weight[r] * temperature * (q_v - p_k)               v = index[r, k]
+ *              = weight[r] * temperature * q_v (1 - p_rest / q_rest)   other v (without rest: weight * temperature * q_v)
+ * so grad is the gradient of sum_r weight[r] * loss[r] by the logits, in their dtype.  An entry of index -1 is not there; equal
+ * indices are outcomes that share a token.  weight NULL: 1; a row of weight 0 is not read, its loss and gradient are 0.
+ * value, index [rows, K] contiguous, 1 <= K <= min(V, DSBD_MAX_TOP); loss [rows]; grad NULL: losses alone; grad may be the logits
+ * themselves with the same stride, and overlaps them in no other way.  A NaN or +inf goes through as the formulas say.
+ * *status: DSBD_DEV_BAD_TOKEN for an index outside [-1, V) (left out), DSBD_DEV_EXHAUSTED for a row whose logits, or whose teacher's
+ * entries, are nothing but -inf or not there: its loss and gradient are 0. */
+typedef struct {
+    int32_t K;
+    float temperature;             /* > 0                                                    */
+    const float *value;
+    const int32_t *index;
+    const float *rest;             /* [rows] or NULL                                         */
+    const float *weight;           /* [rows] or NULL                                         */
+} dsbd_distill_params_t;
+
+int dsbd_distill(const dsbd_rows_t *rows, const dsbd_distill_params_t *params, float *loss, void *grad, int64_t grad_stride,
+                 int32_t *status, dsbd_stream_t stream);
 
 const char *dsbd_status_string(int code);
 

@@ -27,7 +27,7 @@ EXPORTS = ["dsbd_forest_attention", "dsbd_forest_attention_workspace", "dsbd_for
            "dsbd_forest_attention_paged", "dsbd_forest_attention_paged_workspace", "dsbd_kv_commit_paged", "dsbd_kv_commit_paged_workspace",
            "dsbd_forest_build", "dsbd_rope_frequencies", "dsbd_rope_table", "dsbd_rotate_qk", "dsbd_forest_positions",
            "dsbd_kv_append_paged", "dsbd_chunk_attention_paged", "dsbd_chunk_attention_paged_workspace",
-           "dsbd_chunk_attention_paged_launches",
+           "dsbd_chunk_attention_paged_launches", "dsbd_sample_rows", "dsbd_top_logits", "dsbd_distill",
            "dsbd_status_string"]
 
 _vp = C.c_void_p
@@ -148,6 +148,12 @@ def _declare(lib):
     lib.dsbd_chunk_attention_paged_workspace.argtypes = [_vp, _vp]
     lib.dsbd_chunk_attention_paged_launches.restype = C.c_int
     lib.dsbd_chunk_attention_paged_launches.argtypes = [_vp, _vp]
+    lib.dsbd_sample_rows.restype = C.c_int
+    lib.dsbd_sample_rows.argtypes = [_vp] * 7
+    lib.dsbd_top_logits.restype = C.c_int
+    lib.dsbd_top_logits.argtypes = [_vp, C.c_int32, C.c_float] + [_vp] * 5
+    lib.dsbd_distill.restype = C.c_int
+    lib.dsbd_distill.argtypes = [_vp] * 4 + [i64, _vp, _vp]
     return lib
 
 
@@ -940,3 +946,131 @@ def chunk_attention_paged(chunk, Hq, Hkv, d, scale, q, k_pool, v_pool, out=None,
     if rc != OK:
         raise DsbdError("dsbd_chunk_attention_paged", rc)
     return out, status
+
+
+# ---------------------------------------------------------------- rows of logits: draws, largest logits, distillation
+MAX_TOP = 1024               # DSBD_MAX_TOP
+
+
+class RowsT(C.Structure):
+    _fields_ = [("logits", _vp), ("row_stride", C.c_int64), ("rows", C.c_int32), ("V", C.c_int32), ("dtype", C.c_int32)]
+
+
+class SampleParamsT(C.Structure):
+    _fields_ = [("temperature", C.c_float), ("top_p", C.c_float), ("min_p", C.c_float), ("top_k", C.c_int32),
+                ("temperature_r", _vp), ("top_p_r", _vp), ("min_p_r", _vp), ("top_k_r", _vp), ("draws", C.c_int32)]
+
+
+class DistillParamsT(C.Structure):
+    _fields_ = [("K", C.c_int32), ("temperature", C.c_float), ("value", _vp), ("index", _vp), ("rest", _vp), ("weight", _vp)]
+
+
+def _rows(logits):
+    """RowsT of a [rows, V] tensor whose rows are contiguous (a view of a padded buffer's columns will do)."""
+    if logits.dim() != 2 or not logits.is_cuda or logits.dtype not in _DTYPES:
+        raise AssertionError("logits are [rows, V] on the device, fp32 or bf16")
+    R, V = logits.shape
+    if V < 1 or (V > 1 and logits.stride(1) != 1):
+        raise AssertionError("a row's logits lie side by side")
+    stride = logits.stride(0) if R > 1 else V
+    return RowsT(logits.data_ptr(), stride, R, V, _DTYPES[logits.dtype])
+
+
+def _given(t, shape, dtype, device, what):
+    """Address of a caller's tensor, after a look at it."""
+    if t.shape != shape or t.dtype != dtype or t.device != device or not t.is_contiguous():
+        raise AssertionError("%s is %s %s, contiguous, on the logits' device" % (what, dtype, list(shape)))
+    return t.data_ptr()
+
+
+def _or_new(t, shape, dtype, device, stream, what):
+    """The caller's output tensor, or a new one."""
+    if t is None:
+        return _made_on(stream, torch.empty, shape, dtype, device)
+    _given(t, torch.Size(shape), dtype, device, what)
+    return t
+
+
+def _row_call(logits, status, stream):
+    """Checks that the call runs on the logits' device; its status word."""
+    if (stream.device if stream is not None else torch.device("cuda", torch.cuda.current_device())) != logits.device:
+        raise AssertionError("the stream is one of the logits' device")
+    status = _status(status, logits.device, stream)
+    if status.device != logits.device:
+        raise AssertionError("the status word is on the logits' device")
+    return status
+
+
+def sample_rows(logits, uniform, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, token=None, logp=None, status=None, stream=None):
+    """dsbd_sample_rows: draws from each row of logits [rows, V] (fp32 or bf16; rows may lie apart) by the numbers uniform
+    [rows, draws] (fp32 in [0, 1]; [rows]: one draw each).  Each setting is a number, or a tensor [rows] (fp32; top_k int32) of the
+    rows' own; temperature 0 takes the largest logit, top_k 0, top_p 1 and min_p 0 are off.
+    Returns (token int32, logp fp32, status) in the shape of `uniform`."""
+    rows = _rows(logits)
+    R, dev = rows.rows, logits.device
+    if uniform.dim() not in (1, 2) or uniform.shape[0] != R:
+        raise AssertionError("uniform is [rows] or [rows, draws]")
+    u = _given(uniform, uniform.shape, torch.float32, dev, "uniform")
+    status = _row_call(logits, status, stream)
+    token = _or_new(token, uniform.shape, torch.int32, dev, stream, "token")
+    logp = _or_new(logp, uniform.shape, torch.float32, dev, stream, "logp")
+    p = SampleParamsT(1.0, 1.0, 0.0, 0, None, None, None, None, uniform.shape[1] if uniform.dim() == 2 else 1)
+    for name, x, dtype in (("temperature", temperature, torch.float32), ("top_p", top_p, torch.float32),
+                           ("min_p", min_p, torch.float32), ("top_k", top_k, torch.int32)):
+        if isinstance(x, torch.Tensor):
+            setattr(p, name + "_r", _given(x, torch.Size((R,)), dtype, dev, name))
+        else:
+            setattr(p, name, x)
+    rc = load().dsbd_sample_rows(C.addressof(rows), C.addressof(p), u, token.data_ptr(), logp.data_ptr(), status.data_ptr(),
+                                 _stream(stream))
+    if rc != OK:
+        raise DsbdError("dsbd_sample_rows", rc)
+    return token, logp, status
+
+
+def top_logits(logits, K, temperature=1.0, value=None, index=None, rest=None, status=None, stream=None):
+    """dsbd_top_logits: the K largest logits of each row of logits [rows, V] in falling order, of equal ones the lower token first, and
+    the log-sum-exp of the row's other logits / temperature.  Returns (value fp32 [rows, K], index int32 [rows, K], rest fp32 [rows], status)."""
+    rows = _rows(logits)
+    R, dev, K = rows.rows, logits.device, int(K)
+    status = _row_call(logits, status, stream)
+    value = _or_new(value, (R, K), torch.float32, dev, stream, "value")
+    index = _or_new(index, (R, K), torch.int32, dev, stream, "index")
+    rest = _or_new(rest, (R,), torch.float32, dev, stream, "rest")
+    rc = load().dsbd_top_logits(C.addressof(rows), K, temperature, value.data_ptr(), index.data_ptr(), rest.data_ptr(),
+                                status.data_ptr(), _stream(stream))
+    if rc != OK:
+        raise DsbdError("dsbd_top_logits", rc)
+    return value, index, rest, status
+
+
+def distill(logits, value, index, rest=None, weight=None, temperature=1.0, loss=None, grad=True, status=None, stream=None):
+    """dsbd_distill: losses of the student's rows logits [rows, V] against a teacher's entries value, index [rows, K] (and rest [rows],
+    the teacher's other tokens together, as top_logits gives them), and the gradient of sum(weight * loss) by the logits.  grad: True for
+    a new tensor, a tensor [rows, V] (rows may lie apart; the logits themselves: in place), or None for the losses alone.  Returns (loss
+    fp32 [rows], grad or None, status); logits.backward(grad) hands the gradient on to what made the logits."""
+    rows = _rows(logits)
+    R, V, dev = rows.rows, rows.V, logits.device
+    if value.dim() != 2 or value.shape[0] != R:
+        raise AssertionError("value is [rows, K]")
+    K = value.shape[1]
+    f32, each = torch.float32, torch.Size((R,))
+    p = DistillParamsT(K, temperature, _given(value, value.shape, f32, dev, "value"), _given(index, value.shape, torch.int32, dev, "index"),
+                       None if rest is None else _given(rest, each, f32, dev, "rest"),
+                       None if weight is None else _given(weight, each, f32, dev, "weight"))
+    status = _row_call(logits, status, stream)
+    loss = _or_new(loss, (R,), f32, dev, stream, "loss")
+    if grad is True:
+        grad = _made_on(stream, torch.empty, (R, V), logits.dtype, dev)
+    elif grad is False:
+        grad = None
+    at, stride = None, 0
+    if grad is not None:
+        g = _rows(grad)
+        if (g.rows, g.V, g.dtype) != (R, V, rows.dtype) or grad.device != dev:
+            raise AssertionError("the gradient has the logits' shape, type and device")
+        at, stride = g.logits, g.row_stride
+    rc = load().dsbd_distill(C.addressof(rows), C.addressof(p), loss.data_ptr(), at, stride, status.data_ptr(), _stream(stream))
+    if rc != OK:
+        raise DsbdError("dsbd_distill", rc)
+    return loss, grad, status

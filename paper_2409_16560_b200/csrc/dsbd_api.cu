@@ -15,6 +15,7 @@ extern "C" const char *dsbd_status_string(int code) {
         case DSBD_DEV_TIMEOUT: return "device: bounded wait gave up";
         case DSBD_DEV_BAD_PARAM: return "device: per-request width out of range";
         case DSBD_DEV_BAD_CHUNK: return "device: chunk offset, page or position out of range";
+        case DSBD_DEV_BAD_LOGIT: return "device: logit that is NaN or +inf";
         default: return "unknown status";
     }
 }

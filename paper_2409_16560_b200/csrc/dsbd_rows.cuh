@@ -1,0 +1,330 @@
+// Rows of logits in the shared memory of a cluster: what the draws, the largest logits and the distillation share.
+#pragma once
+
+#include <cfloat>
+#include <climits>
+
+#include <cooperative_groups.h>
+#include <cuda_bf16.h>
+#include <math_constants.h>
+
+#include "dsbd_common.cuh"
+
+namespace dsbd {
+namespace rows {
+
+namespace cg = cooperative_groups;
+
+constexpr int kThreads = 512;
+constexpr int kWarps = kThreads / 32;
+constexpr int kMaxCtas = 8;                        // the largest portable cluster
+constexpr int kShareBytes = DSBD_MAX_ROW_BYTES / kMaxCtas;       // of a row in one CTA, at most
+
+// ---- elements ------------------------------------------------------------------------------
+template <class T> constexpr int kPer = 16 / (int)sizeof(T);     // elements of a 16-byte word
+
+__device__ __forceinline__ float value_of(float x) { return x; }
+__device__ __forceinline__ float value_of(__nv_bfloat16 x) { return __bfloat162float(x); }
+
+__device__ __forceinline__ void unpack(const float4 &w, float (&x)[4]) { x[0] = w.x; x[1] = w.y; x[2] = w.z; x[3] = w.w; }
+__device__ __forceinline__ void unpack(const float4 &w, float (&x)[8]) {
+    const uint32_t u[4] = {__float_as_uint(w.x), __float_as_uint(w.y), __float_as_uint(w.z), __float_as_uint(w.w)};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        x[2 * i] = __uint_as_float(u[i] << 16);
+        x[2 * i + 1] = __uint_as_float(u[i] & 0xffff0000u);
+    }
+}
+__device__ __forceinline__ float4 pack(const float (&x)[4]) { return make_float4(x[0], x[1], x[2], x[3]); }
+__device__ __forceinline__ float4 pack(const float (&x)[8]) {
+    float4 w;
+    float *o = &w.x;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const __nv_bfloat162 two = __floats2bfloat162_rn(x[2 * i], x[2 * i + 1]);
+        o[i] = __uint_as_float(*reinterpret_cast<const uint32_t *>(&two));
+    }
+    return w;
+}
+
+// Order of floats as order of unsigned numbers, -0 as +0.
+__device__ __forceinline__ uint32_t key_of(float z) {
+    const uint32_t u = __float_as_uint(z + 0.f);
+    return u ^ ((uint32_t)((int32_t)u >> 31) | 0x80000000u);
+}
+__device__ __forceinline__ float of_key(uint32_t k) {
+    return __uint_as_float(k ^ ((uint32_t)((int32_t)~k >> 31) | 0x80000000u));
+}
+constexpr uint32_t kKeyMasked = 0x007fffffu;       // key_of(-inf)
+
+// ---- a row's share of a CTA --------------------------------------------------------------------
+// CTA c of the cluster holds the tokens [first, first + count), token t at position mis + t - first of its shared memory, so that
+// 16-byte words lie in shared memory as they do in the row, whatever the row's alignment; what a first or last word holds besides
+// is -inf.  Shares are multiples of 16 elements, so all of a row's CTAs have the same mis.
+struct Share {
+    int first, count, mis, words;
+};
+
+inline int share_of(int V, int ctas) { return ((V + ctas - 1) / ctas + 15) / 16 * 16; }
+
+template <class T>
+__device__ __forceinline__ Share share(const T *row, int V, int rank, int per) {
+    Share s;
+    s.first = min(rank * per, V);
+    s.count = min(per, V - s.first);
+    s.mis = (int)((reinterpret_cast<uintptr_t>(row) & 15) / sizeof(T));
+    s.words = s.count > 0 ? (s.mis + s.count + kPer<T> - 1) / kPer<T> : 0;
+    return s;
+}
+
+// Word w of the share, from the row: the elements that are the share's, -inf for the others.
+template <class T>
+__device__ __forceinline__ float4 load_word(const T *row, const Share &s, int w) {
+    constexpr int P = kPer<T>;
+    const int at = w * P - s.mis;                  // of its first element in the share
+    const T *p = row + s.first + at;
+    if (at >= 0 && at + P <= s.count) return ld_stream(reinterpret_cast<const float4 *>(p));
+    float x[P];
+#pragma unroll
+    for (int e = 0; e < P; ++e) x[e] = at + e >= 0 && at + e < s.count ? value_of(p[e]) : -CUDART_INF_F;
+    return pack(x);
+}
+
+// The share into shared memory, 8 words a thread in flight, each also to f(elements) of the thread that brought it.
+template <class T, class F>
+__device__ __forceinline__ void load_share(const T *row, const Share &s, float4 *mem, F f) {
+    constexpr int kDeep = 8;
+    for (int w0 = threadIdx.x; w0 < s.words; w0 += kDeep * kThreads) {
+        float4 raw[kDeep];
+#pragma unroll
+        for (int u = 0; u < kDeep; ++u)
+            if (w0 + u * kThreads < s.words) raw[u] = load_word(row, s, w0 + u * kThreads);
+#pragma unroll
+        for (int u = 0; u < kDeep; ++u)
+            if (w0 + u * kThreads < s.words) {
+                mem[w0 + u * kThreads] = raw[u];
+                float x[kPer<T>];
+                unpack(raw[u], x);
+                f(x);
+            }
+    }
+}
+
+// f(token, z) for this thread's elements of the share, in the words that it brought.
+template <class T, class F>
+__device__ __forceinline__ void each(const Share &s, const float4 *mem, F f) {
+#pragma unroll 2
+    for (int w = threadIdx.x; w < s.words; w += kThreads) {
+        float x[kPer<T>];
+        unpack(mem[w], x);
+        const int t = s.first + w * kPer<T> - s.mis;
+#pragma unroll
+        for (int e = 0; e < kPer<T>; ++e) f(t + e, x[e]);
+    }
+}
+
+// ---- over a CTA, over a cluster -----------------------------------------------------------------
+template <class P>
+__device__ __forceinline__ P shuffle_xor(P v, int o) {
+    static_assert(sizeof(P) % 4 == 0, "");
+    uint32_t u[sizeof(P) / 4];
+    memcpy(u, &v, sizeof(P));
+#pragma unroll
+    for (unsigned i = 0; i < sizeof(P) / 4; ++i) u[i] = __shfl_xor_sync(kFull, u[i], o);
+    memcpy(&v, u, sizeof(P));
+    return v;
+}
+
+// All threads' v, joined, to all threads.  The joining order is fixed.  scratch: kWarps entries that nobody uses.
+template <class P, class F>
+__device__ __forceinline__ P over_cta(P v, F join, P *scratch) {
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) v = join(v, shuffle_xor(v, o));
+    __syncthreads();
+    if ((threadIdx.x & 31) == 0) scratch[threadIdx.x / 32] = v;
+    __syncthreads();
+    v = scratch[threadIdx.x & (kWarps - 1)];
+#pragma unroll
+    for (int o = kWarps / 2; o > 0; o >>= 1) v = join(v, shuffle_xor(v, o));
+    return v;
+}
+
+__device__ __forceinline__ float larger(float x, float y) { return fmaxf(x, y); }
+__device__ __forceinline__ double add(double x, double y) { return x + y; }
+
+// Words that the CTAs of a cluster tell one another.  Two sets, in turn: whoever writes a set for the second time has passed
+// the barrier that its readers reached after reading it.
+template <class P>
+struct Told {
+    P of[2][kMaxCtas];
+};
+
+__device__ __forceinline__ void cluster_barrier(int ctas) {
+    if (ctas > 1) cg::this_cluster().sync();
+    else __syncthreads();
+}
+
+// Before a CTA writes to another's shared memory, that one must have begun: arrive early, wait late.
+__device__ __forceinline__ void begun_arrive(int ctas) {
+    if (ctas > 1) cg::this_cluster().barrier_arrive();
+}
+__device__ __forceinline__ void begun_wait(int ctas) {
+    if (ctas > 1) cg::this_cluster().barrier_wait();
+}
+
+// v, the same in all threads of a CTA, to all CTAs; returns the cluster's, by rank.
+template <class P>
+__device__ __forceinline__ const P *tell(const P &v, Told<P> &told, int &turn, int ctas, int rank) {
+    P *mine = told.of[turn & 1];
+    ++turn;
+    if (ctas == 1) {
+        if (threadIdx.x == 0) mine[0] = v;
+    } else if ((int)threadIdx.x < ctas) {
+        *cg::this_cluster().map_shared_rank(mine + rank, threadIdx.x) = v;
+    }
+    cluster_barrier(ctas);
+    return mine;
+}
+
+// ---- exponentials in 32 bits, and in 64 --------------------------------------------------------------
+__device__ __forceinline__ float exp2_fast(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+
+// What a sum of exponentials relative to `from` is worth relative to `to`, the larger one (both may be -inf); scale: log2(e) / T.
+__device__ __forceinline__ double rescale(float from, float to, double scale) {
+    return from == to ? 1.0 : exp2(((double)from - (double)to) * scale);
+}
+
+// 2^(k / 64) from a table of 64, times a Taylor polynomial of 2^f for the rest, |f| <= 1 / 128: the table-driven scheme of P. T. P. Tang,
+// ACM TOMS 15 (1989).  The degree 5 leaves (ln 2 / 128)^6 / 720 = 4e-17 of the value.
+struct Mass {
+    double scale;                                  // log2(e) / T
+    const double *table;                           // 64 entries in shared memory
+
+    static __device__ __forceinline__ void fill(double *table) {
+        if (threadIdx.x < 64) table[threadIdx.x] = exp2((double)threadIdx.x / 64.0);
+    }
+    // exp(d / T), d <= 0; 0 below 2^-1000 and for d = -inf
+    __device__ __forceinline__ double of(double d) const {
+        const double y = d * scale;
+        if (!(y > -1000.0)) return 0.0;
+        const double magic = 6755399441055744.0;   // 1.5 * 2^52: adding it rounds to whole numbers
+        const double t = fma(y, 64.0, magic);
+        const int k = __double2loint(t);
+        const double f = fma(t - magic, -1.0 / 64.0, y) * 0.6931471805599453;
+        double r = 1.0 / 120.0;
+        r = fma(r, f, 1.0 / 24.0);
+        r = fma(r, f, 1.0 / 6.0);
+        r = fma(r, f, 0.5);
+        r = fma(r, f, 1.0);
+        r = fma(r, f, 1.0);
+        r *= table[k & 63];
+        return __hiloint2double(__double2hiint(r) + ((k >> 6) << 20), __double2loint(r));
+    }
+};
+
+// ---- sorting and scanning in a CTA ---------------------------------------------------------------
+// Bitonic sort of n numbers (a power of two), largest first.
+__device__ __forceinline__ void sort_down(uint64_t *list, int n) {
+    for (int size = 2; size <= n; size <<= 1)
+        for (int step = size >> 1; step > 0; step >>= 1) {
+            __syncthreads();
+            for (int i = threadIdx.x; i < n / 2; i += kThreads) {
+                const int a = 2 * i - (i & (step - 1)), b = a + step;
+                const uint64_t x = list[a], y = list[b];
+                if ((x < y) == ((a & size) == 0)) { list[a] = y; list[b] = x; }
+            }
+        }
+    __syncthreads();
+}
+
+template <class P>
+__device__ __forceinline__ P shuffle_up(P v, int o) {
+    uint32_t u[sizeof(P) / 4];
+    memcpy(u, &v, sizeof(P));
+#pragma unroll
+    for (unsigned i = 0; i < sizeof(P) / 4; ++i) u[i] = __shfl_up_sync(kFull, u[i], o);
+    memcpy(&v, u, sizeof(P));
+    return v;
+}
+
+// Sum of the v of the threads before this one; *total: of all.  scratch: kWarps entries.
+template <class P>
+__device__ __forceinline__ P before(P v, P *total, P *scratch) {
+    const int lane = threadIdx.x & 31, warp = threadIdx.x / 32;
+    P up = v;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const P x = shuffle_up(up, o);
+        if (lane >= o) up += x;
+    }
+    __syncthreads();
+    if (lane == 31) scratch[warp] = up;
+    __syncthreads();
+    P base = 0, all = 0;
+#pragma unroll
+    for (int w = 0; w < kWarps; ++w) {
+        const P x = scratch[w];
+        if (w < warp) base += x;
+        all += x;
+    }
+    *total = all;
+    const P excl = shuffle_up(up, 1);
+    return base + (lane ? excl : P(0));
+}
+
+// ---- launches ----------------------------------------------------------------------------------
+inline int check_rows(const dsbd_rows_t *r) {
+    if (!r || r->rows < 0 || r->V <= 0 || (r->rows > 1 && r->row_stride < r->V)) return DSBD_ERR_INVALID_ARG;
+    if (r->dtype != DSBD_DTYPE_F32 && r->dtype != DSBD_DTYPE_BF16) return DSBD_ERR_UNSUPPORTED;
+    const int size = r->dtype == DSBD_DTYPE_F32 ? 4 : 2;
+    if ((reinterpret_cast<uintptr_t>(r->logits) & (size - 1)) || (int64_t)r->V * size > DSBD_MAX_ROW_BYTES) return DSBD_ERR_UNSUPPORTED;
+    return r->rows > INT_MAX / kMaxCtas ? DSBD_ERR_UNSUPPORTED : DSBD_OK;
+}
+
+// CTAs of a row and their shares, in elements.
+struct Plan {
+    int ctas, per, words;
+};
+
+inline Plan plan_for(const dsbd_rows_t *r) {
+    const int size = r->dtype == DSBD_DTYPE_F32 ? 4 : 2;
+    Plan p;
+    p.ctas = 1;
+    while (p.ctas < kMaxCtas && (int64_t)share_of(r->V, p.ctas) * size > 64 * 1024) p.ctas *= 2;
+    while (p.ctas < kMaxCtas && r->rows * (int64_t)p.ctas < 148 && (int64_t)share_of(r->V, p.ctas) * size > 16 * 1024) p.ctas *= 2;
+    p.per = share_of(r->V, p.ctas);
+    p.words = p.per * size / 16 + 1;
+    return p;
+}
+
+template <class Args>
+int launch(void (*kernel)(Args), int rows, const Plan &p, size_t more, const Args &a, dsbd_stream_t stream) {
+    const size_t bytes = (size_t)p.words * 16 + more;
+    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes) != cudaSuccess) {
+        cudaGetLastError();
+        return DSBD_ERR_CUDA;
+    }
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = (unsigned)p.ctas;
+    attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)(rows * p.ctas));
+    cfg.blockDim = dim3(kThreads);
+    cfg.dynamicSmemBytes = bytes;
+    cfg.stream = reinterpret_cast<cudaStream_t>(stream);
+    cfg.attrs = attr;
+    cfg.numAttrs = 2;
+    if (cudaLaunchKernelEx(&cfg, kernel, a) == cudaSuccess) return DSBD_OK;
+    cudaGetLastError();
+    return DSBD_ERR_CUDA;
+}
+
+}  // namespace rows
+}  // namespace dsbd
