@@ -1,25 +1,29 @@
 // Distillation of rows of logits from a teacher's entries, loss and gradient in one pass.
 //
-// A row belongs to a cluster of 1 to 8 CTAs, which brings it into shared memory once (its gradient is written from there), so the
-// call moves what it cannot do without: each logit in, each gradient out.
+// A row belongs to a cluster of 1 to 8 CTAs, each of which reads its share for the sums and again for the gradient, the first part from shared
+// memory, the rest while it is still in the L2.
 //
 // The tokens that the teacher names are marked by bits.  The others' softmax has a reference of its own (their largest logit):
 // beside a named token of nearly all the mass their sum would vanish in 32 bits, and with it the loss's last term.  Terms of the
 // sums are in 32 bits (2^-22 each), a thread's terms are added in 32, everything behind that, the teacher's softmax and the loss
 // are in 64 bits: p log p - p log q cancels when the student is near the teacher.
+#include <algorithm>
+
 #include "dsbd_rows.cuh"
 
 namespace dsbd {
 namespace rows {
 namespace {
 
-constexpr int kMine = DSBD_MAX_TOP / kThreads;     // entries of a thread: k = threadIdx.x + i * kThreads
+constexpr int NT = 256;
+constexpr int kResident = 3;                       // CTAs of an SM
 
 struct DistillArgs {
     const void *logits;
     int64_t stride;
-    int V, K, ctas, per, words;
+    int V, K, ctas, per, held;                     // held: words of a share in shared memory, at most
     float temperature;
+    double inverse;                                // 1 / temperature
     const float *value;
     const int32_t *index;
     const float *rest, *weight;
@@ -36,8 +40,9 @@ struct Sums {
 
 struct Shared {
     Told<Sums> told;
-    double scratch[kWarps];
-    float scratch_f[kWarps];
+    float teacher[NT / 32];
+    float2 most[NT / 32];
+    double others[NT / 32], named[NT / 32], entries[NT / 32], scratch[NT / 32];
     uint32_t named_twice;
 };
 
@@ -48,7 +53,7 @@ __device__ __forceinline__ void put_share(T *row, const Share &s, F f) {
     T *to = row + s.first;
     const int mis = (int)((reinterpret_cast<uintptr_t>(to) & 15) / sizeof(T));
     const int words = s.count > 0 ? (mis + s.count + P - 1) / P : 0;
-    for (int w = threadIdx.x; w < words; w += kThreads) {
+    for (int w = threadIdx.x; w < words; w += NT) {
         const int at = w * P - mis;
         float g[P];
         f(at, g);
@@ -62,21 +67,37 @@ __device__ __forceinline__ void put_share(T *row, const Share &s, F f) {
     }
 }
 
-template <class T>
-__global__ void __launch_bounds__(kThreads) k_distill(DistillArgs a) {
-    constexpr int P = kPer<T>;
+// MINE entries of a thread: k = threadIdx.x + i * NT.
+//
+// 64-bit chains are kept short and off the others' way (a dependent step takes some 40 cycles, a logarithm more than a thousand): the teacher's
+// exponentials run while the first words are on their way, the student's sums are joined by lanes side by side, and logarithms are
+// for the loss alone, which one CTA works out behind its share of the gradient.
+template <class T, int MINE>
+__global__ void __launch_bounds__(NT, kResident) k_distill(DistillArgs a) {
+    constexpr int P = kPer<T>, D = kDeep<T>;
     extern __shared__ float4 mem[];
     __shared__ Shared sh;
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     begun_arrive(a.ctas);
+    const int lane = threadIdx.x & 31, warp = threadIdx.x / 32;
     const int row = blockIdx.x / a.ctas, rank = blockIdx.x - row * a.ctas;
+    uint32_t *named = reinterpret_cast<uint32_t *>(mem + a.held);      // a bit for each element of the share's words
     const T *z_row = static_cast<const T *>(a.logits) + (int64_t)row * a.stride;
     T *g_row = a.grad ? static_cast<T *>(a.grad) + (int64_t)row * a.grad_stride : nullptr;
     const Share s = share<T>(z_row, a.V, rank, a.per);
-    uint32_t *named = reinterpret_cast<uint32_t *>(mem + a.words);     // a bit for each position of the share's words
-    const T *z_mem = reinterpret_cast<const T *>(mem);
     const float weight = a.weight ? a.weight[row] : 1.f;
+    const float *value = a.value + (int64_t)row * a.K;
+    const int32_t *index = a.index + (int64_t)row * a.K;
+    const float rest = a.rest ? a.rest[row] : -CUDART_INF_F;
+    float t[MINE], z[MINE];                        // the teacher's entry; the student's logit, where this CTA needs it
+    int at[MINE];                                  // token; -1: no entry
+#pragma unroll
+    for (int i = 0; i < MINE; ++i) {
+        const int k = threadIdx.x + i * NT;
+        at[i] = k < a.K ? index[k] : -1;
+        t[i] = k < a.K ? value[k] : -CUDART_INF_F;
+    }
     auto no_gradient = [&] {
         if (g_row) put_share<T>(g_row, s, [](int, float (&g)[P]) {
 #pragma unroll
@@ -89,113 +110,140 @@ __global__ void __launch_bounds__(kThreads) k_distill(DistillArgs a) {
         begun_wait(a.ctas);
         return;
     }
-    // ---- the teacher's entries and the share
-    const float *value = a.value + (int64_t)row * a.K;
-    const int32_t *index = a.index + (int64_t)row * a.K;
-    const float rest = a.rest ? a.rest[row] : -CUDART_INF_F;
-    float t[kMine];
-    int at[kMine];                                 // token; -1: no entry
-    float z[kMine];                                // the student's logit, where this CTA needs it
-    bool here[kMine];                              // its token is in the share
-#pragma unroll
-    for (int i = 0; i < kMine; ++i) {
-        const int k = threadIdx.x + i * kThreads;
-        at[i] = k < a.K ? index[k] : -1;
-        t[i] = k < a.K ? value[k] : -CUDART_INF_F;
-    }
+    float4 raw[D];
+    load_batch<T, NT>(raw, z_row, s, 0);
+    // ---- the teacher's entries
     if (threadIdx.x == 0) sh.named_twice = 0;
-    for (int w = threadIdx.x; w <= s.words * P / 32; w += kThreads) named[w] = 0;
+    for (int w = threadIdx.x; w < (s.words + D * NT - 1) / (D * NT) * NT; w += NT) named[w] = 0;
+    float mine = -CUDART_INF_F;
 #pragma unroll
-    for (int i = 0; i < kMine; ++i) {
+    for (int i = 0; i < MINE; ++i) {
         if (at[i] < -1 || at[i] >= a.V) {
             if (rank == 0) report(a.status, DSBD_DEV_BAD_TOKEN);
             at[i] = -1;
         }
         if (at[i] < 0) t[i] = -CUDART_INF_F;
-        here[i] = at[i] >= s.first && at[i] < s.first + s.count;
-        z[i] = rank == 0 && at[i] >= 0 ? value_of(z_row[at[i]]) : 0.f;
+        mine = fmaxf(mine, t[i]);
     }
-    load_share<T>(z_row, s, mem, [](const float (&)[P]) {});
+    auto here = [&](int token) { return token >= s.first && token < s.first + s.count; };
+#pragma unroll
+    for (int i = 0; i < MINE; ++i) z[i] = here(at[i]) || (rank == 0 && at[i] >= 0) ? value_of(z_row[at[i]]) : -CUDART_INF_F;
+    mine = warp_most(mine);
+    if (lane == 0) sh.teacher[warp] = mine;
     __syncthreads();
 #pragma unroll
-    for (int i = 0; i < kMine; ++i)
-        if (here[i]) {
+    for (int i = 0; i < MINE; ++i)
+        if (here(at[i])) {
             const int pos = s.mis + at[i] - s.first;
             const uint32_t bit = 1u << (pos & 31);
             if (atomicOr(&named[pos >> 5], bit) & bit) sh.named_twice = 1;
-            z[i] = value_of(z_mem[pos]);
         }
+    double top_t = (double)rest;
+#pragma unroll
+    for (int w = 0; w < NT / 32; ++w) mine = fmaxf(mine, sh.teacher[w]);
+    top_t = fmax(top_t, (double)mine * a.inverse);
     __syncthreads();
+    // the teacher's masses relative to its largest one
+    double e[MINE];
+#pragma unroll
+    for (int i = 0; i < MINE; ++i) e[i] = t[i] != -CUDART_INF_F ? exp((double)t[i] * a.inverse - top_t) : 0.0;
+    const double e_rest = rest != -CUDART_INF_F ? exp((double)rest - top_t) : 0.0;
     // an entry whose token an earlier one has already named: the first one stands for all of them
-    bool stands[kMine];
-#pragma unroll
-    for (int i = 0; i < kMine; ++i) stands[i] = here[i];
+    bool stands[MINE];
     const bool twice = sh.named_twice != 0;
-    if (twice)
-        for (int i = 0; i < kMine; ++i)
-            for (int k = 0; here[i] && k < threadIdx.x + i * kThreads; ++k)
-                if (index[k] == at[i]) stands[i] = false;
+#pragma unroll
+    for (int i = 0; i < MINE; ++i) {
+        stands[i] = here(at[i]);
+        if (twice)
+            for (int k = 0; stands[i] && k < (int)threadIdx.x + i * NT; ++k) stands[i] = index[k] != at[i];
+    }
     // ---- the student's sums
-    const double scale = 1.4426950408889634 / (double)a.temperature;
+    const double scale = 1.4426950408889634 * a.inverse;
     const float scale_f = (float)scale;
-    auto words = [&](auto f) {
-#pragma unroll 2
-        for (int w = threadIdx.x; w < s.words; w += kThreads) {
+    Rest others;
+    for (int w0 = 0; w0 < s.words;) {
+        // the warp's 1024 elements of the batch have 32 words of marks
+        const bool some = __any_sync(kFull, named[w0 * P / 32 + threadIdx.x] != 0);
+        float top = -CUDART_INF_F;
+#pragma unroll
+        for (int u = 0; u < D; ++u) {
+            const int w = batch_word<D>(w0, u);
+            if (w < a.held) mem[w] = raw[u];
             float x[P];
-            unpack(mem[w], x);
-            f(x, named[w * P >> 5] >> (w * P & 31));
+            unpack(raw[u], x);
+            if (some) {
+                const uint32_t marks = named[w * P >> 5] >> (w * P & 31) & ((1u << P) - 1);
+                if (marks) {
+#pragma unroll
+                    for (int i = 0; i < P; ++i) x[i] = marks >> i & 1 ? -CUDART_INF_F : x[i];
+                    raw[u] = pack(x);
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < P; ++i) top = fmaxf(top, x[i]);
         }
-    };
-    float mine = -CUDART_INF_F, sum = 0.f;
-    words([&](const float (&x)[P], uint32_t marks) {
+        others.add_words<T>(raw, top, scale_f);
+        if ((w0 += D * NT) < s.words) load_batch<T, NT>(raw, z_row, s, w0);
+    }
+    float2 most = {others.high, -CUDART_INF_F};
 #pragma unroll
-        for (int e = 0; e < P; ++e) mine = fmaxf(mine, marks >> e & 1 ? -CUDART_INF_F : x[e]);
-    });
-    const float from = mine == -CUDART_INF_F ? 0.f : mine;
-    words([&](const float (&x)[P], uint32_t marks) {
+    for (int i = 0; i < MINE; ++i)
+        if (stands[i]) most.y = fmaxf(most.y, z[i]);
+    const bool entries = warp * 32 < a.K;          // the warp has some
+    most = {warp_most(most.x), entries ? warp_most(most.y) : -CUDART_INF_F};
+    if (lane == 0) sh.most[warp] = most;
+    __syncthreads();
 #pragma unroll
-        for (int e = 0; e < P; ++e) sum += exp2_fast(((marks >> e & 1 ? -CUDART_INF_F : x[e]) - from) * scale_f);
-    });
-    Sums own;
-    own.top_others = over_cta(mine, larger, sh.scratch_f);
-    own.others = over_cta((double)sum * rescale(mine, own.top_others, scale), add, sh.scratch);
-    mine = -CUDART_INF_F;
+    for (int w = 0; w < NT / 32; ++w) most = {fmaxf(most.x, sh.most[w].x), fmaxf(most.y, sh.most[w].y)};
+    const double sum_others = warp_total(others.high == most.x ? others.sum : others.sum * exp2_fast((others.high - most.x) * scale_f));
+    double sum_named = 0.0, sum_entries = 0.0;
+    if (entries) {
+        float n = 0.f;
 #pragma unroll
-    for (int i = 0; i < kMine; ++i)
-        if (stands[i]) mine = fmaxf(mine, z[i]);
-    own.top_named = over_cta(mine, larger, sh.scratch_f);
-    double part = 0.0;
+        for (int i = 0; i < MINE; ++i) {
+            if (stands[i] && z[i] != -CUDART_INF_F) n += exp2_fast((z[i] - most.y) * scale_f);
+            sum_entries += e[i];
+        }
+        sum_named = warp_total(n);
+        sum_entries = warp_total(sum_entries);
+    }
+    if (lane == 0) {
+        sh.others[warp] = sum_others;
+        sh.named[warp] = sum_named;
+        sh.entries[warp] = sum_entries;
+    }
+    __syncthreads();
+    Sums own = {0.0, 0.0, most.x, most.y};
+    double teacher = e_rest;
 #pragma unroll
-    for (int i = 0; i < kMine; ++i)
-        if (stands[i] && z[i] != -CUDART_INF_F) part += rescale(z[i], own.top_named, scale);
-    own.named = over_cta(part, add, sh.scratch);
-    // ---- the teacher's softmax (in every CTA)
-    const double T_ = (double)a.temperature;
-    mine = -CUDART_INF_F;
-#pragma unroll
-    for (int i = 0; i < kMine; ++i) mine = fmaxf(mine, t[i]);
-    const double top_t = fmax((double)over_cta(mine, larger, sh.scratch_f) / T_, (double)rest);
-    part = threadIdx.x == 0 && rest != -CUDART_INF_F ? exp((double)rest - top_t) : 0.0;
-#pragma unroll
-    for (int i = 0; i < kMine; ++i)
-        if (t[i] != -CUDART_INF_F) part += exp((double)t[i] / T_ - top_t);
-    const double log_t = top_t + log(over_cta(part, add, sh.scratch));
+    for (int w = 0; w < NT / 32; ++w) {
+        own.others += sh.others[w];
+        own.named += sh.named[w];
+        teacher += sh.entries[w];
+    }
     begun_wait(a.ctas);
     int turn = 0;
     const Sums *all = tell(own, sh.told, turn, a.ctas, rank);
-    float top_others = -CUDART_INF_F, top = -CUDART_INF_F;
-    for (int c = 0; c < a.ctas; ++c) {
-        top_others = fmaxf(top_others, all[c].top_others);
-        top = fmaxf(top, all[c].top_named);
-    }
-    top = fmaxf(top, top_others);
-    double others = 0.0, whole = 0.0;
-    for (int c = 0; c < a.ctas; ++c) {
-        others += all[c].others * rescale(all[c].top_others, top_others, scale);
-        whole += all[c].named * rescale(all[c].top_named, top, scale);
-    }
-    whole += others * rescale(top_others, top, scale);
-    if (whole == 0.0 || log_t == -CUDART_INF) {
+    // the others' sum relative to their largest logit, base; of all relative to the row's
+    float base = all[0].top_others, top = all[0].top_named;
+#pragma unroll
+    for (int c = 1; c < kMaxCtas; ++c)
+        if (c < a.ctas) {
+            base = fmaxf(base, all[c].top_others);
+            top = fmaxf(top, all[c].top_named);
+        }
+    top = fmaxf(top, base);
+    auto worth = [&](float from, float to) { return from == to ? 1.0 : (double)exp2_fast((from - to) * scale_f); };
+    double rest_sum = 0.0, whole = 0.0;
+#pragma unroll
+    for (int c = 0; c < kMaxCtas; ++c)
+        if (c < a.ctas) {
+            rest_sum += all[c].others * worth(all[c].top_others, base);
+            whole += all[c].named * worth(all[c].top_named, top);
+        }
+    const double others_top = rest_sum * worth(base, top);
+    whole += others_top;
+    if (whole == 0.0 || teacher == 0.0) {
         no_gradient();
         if (rank == 0 && threadIdx.x == 0) {
             a.loss[row] = 0.f;
@@ -203,50 +251,104 @@ __global__ void __launch_bounds__(kThreads) k_distill(DistillArgs a) {
         }
         return;
     }
-    const double log_q = (double)top / T_ + log(whole);                 // of the student's sum
-    const double log_others = (double)top_others / T_ + log(others) - log_q;
-    const double p_rest = rest != -CUDART_INF_F ? exp((double)rest - log_t) : 0.0;
-    // ---- the loss
-    if (rank == 0) {
-        part = threadIdx.x == 0 && p_rest != 0.0 ? p_rest * ((double)rest - log_t - log_others) : 0.0;
-#pragma unroll
-        for (int i = 0; i < kMine; ++i)
-            if (t[i] != -CUDART_INF_F) {
-                const double log_p = (double)t[i] / T_ - log_t, p = exp(log_p);
-                if (p != 0.0) part += p * (log_p - ((double)z[i] / T_ - log_q));
-            }
-        part = over_cta(part, add, sh.scratch);
-        if (threadIdx.x == 0) a.loss[row] = (float)(T_ * T_ * part);
-    }
-    if (!g_row) return;
+    const double per_whole = inverse_of(whole), per_teacher = inverse_of(teacher);
     // ---- the gradient: the others', then the named tokens' over it
-    const double unit = (double)weight * T_;
-    double factor = 0.0;
-    if (others != 0.0) factor = unit * (a.rest ? (exp(log_others) - p_rest) / others : rescale(top_others, top, scale) / whole);
-    const float factor_f = (float)factor;
-    const float base = top_others == -CUDART_INF_F ? 0.f : top_others;
-    const bool along = ((reinterpret_cast<uintptr_t>(g_row + s.first) ^ reinterpret_cast<uintptr_t>(z_row + s.first)) & 15) == 0;
-    put_share<T>(g_row, s, [&](int first, float (&g)[P]) {
-        float x[P];
-        if (along) {
-            unpack(mem[(first + s.mis) / P], x);
+    if (g_row) {
+        const double q = others_top * per_whole;
+        const float factor_f = rest_sum != 0.0 ? (float)((double)weight * a.temperature * (a.rest ? q - e_rest * per_teacher : q) * inverse_of(rest_sum)) : 0.f;
+        if (base == -CUDART_INF_F) base = 0.f;
+        const float2 base2 = {-base, -base}, scale2 = {scale_f, scale_f}, factor2 = {factor_f, factor_f};
+        auto slope = [&](float (&x)[P]) {
+#pragma unroll
+            for (int i = 0; i < P; i += 2) {
+                const float2 y = mul2(add2({x[i], x[i + 1]}, base2), scale2), g = mul2({exp2_fast(y.x), exp2_fast(y.y)}, factor2);
+                x[i] = g.x;
+                x[i + 1] = g.y;
+            }
+        };
+        if (((reinterpret_cast<uintptr_t>(g_row) ^ reinterpret_cast<uintptr_t>(z_row)) & 15) == 0) {
+            // words of the gradient lie as the logits' do
+            float4 *to = reinterpret_cast<float4 *>(g_row + s.first - s.mis);
+            for (int w0 = 0; w0 < s.words; w0 += D * NT) {
+                if (w0 + D * NT <= a.held) {
+#pragma unroll
+                    for (int u = 0; u < D; ++u) raw[u] = mem[batch_word<D>(w0, u)];
+                } else {
+                    load_batch<T, NT>(raw, z_row, s, w0);
+                }
+#pragma unroll
+                for (int u = 0; u < D; ++u) {
+                    const int w = batch_word<D>(w0, u), first = w * P - s.mis;
+                    float x[P];
+                    unpack(raw[u], x);
+                    slope(x);
+                    if (first >= 0 && first + P <= s.count) {
+                        __stcs(to + w, pack(x));
+                    } else {
+#pragma unroll
+                        for (int i = 0; i < P; ++i)
+                            if (first + i >= 0 && first + i < s.count) g_row[s.first + first + i] = T(x[i]);
+                    }
+                }
+            }
         } else {
+            put_share<T>(g_row, s, [&](int first, float (&x)[P]) {
 #pragma unroll
-            for (int e = 0; e < P; ++e) x[e] = first + e >= 0 && first + e < s.count ? value_of(z_mem[s.mis + first + e]) : 0.f;
+                for (int i = 0; i < P; ++i)
+                    x[i] = first + i >= 0 && first + i < s.count ? value_of(z_row[s.first + first + i]) : -CUDART_INF_F;
+                slope(x);
+            });
         }
+        __syncthreads();
 #pragma unroll
-        for (int e = 0; e < P; ++e) g[e] = factor_f * exp2_fast((x[e] - base) * scale_f);
-    });
+        for (int i = 0; i < MINE; ++i)
+            if (stands[i]) {
+                double p = e[i];
+                if (twice)
+                    for (int k = threadIdx.x + i * NT + 1; k < a.K; ++k)
+                        if (index[k] == at[i]) p += exp((double)value[k] * a.inverse - top_t);
+                const double q = (double)exp2_fast((z[i] - top) * scale_f) * per_whole;
+                g_row[at[i]] = T((float)((double)weight * a.temperature * (q - p * per_teacher)));
+            }
+    }
+    // ---- the loss: sum p (log p - log q), log p = t / T - log of the teacher's sum, log q = z / T - log of the student's
+    if (rank) return;
+    double sum = 0.0;
+#pragma unroll
+    for (int i = 0; i < MINE; ++i)
+        if (e[i] != 0.0) sum += e[i] * (((double)t[i] - (double)z[i]) * a.inverse);
+    if (entries) sum = warp_sum(sum);
+    if (lane == 0) sh.scratch[warp] = sum;
     __syncthreads();
-#pragma unroll
-    for (int i = 0; i < kMine; ++i)
-        if (stands[i]) {
-            double p = t[i] != -CUDART_INF_F ? exp((double)t[i] / T_ - log_t) : 0.0;
-            if (twice)
-                for (int k = threadIdx.x + i * kThreads + 1; k < a.K; ++k)
-                    if (index[k] == at[i]) p += exp((double)value[k] / T_ - log_t);
-            g_row[at[i]] = T((float)(unit * (exp((double)z[i] / T_ - log_q) - p)));
-        }
+    if (warp) return;
+    sum = 0.0;
+    for (int w = 0; w < NT / 32; ++w) sum += sh.scratch[w];
+    const double v = log(lane == 0 ? whole : lane == 1 ? teacher : rest_sum);
+    const double log_t = __shfl_sync(kFull, v, 1) + top_t, log_q = __shfl_sync(kFull, v, 0) + (double)top * a.inverse;
+    const double log_others = __shfl_sync(kFull, v, 2) + (double)base * a.inverse - log_q;
+    sum += (teacher - e_rest) * (log_q - log_t);
+    if (e_rest != 0.0) sum += e_rest * ((double)rest - log_t - log_others);
+    if (lane == 0) a.loss[row] = (float)((double)a.temperature * a.temperature * (sum * per_teacher));
+}
+
+template <class T>
+int run_distill(const DistillArgs &a, int rows, const Plan &plan, size_t bytes, dsbd_stream_t stream) {
+    return a.K <= NT ? launch<NT>(k_distill<T, 1>, rows, plan, bytes, a, stream)
+                     : launch<NT>(k_distill<T, DSBD_MAX_TOP / NT>, rows, plan, bytes, a, stream);
+}
+
+// CTAs of a row: shares of up to 128 KB (a CTA's fixed chain, some 12000 cycles, counts for less than with smaller ones; with larger
+// ones the rows under way outgrow the L2, from which what is not held is read again), and more where the SMs would stand idle.
+inline Plan plan_distill(const dsbd_rows_t *r) {
+    const int size = r->dtype == DSBD_DTYPE_F32 ? 4 : 2;
+    Plan p;
+    p.ctas = 1;
+    while (p.ctas < kMaxCtas && (share_of(r->V, p.ctas) * size > 128 * 1024 ||
+           (r->rows * 2 * (int64_t)p.ctas <= 148 * kResident && share_of(r->V, 2 * p.ctas) >= NT * 16)))
+        p.ctas *= 2;
+    p.per = share_of(r->V, p.ctas);
+    p.words = 0;
+    return p;
 }
 
 }  // namespace
@@ -265,13 +367,16 @@ extern "C" int dsbd_distill(const dsbd_rows_t *rows, const dsbd_distill_params_t
     if (p->K > DSBD_MAX_TOP || (reinterpret_cast<uintptr_t>(grad) & (size - 1))) return DSBD_ERR_UNSUPPORTED;
     if (rows->rows == 0) return DSBD_OK;
     if (!rows->logits || !p->value || !p->index || !loss) return DSBD_ERR_INVALID_ARG;
-    const Plan plan = plan_for(rows);
+    const Plan plan = plan_distill(rows);
     DistillArgs a = {};
     a.logits = rows->logits; a.stride = rows->row_stride; a.V = rows->V; a.K = p->K;
-    a.ctas = plan.ctas; a.per = plan.per; a.words = plan.words; a.temperature = p->temperature;
+    a.ctas = plan.ctas; a.per = plan.per; a.temperature = p->temperature;
     a.value = p->value; a.index = p->index; a.rest = p->rest; a.weight = p->weight;
     a.loss = loss; a.grad = grad; a.grad_stride = grad_stride; a.status = status;
-    const size_t marks = ((size_t)plan.words * 16 / size / 32 + 1) * 4;
-    return size == 4 ? launch(k_distill<float>, rows->rows, plan, marks, a, stream)
-                     : launch(k_distill<__nv_bfloat16>, rows->rows, plan, marks, a, stream);
+    // whole batches of 32 elements a thread; without a gradient nothing is read twice
+    const int batch = NT * 32 * size / 16, words = plan.per * size / 16 + 1, batches = (words + batch - 1) / batch;
+    a.held = grad ? std::min(batches * batch, 48 * 1024 / 16 / batch * batch) : 0;
+    const size_t bytes = (size_t)a.held * 16 + (size_t)batches * NT * 4;
+    a.inverse = 1.0 / (double)p->temperature;
+    return size == 4 ? run_distill<float>(a, rows->rows, plan, bytes, stream) : run_distill<__nv_bfloat16>(a, rows->rows, plan, bytes, stream);
 }

@@ -90,6 +90,41 @@ __device__ __forceinline__ float4 load_word(const T *row, const Share &s, int w)
     return pack(x);
 }
 
+template <class T>
+__device__ __forceinline__ float4 masked_word() {
+    float x[kPer<T>];
+#pragma unroll
+    for (int e = 0; e < kPer<T>; ++e) x[e] = -CUDART_INF_F;
+    return pack(x);
+}
+
+// 16-byte words of a thread in a batch: 32 elements.
+template <class T> constexpr int kDeep = 32 / kPer<T>;
+// Word u of this thread in the batch from word w0 on: a warp's words of a batch lie side by side.
+template <int D>
+__device__ __forceinline__ int batch_word(int w0, int u) {
+    return w0 + (threadIdx.x / 32 * D + u) * 32 + (threadIdx.x & 31);
+}
+
+template <class T, int NT>
+__device__ __forceinline__ void load_batch(float4 (&raw)[kDeep<T>], const T *row, const Share &s, int w0) {
+    constexpr int D = kDeep<T>;
+    if (w0 > 0 && w0 + D * NT < s.words) {
+        const float4 *p = reinterpret_cast<const float4 *>(row + s.first - s.mis) + batch_word<D>(w0, 0);
+#pragma unroll
+        for (int u = 0; u < D; ++u) raw[u] = ld_stream(p + u * 32);
+    } else {
+#pragma unroll
+        for (int u = 0; u < D; ++u) raw[u] = batch_word<D>(w0, u) < s.words ? load_word(row, s, batch_word<D>(w0, u)) : masked_word<T>();
+    }
+}
+
+// A whole word into shared memory, later.
+__device__ __forceinline__ void copy_async(float4 *to, const float4 *from) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"((uint32_t)__cvta_generic_to_shared(to)), "l"(from) : "memory");
+}
+__device__ __forceinline__ void copies_here() { asm volatile("cp.async.wait_all;" ::: "memory"); }
+
 // The share into shared memory, 8 words a thread in flight, each also to f(elements) of the thread that brought it.
 template <class T, class F>
 __device__ __forceinline__ void load_share(const T *row, const Share &s, float4 *mem, F f) {
@@ -136,21 +171,52 @@ __device__ __forceinline__ P shuffle_xor(P v, int o) {
 }
 
 // All threads' v, joined, to all threads.  The joining order is fixed.  scratch: kWarps entries that nobody uses.
-template <class P, class F>
+template <int NT = kThreads, class P, class F>
 __device__ __forceinline__ P over_cta(P v, F join, P *scratch) {
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) v = join(v, shuffle_xor(v, o));
     __syncthreads();
     if ((threadIdx.x & 31) == 0) scratch[threadIdx.x / 32] = v;
     __syncthreads();
-    v = scratch[threadIdx.x & (kWarps - 1)];
+    v = scratch[threadIdx.x & (NT / 32 - 1)];
 #pragma unroll
-    for (int o = kWarps / 2; o > 0; o >>= 1) v = join(v, shuffle_xor(v, o));
+    for (int o = NT / 64; o > 0; o >>= 1) v = join(v, shuffle_xor(v, o));
     return v;
+}
+
+// A place behind *n in shared memory.  (atomicAdd of a constant becomes a vote of the warp's active lanes and a leader's addition, three times the
+// instructions where one lane comes, as nearly always here.)
+__device__ __forceinline__ uint32_t next_place(uint32_t *n) {
+    uint32_t was;
+    asm volatile("atom.shared.add.u32 %0, [%1], 1;" : "=r"(was) : "r"((uint32_t)__cvta_generic_to_shared(n)) : "memory");
+    return was;
 }
 
 __device__ __forceinline__ float larger(float x, float y) { return fmaxf(x, y); }
 __device__ __forceinline__ double add(double x, double y) { return x + y; }
+
+// Over a warp without shuffles, which wait in one queue with the loads and stores of all of an SM's warps: 250 cycles each beside CTAs that
+// stream.  Largest of numbers that are not NaN:
+__device__ __forceinline__ float warp_most(float x) { return of_key(__reduce_max_sync(kFull, key_of(x))); }
+
+// Sum of numbers in [0, 512), in steps of 2^-39 (so in no order); NaN if one is.
+__device__ __forceinline__ double warp_total(float x) {
+    const uint32_t high = (uint32_t)(x * 0x1p15f), low = (uint32_t)(fmaf((float)high, -0x1p-15f, x) * 0x1p39f);
+    const double sum = (double)__reduce_add_sync(kFull, high) * 0x1p-15 + (double)__reduce_add_sync(kFull, low) * 0x1p-39;
+    return __any_sync(kFull, x != x) ? (double)CUDART_NAN_F : sum;
+}
+// The same of [0, 16), in steps of 2^-44.
+__device__ __forceinline__ double warp_total(double x) {
+    const uint32_t high = (uint32_t)(x * 0x1p20), low = (uint32_t)(fma((double)high, -0x1p-20, x) * 0x1p44);
+    const double sum = (double)__reduce_add_sync(kFull, high) * 0x1p-20 + (double)__reduce_add_sync(kFull, low) * 0x1p-44;
+    return __any_sync(kFull, x != x) ? (double)CUDART_NAN_F : sum;
+}
+
+// 1 / x by a step of Newton's from the reciprocal in 32 bits: 2^-46 off.
+__device__ __forceinline__ double inverse_of(double x) {
+    const double r = (double)__frcp_rn((float)x);
+    return r * fma(-x, r, 2.0);
+}
 
 // Words that the CTAs of a cluster tell one another.  Two sets, in turn: whoever writes a set for the second time has passed
 // the barrier that its readers reached after reading it.
@@ -193,33 +259,116 @@ __device__ __forceinline__ float exp2_fast(float x) {
     return y;
 }
 
+__device__ __forceinline__ float max_nan(float x, float y) {
+    float z;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(z) : "f"(x), "f"(y));
+    return z;
+}
+
+// Two numbers in one instruction.
+__device__ __forceinline__ float2 add2(float2 x, float2 y) {
+    float2 z;
+    asm("{.reg .b64 a, b, d;\n\tmov.b64 a, {%2, %3};\n\tmov.b64 b, {%4, %5};\n\tadd.rn.f32x2 d, a, b;\n\tmov.b64 {%0, %1}, d;\n\t}"
+        : "=f"(z.x), "=f"(z.y) : "f"(x.x), "f"(x.y), "f"(y.x), "f"(y.y));
+    return z;
+}
+__device__ __forceinline__ float2 mul2(float2 x, float2 y) {
+    float2 z;
+    asm("{.reg .b64 a, b, d;\n\tmov.b64 a, {%2, %3};\n\tmov.b64 b, {%4, %5};\n\tmul.rn.f32x2 d, a, b;\n\tmov.b64 {%0, %1}, d;\n\t}"
+        : "=f"(z.x), "=f"(z.y) : "f"(x.x), "f"(x.y), "f"(y.x), "f"(y.y));
+    return z;
+}
+// 2^((x - top) scale) of two.
+__device__ __forceinline__ float2 exp2_two(float x, float y, float top, float scale) {
+    const float2 a = mul2(add2({x, y}, {-top, -top}), {scale, scale});
+    return {exp2_fast(a.x), exp2_fast(a.y)};
+}
+
 // What a sum of exponentials relative to `from` is worth relative to `to`, the larger one (both may be -inf); scale: log2(e) / T.
 __device__ __forceinline__ double rescale(float from, float to, double scale) {
     return from == to ? 1.0 : exp2(((double)from - (double)to) * scale);
 }
 
-// 2^(k / 64) from a table of 64, times a Taylor polynomial of 2^f for the rest, |f| <= 1 / 128: the table-driven scheme of P. T. P. Tang,
-// ACM TOMS 15 (1989).  The degree 5 leaves (ln 2 / 128)^6 / 720 = 4e-17 of the value.
+// A sum of exponentials relative to the largest logit in it.
+struct Sum {
+    float high;
+    double sum;
+    __device__ __forceinline__ void add(const Sum &o, double scale) {
+        const float top = fmaxf(high, o.high);
+        sum = sum * rescale(high, top, scale) + o.sum * rescale(o.high, top, scale);
+        high = top;
+    }
+};
+
+// A sum of exponentials as one thread has it, relative to the largest logit in it.
+struct Rest {
+    float high = -INFINITY, sum = 0.f;
+    __device__ __forceinline__ void raise(float to, float scale) {
+        if (to > high) {
+            sum *= exp2_fast((high - to) * scale);
+            high = to;
+        }
+    }
+    __device__ __forceinline__ void add(float z, float scale) {
+        raise(z, scale);
+        sum += z == -CUDART_INF_F ? 0.f : exp2_fast((z - high) * scale);
+    }
+    // a batch of words of which top is the largest element
+    template <class T>
+    __device__ __forceinline__ void add_words(const float4 (&raw)[kDeep<T>], float top, float scale) {
+        raise(top, scale);
+        const float from = high == -CUDART_INF_F ? 0.f : high;
+        float2 s[2] = {{0.f, 0.f}, {0.f, 0.f}};
+#pragma unroll
+        for (int u = 0; u < kDeep<T>; ++u) {
+            float x[kPer<T>];
+            unpack(raw[u], x);
+#pragma unroll
+            for (int e = 0; e < kPer<T>; e += 2) s[u & 1] = add2(s[u & 1], exp2_two(x[e], x[e + 1], from, scale));
+        }
+        s[0] = add2(s[0], s[1]);
+        sum += s[0].x + s[0].y;
+    }
+};
+
+// A float as a double by moving its bits: the conversion instruction has a sixteenth of an SM's lanes and sets the pace of a pass of
+// exponentials.  Zeros and denormals come out off by up to 2^-126, infinities as 2^128.
+__device__ __forceinline__ double widen(float x) {
+    const uint32_t u = __float_as_uint(x);
+    return __hiloint2double((int)((u & 0x80000000u) | (((u & 0x7fffffffu) >> 3) + 0x38000000u)), (int)(u << 29));
+}
+
+// exp((z - top) / T) in 64 bits: 2^(k / 64) from a table of 64, times a Taylor polynomial of 2^f for the rest, |f| <= 1 / 128: the
+// table-driven scheme of P. T. P. Tang, ACM TOMS 15 (1989).  The degree 4 leaves (ln 2 / 128)^5 / 120 = 4e-14 of the value.
+// Exactly 1 for the largest logit, and the same for equal ones.
 struct Mass {
-    double scale;                                  // log2(e) / T
+    double scale;                                  // 64 log2(e) / T
+    double top_wide;
+    float least;                                   // logits below have less than 2^-1000: 0
+    bool tiny;                                     // a temperature beside which what widen() moves is not nothing
     const double *table;                           // 64 entries in shared memory
 
     static __device__ __forceinline__ void fill(double *table) {
         if (threadIdx.x < 64) table[threadIdx.x] = exp2((double)threadIdx.x / 64.0);
     }
-    // exp(d / T), d <= 0; 0 below 2^-1000 and for d = -inf
-    __device__ __forceinline__ double of(double d) const {
-        const double y = d * scale;
-        if (!(y > -1000.0)) return 0.0;
+    __device__ __forceinline__ Mass(float T, float top, const double *table) : scale(64.0 * 1.4426950408889634 / (double)T), table(table) {
+        tiny = T < 1e-20f;
+        top_wide = tiny ? (double)top : widen(top);
+        least = (float)((double)top - 693.0 * (double)T);
+    }
+    // z <= top; 0 for -inf
+    __device__ __forceinline__ double of(float z) const {
+        if (!(z >= least)) return 0.0;
+        const double d = (tiny ? (double)z : widen(z)) - top_wide;
         const double magic = 6755399441055744.0;   // 1.5 * 2^52: adding it rounds to whole numbers
-        const double t = fma(y, 64.0, magic);
+        const double t = fma(d, scale, magic);
         const int k = __double2loint(t);
-        const double f = fma(t - magic, -1.0 / 64.0, y) * 0.6931471805599453;
-        double r = 1.0 / 120.0;
-        r = fma(r, f, 1.0 / 24.0);
-        r = fma(r, f, 1.0 / 6.0);
-        r = fma(r, f, 0.5);
-        r = fma(r, f, 1.0);
+        const double f = fma(d, scale, magic - t);
+        constexpr double kUnit = 0.6931471805599453 / 64.0;
+        double r = kUnit * kUnit * kUnit * kUnit / 24.0;
+        r = fma(r, f, kUnit * kUnit * kUnit / 6.0);
+        r = fma(r, f, kUnit * kUnit / 2.0);
+        r = fma(r, f, kUnit);
         r = fma(r, f, 1.0);
         r *= table[k & 63];
         return __hiloint2double(__double2hiint(r) + ((k >> 6) << 20), __double2loint(r));
@@ -228,11 +377,12 @@ struct Mass {
 
 // ---- sorting and scanning in a CTA ---------------------------------------------------------------
 // Bitonic sort of n numbers (a power of two), largest first.
+template <int NT = kThreads>
 __device__ __forceinline__ void sort_down(uint64_t *list, int n) {
     for (int size = 2; size <= n; size <<= 1)
         for (int step = size >> 1; step > 0; step >>= 1) {
             __syncthreads();
-            for (int i = threadIdx.x; i < n / 2; i += kThreads) {
+            for (int i = threadIdx.x; i < n / 2; i += NT) {
                 const int a = 2 * i - (i & (step - 1)), b = a + step;
                 const uint64_t x = list[a], y = list[b];
                 if ((x < y) == ((a & size) == 0)) { list[a] = y; list[b] = x; }
@@ -301,10 +451,10 @@ inline Plan plan_for(const dsbd_rows_t *r) {
     return p;
 }
 
-template <class Args>
+template <int NT = kThreads, class Args>
 int launch(void (*kernel)(Args), int rows, const Plan &p, size_t more, const Args &a, dsbd_stream_t stream) {
     const size_t bytes = (size_t)p.words * 16 + more;
-    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes) != cudaSuccess) {
+    if (bytes > 16 * 1024 && cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes) != cudaSuccess) {
         cudaGetLastError();
         return DSBD_ERR_CUDA;
     }
@@ -316,7 +466,7 @@ int launch(void (*kernel)(Args), int rows, const Plan &p, size_t more, const Arg
     attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)(rows * p.ctas));
-    cfg.blockDim = dim3(kThreads);
+    cfg.blockDim = dim3(NT);
     cfg.dynamicSmemBytes = bytes;
     cfg.stream = reinterpret_cast<cudaStream_t>(stream);
     cfg.attrs = attr;

@@ -11,13 +11,12 @@
 //     whole numbers (2^62 / V' of the largest token's mass, V' the power of two from V on), so sums do not depend on their order.
 // The draw is the first kept token in the tokens' order whose cumulative mass exceeds u times the whole.  Masses and sums are in 64
 // bits: a token changes when a sum moves across it, and a long-tailed row has cells narrower than the rounding of sums in 32 bits.
-#include "dsbd_rows.cuh"
+#include "dsbd_top.cuh"
 
 namespace dsbd {
 namespace rows {
 namespace {
 
-constexpr int kBins = 512;
 static_assert(kBins == kThreads, "a thread for each bin");
 constexpr int kTop = DSBD_MAX_TOP;                 // tokens that a cut by list keeps, at most
 constexpr int kList = 2 * kTop;                    // entries of the list
@@ -33,17 +32,6 @@ struct SampleArgs {
     const float *uniform;
     int32_t *token;
     float *logp;
-    int32_t *status;
-};
-
-struct TopArgs {
-    const void *logits;
-    int64_t stride;
-    int rows, V, K, ctas, per;
-    float temperature;
-    float *value;
-    int32_t *index;
-    float *rest;
     int32_t *status;
 };
 
@@ -132,17 +120,6 @@ __device__ __forceinline__ bool bring(Row<T> &r, const T *row, float4 *mem, int3
     return true;
 }
 
-// Number of the bin of width 1 / scale below the row's largest logit; falls nowhere as z grows.
-__device__ __forceinline__ int bin_below(float top, float z, float scale) {
-    return min(__float2int_rz((top - z) * scale), kBins - 1);
-}
-
-// Bins that span `width`; none (everything in one) where the width has no finite inverse.
-__device__ __forceinline__ float bins_over(float width) {
-    const float scale = (float)(kBins - 1) / width;
-    return scale < 1e30f ? scale : 0.f;
-}
-
 // The cluster's totals of bin threadIdx.x, after a barrier behind the filling.
 template <class T>
 __device__ __forceinline__ uint32_t bin_count(const Row<T> &r, Hist &h) {
@@ -169,9 +146,15 @@ __device__ __forceinline__ void clear(Hist &h) {
 
 // Mass as a whole number.
 struct Whole {
-    Mass mass;
-    double unit, top;
-    __device__ __forceinline__ uint64_t of(float z) const { return __double2ull_rz(mass.of((double)z - top) * unit); }
+    const Mass &mass;
+    double unit;
+    __device__ __forceinline__ uint64_t of(float z) const {
+        // (by its bits, see widen)
+        const uint64_t bits = (uint64_t)__double_as_longlong(mass.of(z) * unit);
+        const int up = (int)(bits >> 52) - 1075;
+        const uint64_t digits = (bits & 0xfffffffffffffull) | 0x10000000000000ull;
+        return up >= 0 ? digits << up : up > -53 ? digits >> -up : 0;
+    }
 };
 
 // The token of rank `rank` (from 0) among those of the share that `is` holds for, of all CTAs, in the tokens' order.
@@ -355,8 +338,6 @@ __device__ int list_top(Row<T> &r, int k) {
     return (int)sum;
 }
 
-__device__ __forceinline__ float logit_of(uint64_t entry) { return of_key((uint32_t)(entry >> 32)); }
-__device__ __forceinline__ int token_of(uint64_t entry) { return (int)~(uint32_t)entry; }
 
 // ------------------------------------------------------------------------------------ draws
 struct Settings {
@@ -391,7 +372,7 @@ __device__ void draw_listed(Row<T> &r, const SampleArgs &a, int row, const Setti
 #pragma unroll
     for (int i = 0; i < kMine; ++i) {
         const int at = threadIdx.x * kMine + i;
-        w[i] = at < n ? mass.of((double)logit_of(sh.list[at]) - (double)r.top) : 0.0;
+        w[i] = at < n ? mass.of(logit_of(sh.list[at])) : 0.0;
         mine += w[i];
     }
     double upto = before(mine, &total, sh.sums);
@@ -424,7 +405,7 @@ __device__ void draw_listed(Row<T> &r, const SampleArgs &a, int row, const Setti
 #pragma unroll
     for (int i = 0; i < kMine; ++i) {
         const int at = threadIdx.x * kMine + i;
-        w[i] = at < n ? mass.of((double)of_key((uint32_t)sh.list[at]) - (double)r.top) : 0.0;
+        w[i] = at < n ? mass.of(of_key((uint32_t)sh.list[at])) : 0.0;
         mine += w[i];
     }
     upto = before(mine, &total, sh.sums);
@@ -469,7 +450,7 @@ __device__ void draw_shared(Row<T> &r, const SampleArgs &a, int row, const Setti
         double sum = 0.0;
 #pragma unroll
         for (int e = 0; e < kPer<T>; ++e) {
-            m[e] = x[e] > z_cut || (x[e] == z_cut && t + e <= cut.token) ? mass.of((double)x[e] - top) : 0.0;
+            m[e] = x[e] > z_cut || (x[e] == z_cut && t + e <= cut.token) ? mass.of(x[e]) : 0.0;
             if (!(m[e] >= least)) m[e] = 0.0;
             sum += m[e];
         }
@@ -580,7 +561,7 @@ __global__ void __launch_bounds__(kThreads) k_sample(SampleArgs a) {
             }
         return;
     }
-    const Mass mass = {1.4426950408889634 / (double)set.T, sh.table};
+    const Mass mass(set.T, r.top, sh.table);
     Cut cut = {kKeyMasked, -1};                    // everything above -inf
     const bool by_rank = set.k > 0 && set.k < a.V;
     if (by_rank && set.k <= kTop) {
@@ -590,112 +571,10 @@ __global__ void __launch_bounds__(kThreads) k_sample(SampleArgs a) {
             return;
         }
     }
-    const Whole whole = {mass, (double)(1ull << (30 + __clz(a.V - 1 | 1))), (double)r.top};
+    const Whole whole = {mass, (double)(1ull << (30 + __clz(a.V - 1 | 1)))};
     if (by_rank) cut = cut_at<false>(r, cut, (uint32_t)set.k, 0.0, whole, 2.f * (r.top - r.low));
     if (set.p < 1.f) cut = cut_at<true>(r, cut, 0, (double)set.p, whole, 64.f * 0.6931472f * set.T);
     draw_shared(r, a, row, set, cut, mass);
-}
-
-// ------------------------------------------------------------------------------------ largest logits
-template <class T>
-__global__ void __launch_bounds__(kThreads) k_top(TopArgs a) {
-    extern __shared__ float4 mem[];
-    __shared__ Shared sh;
-    asm volatile("griddepcontrol.wait;" ::: "memory");
-    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-    begun_arrive(a.ctas);
-    const int row = blockIdx.x / a.ctas, rank = blockIdx.x - row * a.ctas;
-    const T *at = static_cast<const T *>(a.logits) + (int64_t)row * a.stride;
-    float *value_out = a.value + (int64_t)row * a.K;
-    int32_t *index_out = a.index + (int64_t)row * a.K;
-    Row<T> r = {share<T>(at, a.V, rank, a.per), mem, sh, a.ctas, rank, a.V, 0, 0, 0.f, 0.f, 0.f};
-    if (!bring<T>(r, at, mem, a.status)) {
-        if (rank == 0) {
-            for (int i = threadIdx.x; i < a.K; i += kThreads) {
-                value_out[i] = CUDART_NAN_F;
-                index_out[i] = -1;
-            }
-            if (threadIdx.x == 0 && a.rest) a.rest[row] = CUDART_NAN_F;
-        }
-        return;
-    }
-    int n = list_top(r, a.K);
-    if (n < 0) {
-        // more ties than the list holds: the cut, then the K tokens that it keeps
-        const Cut cut = cut_at<false>(r, Cut{kKeyMasked, -1}, (uint32_t)a.K, 0.0, Whole{}, 2.f * (r.top - r.low));
-        if (threadIdx.x == 0) sh.listed = 0;
-        __syncthreads();
-        each<T>(r.s, r.mem, [&](int t, float z) {
-            const uint32_t key = key_of(z);
-            if (cut.keeps(key, t)) sh.list[atomicAdd(&sh.listed, 1u)] = ((uint64_t)key << 32) | (uint32_t)~t;
-        });
-        __syncthreads();
-        const Note *all = r.tell_all({0.0, 0.f, 0.f, sh.listed, 0});
-        if (rank == 0) {
-            uint32_t from = all[0].a;
-            for (int c = 1; c < a.ctas; ++c) {
-                const uint64_t *list = r.of(&sh.list[0], c);
-                for (uint32_t i = threadIdx.x; i < all[c].a; i += kThreads) sh.list[from + i] = list[i];
-                from += all[c].a;
-            }
-            int size = 2;
-            while (size < a.K) size <<= 1;
-            for (int i = a.K + threadIdx.x; i < size; i += kThreads) sh.list[i] = 0;
-            sort_down(sh.list, size);
-        }
-        n = a.K;
-    }
-    // the last entry, which everything that is not kept lies behind
-    const int kept = min(n, a.K);
-    Note last = {0.0, 0.f, 0.f, 0, 0};
-    if (rank == 0) {
-        last.a = (uint32_t)(sh.list[kept - 1] >> 32);
-        last.b = ~(uint32_t)sh.list[kept - 1];
-    }
-    last = r.tell_all(last)[0];
-    if (a.rest) {
-        // Each thread's sum is relative to the largest of its logits that are not kept (relative to one that is kept it may vanish).
-        // Terms in 32 bits (2^-22 each, by ex2.approx and the rounded argument), a thread's words together, the threads' sums in 64.
-        const float z0 = of_key(last.a);
-        const int t0 = (int)last.b;
-        const double scale = 1.4426950408889634 / (double)a.temperature;
-        const float scale_f = (float)scale;
-        float mine = -CUDART_INF_F, sum = 0.f;
-        each<T>(r.s, r.mem, [&](int t, float z) {
-            if (z < z0 || (z == z0 && t > t0)) mine = fmaxf(mine, z);
-        });
-        const float from = mine == -CUDART_INF_F ? 0.f : mine;
-        each<T>(r.s, r.mem, [&](int t, float z) {
-            if (z < z0 || (z == z0 && t > t0)) sum += exp2_fast((z - from) * scale_f);
-        });
-        const float high = over_cta(mine, larger, reinterpret_cast<float *>(sh.scratch));
-        const double part = over_cta((double)sum * rescale(mine, high, scale), add, sh.sums);
-        const Note *all = r.tell_all({part, high, 0.f, 0, 0});
-        if (rank == 0 && threadIdx.x == 0) {
-            float top = -CUDART_INF_F;
-            for (int c = 0; c < a.ctas; ++c) top = fmaxf(top, all[c].high);
-            double whole = 0.0;
-            for (int c = 0; c < a.ctas; ++c) whole += all[c].sum * rescale(all[c].high, top, scale);
-            a.rest[row] = whole > 0.0 ? (float)((double)top / (double)a.temperature + log(whole)) : -CUDART_INF_F;
-        }
-    }
-    if (rank) return;
-    for (int i = threadIdx.x; i < kept; i += kThreads) {
-        value_out[i] = logit_of(sh.list[i]);
-        index_out[i] = token_of(sh.list[i]);
-    }
-    if (threadIdx.x < 32)
-        // fewer than K above -inf: the first tokens at -inf
-        for (int t0 = 0, at_out = kept; at_out < a.K && t0 < a.V; t0 += 32) {
-            const int t = t0 + threadIdx.x;
-            const unsigned m = __ballot_sync(kFull, t < a.V && value_of(at[min(t, a.V - 1)]) == -CUDART_INF_F);
-            const int to = at_out + __popc(m & ((1u << threadIdx.x) - 1));
-            if ((m >> threadIdx.x & 1) && to < a.K) {
-                value_out[to] = -CUDART_INF_F;
-                index_out[to] = t;
-            }
-            at_out += __popc(m);
-        }
 }
 
 }  // namespace
@@ -723,21 +602,4 @@ extern "C" int dsbd_sample_rows(const dsbd_rows_t *rows, const dsbd_sample_param
     a.uniform = uniform; a.token = token; a.logp = logp; a.status = status;
     return rows->dtype == DSBD_DTYPE_F32 ? launch(k_sample<float>, rows->rows, plan, 0, a, stream)
                                          : launch(k_sample<__nv_bfloat16>, rows->rows, plan, 0, a, stream);
-}
-
-extern "C" int dsbd_top_logits(const dsbd_rows_t *rows, int32_t K, float temperature, float *value, int32_t *index, float *rest,
-                               int32_t *status, dsbd_stream_t stream) {
-    int rc = check_rows(rows);
-    if (rc) return rc;
-    if (K <= 0 || K > rows->V || !(temperature > 0.f && temperature <= FLT_MAX) || !status) return DSBD_ERR_INVALID_ARG;
-    if (K > DSBD_MAX_TOP) return DSBD_ERR_UNSUPPORTED;
-    if (rows->rows == 0) return DSBD_OK;
-    if (!rows->logits || !value || !index) return DSBD_ERR_INVALID_ARG;
-    const Plan plan = plan_for(rows);
-    TopArgs a = {};
-    a.logits = rows->logits; a.stride = rows->row_stride; a.rows = rows->rows; a.V = rows->V; a.K = K;
-    a.ctas = plan.ctas; a.per = plan.per; a.temperature = temperature;
-    a.value = value; a.index = index; a.rest = rest; a.status = status;
-    return rows->dtype == DSBD_DTYPE_F32 ? launch(k_top<float>, rows->rows, plan, 0, a, stream)
-                                         : launch(k_top<__nv_bfloat16>, rows->rows, plan, 0, a, stream);
 }
