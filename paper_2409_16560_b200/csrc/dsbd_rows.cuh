@@ -332,7 +332,8 @@ struct Rest {
 };
 
 // A float as a double by moving its bits: the conversion instruction has a sixteenth of an SM's lanes and sets the pace of a pass of
-// exponentials.  Zeros and denormals come out off by up to 2^-126, infinities as 2^128.
+// exponentials.  Zeros and denormals come out off by up to 2^-126 (nothing beside a temperature of kLeastTemperature), infinities as 2^128.
+constexpr float kLeastTemperature = DSBD_MIN_TEMPERATURE;
 __device__ __forceinline__ double widen(float x) {
     const uint32_t u = __float_as_uint(x);
     return __hiloint2double((int)((u & 0x80000000u) | (((u & 0x7fffffffu) >> 3) + 0x38000000u)), (int)(u << 29));
@@ -343,23 +344,25 @@ __device__ __forceinline__ double widen(float x) {
 // Exactly 1 for the largest logit, and the same for equal ones.
 struct Mass {
     double scale;                                  // 64 log2(e) / T
+    double reach;                                  // 693 T: logits further below have less than 2^-999, and count as 0
     double top_wide;
-    float least;                                   // logits below have less than 2^-1000: 0
-    bool tiny;                                     // a temperature beside which what widen() moves is not nothing
+    float least;
     const double *table;                           // 64 entries in shared memory
 
     static __device__ __forceinline__ void fill(double *table) {
         if (threadIdx.x < 64) table[threadIdx.x] = exp2((double)threadIdx.x / 64.0);
     }
-    __device__ __forceinline__ Mass(float T, float top, const double *table) : scale(64.0 * 1.4426950408889634 / (double)T), table(table) {
-        tiny = T < 1e-20f;
-        top_wide = tiny ? (double)top : widen(top);
-        least = (float)((double)top - 693.0 * (double)T);
+    __device__ __forceinline__ Mass(float T, float top, const double *table)
+        : scale(64.0 * 1.4426950408889634 / (double)T), reach(693.0 * (double)T), table(table) {
+        relative_to(top);
+    }
+    __device__ __forceinline__ void relative_to(float top) {
+        top_wide = widen(top);
+        least = (float)((double)top - reach);
     }
     // z <= top; 0 for -inf
     __device__ __forceinline__ double of(float z) const {
-        if (!(z >= least)) return 0.0;
-        const double d = (tiny ? (double)z : widen(z)) - top_wide;
+        const double d = widen(z) - top_wide;
         const double magic = 6755399441055744.0;   // 1.5 * 2^52: adding it rounds to whole numbers
         const double t = fma(d, scale, magic);
         const int k = __double2loint(t);
@@ -371,7 +374,8 @@ struct Mass {
         r = fma(r, f, kUnit);
         r = fma(r, f, 1.0);
         r *= table[k & 63];
-        return __hiloint2double(__double2hiint(r) + ((k >> 6) << 20), __double2loint(r));
+        // (no branch: the steps of several logits take turns)
+        return z >= least ? __hiloint2double(__double2hiint(r) + ((k >> 6) << 20), __double2loint(r)) : 0.0;
     }
 };
 
@@ -391,6 +395,67 @@ __device__ __forceinline__ void sort_down(uint64_t *list, int n) {
     __syncthreads();
 }
 
+// n numbers, largest first, by their bins (an order of its own: bin(x) falls nowhere as x falls), and in a bin by counting.  tmp: n numbers.  count:
+// BINS numbers, scan: one for each warp.  Where a bin has many, by sort_down (list has room for a power of two then).
+// A step of a sort in shared memory takes 500 cycles, 66 steps for 2048 numbers; this takes about 4000 in all.
+template <int NT, int BINS, class F>
+__device__ __forceinline__ void order_down(uint64_t *list, uint64_t *tmp, int n, uint32_t *count, uint32_t *scan, F bin) {
+    static_assert(BINS % NT == 0, "");
+    constexpr int kEach = BINS / NT;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x / 32;
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) count[threadIdx.x + i * NT] = 0;
+    __syncthreads();
+    for (int i = threadIdx.x; i < n; i += NT) atomicAdd(&count[bin(list[i])], 1u);
+    __syncthreads();
+    uint32_t c[kEach], sum = 0, most = 0;
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+        c[i] = count[threadIdx.x * kEach + i];
+        sum += c[i];
+        most = max(most, c[i]);
+    }
+    uint32_t up = sum;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const uint32_t x = __shfl_up_sync(kFull, up, o);
+        if (lane >= o) up += x;
+    }
+    if (lane == 31) scan[warp] = up;
+    if (__syncthreads_or(most > 48)) {
+        int size = 2;
+        while (size < n) size <<= 1;
+        for (int i = n + threadIdx.x; i < size; i += NT) list[i] = 0;
+        sort_down<NT>(list, size);
+        return;
+    }
+    uint32_t at = up - sum;
+#pragma unroll
+    for (int w = 0; w < NT / 32; ++w) at += w < warp ? scan[w] : 0;
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+        count[threadIdx.x * kEach + i] = at;
+        at += c[i];
+    }
+    __syncthreads();
+    for (int i = threadIdx.x; i < n; i += NT) {
+        const uint64_t x = list[i];
+        tmp[atomicAdd(&count[bin(x)], 1u)] = x;
+    }
+    __syncthreads();
+    // (count: where each bin ends)
+    for (int i = threadIdx.x; i < n; i += NT) {
+        const uint64_t x = tmp[i];
+        const int b = bin(x);
+        const uint32_t begin = b ? count[b - 1] : 0, end = count[b];
+        uint32_t rank = begin;
+        for (uint32_t k = begin; k < end; ++k) rank += tmp[k] > x;
+        list[rank] = x;
+    }
+    __syncthreads();
+}
+
 template <class P>
 __device__ __forceinline__ P shuffle_up(P v, int o) {
     uint32_t u[sizeof(P) / 4];
@@ -401,8 +466,8 @@ __device__ __forceinline__ P shuffle_up(P v, int o) {
     return v;
 }
 
-// Sum of the v of the threads before this one; *total: of all.  scratch: kWarps entries.
-template <class P>
+// Sum of the v of the threads before this one; *total: of all.  scratch: an entry for each warp.
+template <int NT = kThreads, class P>
 __device__ __forceinline__ P before(P v, P *total, P *scratch) {
     const int lane = threadIdx.x & 31, warp = threadIdx.x / 32;
     P up = v;
@@ -416,7 +481,7 @@ __device__ __forceinline__ P before(P v, P *total, P *scratch) {
     __syncthreads();
     P base = 0, all = 0;
 #pragma unroll
-    for (int w = 0; w < kWarps; ++w) {
+    for (int w = 0; w < NT / 32; ++w) {
         const P x = scratch[w];
         if (w < warp) base += x;
         all += x;
@@ -452,8 +517,7 @@ inline Plan plan_for(const dsbd_rows_t *r) {
 }
 
 template <int NT = kThreads, class Args>
-int launch(void (*kernel)(Args), int rows, const Plan &p, size_t more, const Args &a, dsbd_stream_t stream) {
-    const size_t bytes = (size_t)p.words * 16 + more;
+int launch(void (*kernel)(Args), int rows, const Plan &p, size_t bytes, const Args &a, dsbd_stream_t stream) {
     if (bytes > 16 * 1024 && cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes) != cudaSuccess) {
         cudaGetLastError();
         return DSBD_ERR_CUDA;

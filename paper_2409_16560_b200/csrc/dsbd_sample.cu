@@ -1,16 +1,19 @@
-// Draws from rows of logits with each row's own temperature, top-k, top-p and min-p, and the largest logits of rows.
+// Draws from rows of logits with each row's own temperature, top-k, top-p and min-p.
 //
-// A row belongs to a cluster of 1 to 8 CTAs, which brings it into shared memory once; every later step reads it there.
-//
-// Cuts.  Temperature, top-k, top-p and min-p all keep a prefix of the tokens in falling order of (logit, -token), so a row's cuts are one
-// pair (key, token): kept is what lies at or above it.
-//   up to kTop tokens: each thread has the largest of its words; the k-th largest of those maxima (by bins) is at or below the
-//     k-th largest logit, and little more than k tokens reach it.  They go to a list in one CTA, which sorts it.
-//   otherwise, or where more tokens tie than the list holds: a histogram of 512 bins over the cluster, linear in the logit first,
-//     then in the bits of the keys of the bin that the cut is in, until that is one key; equal keys go by token.  Masses are
-//     whole numbers (2^62 / V' of the largest token's mass, V' the power of two from V on), so sums do not depend on their order.
 // The draw is the first kept token in the tokens' order whose cumulative mass exceeds u times the whole.  Masses and sums are in 64
 // bits: a token changes when a sum moves across it, and a long-tailed row has cells narrower than the rounding of sums in 32 bits.
+//
+// Temperature, top-k, top-p and min-p all keep a prefix of the tokens in falling order of (logit, -token).
+//   k_draw: rows that need one pass.  No cut: each warp's batches of 1024 tokens leave their mass, relative to their largest logit; the
+//     batch that the target falls into is read again.  Top-k up to a few hundred (and with it top-p and min-p), or the largest logit: the k
+//     largest logits come to a list in one CTA, sorted, and all the rest is done there.
+//   k_draw_cut: the other rows.  A cluster of 1 to 8 CTAs brings the row into shared memory once; every later step reads it there.
+//     Larger top-k: each thread has the largest of its words; the k-th largest of those maxima (by bins) is at or below the k-th largest
+//     logit, and little more than k tokens reach it.  Top-p, min-p: a histogram of masses by bins of the logit, rounded down a little, says which
+//     bins certainly hold the prefix.  These tokens go to a list in one CTA, as above.
+//     Where the list does not hold them: a histogram of 512 bins over the cluster, linear in the logit first, then in the bits of the
+//     keys of the bin that the cut is in, until that is one key; equal keys go by token.  Masses are then whole numbers (2^62 / V' of the
+//     largest token's mass, V' the power of two from V on), so sums do not depend on their order.  Then the draw over all shares.
 #include "dsbd_top.cuh"
 
 namespace dsbd {
@@ -19,12 +22,14 @@ namespace {
 
 static_assert(kBins == kThreads, "a thread for each bin");
 constexpr int kTop = DSBD_MAX_TOP;                 // tokens that a cut by list keeps, at most
-constexpr int kList = 2 * kTop;                    // entries of the list
+constexpr int kList = 4 * kTop;                    // entries of the list
 
 struct SampleArgs {
     const void *logits;
     int64_t stride;
-    int rows, V, draws, ctas, per;
+    int V, draws, ctas, per;
+    int list_most;                                 // largest top-k that k_draw takes
+    int words, list_room;                          // k_draw_cut: 16-byte words of shared memory before the list, entries of the list
     float temperature, top_p, min_p;
     int top_k;
     const float *temperature_r, *top_p_r, *min_p_r;
@@ -48,11 +53,7 @@ struct Note {
 struct Shared {
     double table[64];
     Told<Note> told;
-    union {
-        Hist hist[2];
-        double mass[kTop];                         // of the list's entries, in the CTA that sorts
-    };
-    uint64_t list[kList];
+    Hist hist[2];
     Note scratch[kWarps];
     double sums[kWarps + 1];
     uint64_t scan[kWarps];
@@ -74,11 +75,14 @@ struct Row {
     Share s;
     const float4 *mem;
     Shared &sh;
-    int ctas, rank, V;
+    uint64_t *list;                                // of `room` entries
+    int room, ctas, rank, V;
     int note_turn, hist_turn;
     float top, low;                                // the largest logit; the smallest of the threads' finite maxima
     float mine;                                    // this thread's maximum
 
+    // (rank 0, which needs its share no more once the list is whole)
+    __device__ __forceinline__ uint64_t *tmp() const { return reinterpret_cast<uint64_t *>(const_cast<float4 *>(mem)); }
     __device__ __forceinline__ const Note *tell_all(const Note &n) { return tell(n, sh.told, note_turn, ctas, rank); }
     template <class P>
     __device__ __forceinline__ P *of(P *p, int c) const { return ctas > 1 ? cg::this_cluster().map_shared_rank(p, c) : p; }
@@ -291,6 +295,77 @@ __device__ Cut cut_at(Row<T> &r, Cut within, uint32_t k, double p, const Whole &
     }
 }
 
+// The tokens of the bins up to `last` below the row's largest logit, as (key, ~token) in falling order, in the list of rank 0; returns
+// their number there, and -1 everywhere if the list does not hold them.
+template <class T>
+__device__ int list_bins(Row<T> &r, float scale, int last) {
+    Shared &sh = r.sh;
+    if (threadIdx.x == 0) sh.listed = 0;
+    __syncthreads();
+    each<T>(r.s, r.mem, [&](int t, float z) {
+        if (z == -CUDART_INF_F || (last < kBins - 1 && (r.top - z) * scale >= (float)(last + 1))) return;
+        const uint32_t at = next_place(&sh.listed);
+        if (at < (uint32_t)r.room) r.list[at] = entry_of(z, t);
+    });
+    __syncthreads();
+    const Note *all = r.tell_all({0.0, 0.f, 0.f, sh.listed, 0});
+    uint32_t sum = 0;
+    for (int c = 0; c < r.ctas; ++c) sum += all[c].a;
+    if (sum > (uint32_t)r.room) return -1;
+    if (r.rank == 0) {
+        uint32_t at = all[0].a;
+        for (int c = 1; c < r.ctas; ++c) {
+            const uint64_t *from = r.of(r.list, c);
+            for (uint32_t i = threadIdx.x; i < all[c].a; i += kThreads) r.list[at + i] = from[i];
+            at += all[c].a;
+        }
+    }
+    cluster_barrier(r.ctas);                       // (the others' lists have been read)
+    if (r.rank == 0) {
+        const float finer = scale * ((float)kBins / (float)(last + 1));
+        order_down<kThreads, kBins>(r.list, r.tmp(), (int)sum, sh.hist[0].count, reinterpret_cast<uint32_t *>(sh.scan),
+                                    [&](uint64_t e) { return bin_below(r.top, logit_of(e), finer); });
+    }
+    return (int)sum;
+}
+
+// The tokens that certainly hold the shortest prefix of p of the mass (p < 1), or those of at least m of the largest one's, listed as in
+// list_bins; *whole: the row's mass (p < 1).  A bin's mass is summed in steps of 2^-14 of its largest, rounded down: what is found to have p of the whole
+// has it, and the list is exact.
+template <class T>
+__device__ int list_mass(Row<T> &r, float p, float m, float T_, const Mass &mass, double *whole) {
+    Shared &sh = r.sh;
+    constexpr float kOctaves = 48.f;               // that the bins span
+    const float scale = bins_over(kOctaves * 0.6931472f * T_), step = kOctaves / (float)(kBins - 1);
+    int last = kBins - 1;
+    if (m > 0.f) last = min(last, (int)(-log2f(m) / step) + 1);
+    if (p < 1.f) {
+        Hist &h = sh.hist[r.hist_turn++ & 1];
+        clear<false>(h);
+        double sum = 0.0;
+        each<T>(r.s, r.mem, [&](int, float z) {
+            sum += mass.of(z);
+            const float x = (r.top - z) * scale;
+            const int b = (int)fminf(x, (float)(kBins - 1));
+            if (b < kBins - 1) atomicAdd(&h.count[b], (uint32_t)(exp2_fast(((float)b - x) * step) * 16384.f));
+        });
+        sum = over_cta(sum, add, sh.sums);
+        if (threadIdx.x == 0) sh.picked_bin = kBins - 1;
+        const Note *all = r.tell_all({sum, 0.f, 0.f, 0, 0});
+        sum = 0.0;
+        for (int c = 0; c < r.ctas; ++c) sum += all[c].sum;
+        *whole = sum;
+        const double v = (double)((float)bin_count(r, h) * exp2_fast(-(float)threadIdx.x * step)) * (1.0 / 16384.0);
+        double all_bins;
+        const double upto = before(v, &all_bins, sh.sums);
+        const double goal = (double)p * sum * (1.0 + 1e-4);
+        if (upto < goal && upto + v >= goal) sh.picked_bin = threadIdx.x;
+        __syncthreads();
+        last = min(last, (int)sh.picked_bin);
+    }
+    return list_bins(r, scale, last);
+}
+
 // The tokens at or above the k-th largest logit, as (key, ~token) in falling order, in the list of rank 0; returns their
 // number there, and -1 everywhere if the list does not hold them.  k <= kTop; fewer than k where the row has fewer above -inf.
 template <class T>
@@ -299,10 +374,7 @@ __device__ int list_top(Row<T> &r, int k) {
     const float scale = bins_over(r.top - r.low);
     Hist &h = sh.hist[r.hist_turn++ & 1];
     clear<false>(h);
-    if (threadIdx.x == 0) {
-        sh.listed = 0;
-        sh.picked_bin = kBins - 1;
-    }
+    if (threadIdx.x == 0) sh.picked_bin = kBins - 1;
     if (r.mine > -CUDART_INF_F) atomicAdd(&h.count[bin_below(r.top, r.mine, scale)], 1u);
     cluster_barrier(r.ctas);
     uint64_t total;
@@ -310,40 +382,27 @@ __device__ int list_top(Row<T> &r, int k) {
     if (excl < (uint64_t)k && excl + n >= (uint64_t)k) sh.picked_bin = threadIdx.x;
     __syncthreads();
     const int last = (int)sh.picked_bin;
-    each<T>(r.s, r.mem, [&](int t, float z) {
-        if (z == -CUDART_INF_F || (last < kBins - 1 && (r.top - z) * scale >= (float)(last + 1))) return;
-        const uint32_t at = atomicAdd(&sh.listed, 1u);
-        if (at < (uint32_t)kList) sh.list[at] = ((uint64_t)key_of(z) << 32) | (uint32_t)~t;
-    });
-    __syncthreads();
-    const Note *all = r.tell_all({0.0, 0.f, 0.f, sh.listed, 0});
-    uint32_t sum = 0;
-    for (int c = 0; c < r.ctas; ++c) sum += all[c].a;
-    if (sum > (uint32_t)kList) return -1;
-    if (r.rank == 0) {
-        uint32_t at = all[0].a;
-        for (int c = 1; c < r.ctas; ++c) {
-            const uint64_t *from = r.of(&sh.list[0], c);
-            for (uint32_t i = threadIdx.x; i < all[c].a; i += kThreads) sh.list[at + i] = from[i];
-            at += all[c].a;
-        }
-    }
-    cluster_barrier(r.ctas);                       // (the others' lists have been read)
-    if (r.rank == 0) {
-        int size = 2;
-        while (size < (int)sum) size <<= 1;
-        for (int i = sum + threadIdx.x; i < size; i += kThreads) sh.list[i] = 0;
-        sort_down(sh.list, size);
-    }
-    return (int)sum;
+    return list_bins(r, scale, last);
 }
-
 
 // ------------------------------------------------------------------------------------ draws
 struct Settings {
     float T, p, m;
-    int k;
+    int k;                                         // 0: off
 };
+
+enum Kind { kBad, kGreedy, kListed, kPlain, kCut };
+
+__device__ __forceinline__ Kind settings_of(const SampleArgs &a, int row, Settings &set) {
+    set = {a.temperature, a.top_p, a.min_p, a.top_k};
+    if (a.temperature_r) set.T = a.temperature_r[row];
+    if (a.top_p_r) set.p = a.top_p_r[row];
+    if (a.min_p_r) set.m = a.min_p_r[row];
+    if (a.top_k_r) set.k = a.top_k_r[row];
+    if (set.k <= 0 || set.k >= a.V) set.k = 0;
+    if (!((set.T == 0.f || set.T >= kLeastTemperature) && set.T < CUDART_INF_F && set.p > 0.f && set.m >= 0.f && set.m <= 1.f)) return kBad;
+    return set.T == 0.f ? kGreedy : set.k ? (set.k <= a.list_most ? kListed : kCut) : set.p >= 1.f && set.m == 0.f ? kPlain : kCut;
+}
 
 // A uniform number's target in a mass of `total`: below it, so that some token exceeds it.
 __device__ __forceinline__ double target(float u, double total) {
@@ -361,63 +420,61 @@ __device__ __forceinline__ void put_draw(const SampleArgs &a, int row, int d, in
     if (a.logp) a.logp[(int64_t)row * a.draws + d] = (float)logp;
 }
 
-// Draws of a list of n entries in falling order (rank 0 alone): its cuts are prefixes.
-template <class T>
-__device__ void draw_listed(Row<T> &r, const SampleArgs &a, int row, const Settings &set, int n, const Mass &mass) {
-    Shared &sh = r.sh;
+// Draws of a list of n entries in falling order (one CTA alone): its cuts are prefixes.  whole: the mass that top-p is of; 0: the list's.
+// tmp: scratch of n numbers; sums, scan: one for each warp; count: kBins.
+template <int NT, int MOST>
+__device__ void draw_listed(uint64_t *list, uint64_t *tmp, double *sums, uint32_t *count, uint32_t *scan, const SampleArgs &a, int row, const Settings &set, int n,
+                            double whole, const Mass &mass, float top) {
     const int lane = threadIdx.x & 31, warp = threadIdx.x / 32;
-    n = min(n, set.k);
-    constexpr int kMine = kTop / kThreads;         // entries of a thread, side by side
+    constexpr int kMine = MOST / NT;               // entries of a thread, side by side
+    __shared__ uint32_t first_out;
     double w[kMine], total, mine = 0.0;
+    if (threadIdx.x == 0) first_out = (uint32_t)n;
 #pragma unroll
     for (int i = 0; i < kMine; ++i) {
         const int at = threadIdx.x * kMine + i;
-        w[i] = at < n ? mass.of(logit_of(sh.list[at])) : 0.0;
+        w[i] = at < n ? mass.of(logit_of(list[at])) : 0.0;
         mine += w[i];
     }
-    double upto = before(mine, &total, sh.sums);
-    uint32_t out = 0x7fffffffu;                    // the first entry that is cut off
-#pragma unroll
-    for (int i = kMine - 1; i >= 0; --i) {
-        double b = upto;
-        for (int j = 0; j < i; ++j) b += w[j];
-        const int at = threadIdx.x * kMine + i;
-        if (at < n && ((set.p < 1.f && !(b < (double)set.p * total)) || !(w[i] >= (double)set.m))) out = at;
-    }
-    n = (int)min((uint32_t)n, over_cta(out, [](uint32_t x, uint32_t y) { return min(x, y); }, reinterpret_cast<uint32_t *>(sh.scratch)));
-    // the kept ones in the tokens' order: (~token, place) falling
+    double upto = before<NT>(mine, &total, sums);  // (barriers)
+    if (whole != 0.0) total = whole;
     uint64_t e[kMine];
 #pragma unroll
     for (int i = 0; i < kMine; ++i) {
         const int at = threadIdx.x * kMine + i;
-        e[i] = at < n ? sh.list[at] : 0;
+        if (at < n && ((set.p < 1.f && !(upto < (double)set.p * total)) || !(w[i] >= (double)set.m) || w[i] == 0.0)) atomicMin(&first_out, (uint32_t)at);
+        upto += w[i];
+        e[i] = at < n ? list[at] : 0;
     }
     __syncthreads();
-    int size = 2;
-    while (size < n) size <<= 1;
+    n = (int)first_out;
+    // the kept ones in the tokens' order: (~token, key) falling
 #pragma unroll
     for (int i = 0; i < kMine; ++i) {
         const int at = threadIdx.x * kMine + i;
-        if (at < size) sh.list[at] = at < n ? (e[i] << 32) | (e[i] >> 32) : 0;
+        if (at < n) list[at] = (e[i] << 32) | (e[i] >> 32);
     }
-    sort_down(sh.list, size);
+    const float per_bin = (float)kBins / (float)a.V;
+    order_down<NT, kBins>(list, tmp, n, count, scan, [&](uint64_t x) { return min((int)((float)~(uint32_t)(x >> 32) * per_bin), kBins - 1); });
+    double *upto_of = reinterpret_cast<double *>(tmp);
     mine = 0.0;
 #pragma unroll
     for (int i = 0; i < kMine; ++i) {
         const int at = threadIdx.x * kMine + i;
-        w[i] = at < n ? mass.of(of_key((uint32_t)sh.list[at])) : 0.0;
+        w[i] = at < n ? mass.of(of_key((uint32_t)list[at])) : 0.0;
         mine += w[i];
     }
-    upto = before(mine, &total, sh.sums);
+    upto = before<NT>(mine, &total, sums);
 #pragma unroll
     for (int i = 0; i < kMine; ++i) {
         upto += w[i];
         const int at = threadIdx.x * kMine + i;
-        if (at < n) sh.mass[at] = upto;
+        if (at < n) upto_of[at] = upto;
     }
     __syncthreads();
-    total = sh.mass[n - 1];
-    for (int d = warp; d < a.draws; d += kWarps) {
+    total = upto_of[n - 1];
+    const double log_total = log(total);
+    for (int d = warp; d < a.draws; d += NT / 32) {
         const float u = a.uniform[(int64_t)row * a.draws + d];
         if (!(u >= 0.f && u <= 1.f)) {
             if (lane == 0) no_draw(a, row, d, DSBD_DEV_BAD_PARAM);
@@ -425,12 +482,11 @@ __device__ void draw_listed(Row<T> &r, const SampleArgs &a, int row, const Setti
         }
         const double t = target(u, total);
         int at = 0;
-        for (int i = lane; i < n; i += 32) at += sh.mass[i] <= t;
+        for (int i = lane; i < n; i += 32) at += upto_of[i] <= t;
         at = min((int)__reduce_add_sync(kFull, (unsigned)at), n - 1);
         if (lane == 0) {
-            const uint64_t x = sh.list[at];
-            put_draw(a, row, d, (int)~(uint32_t)(x >> 32),
-                     ((double)of_key((uint32_t)x) - (double)r.top) / (double)set.T - log(total));
+            const uint64_t x = list[at];
+            put_draw(a, row, d, (int)~(uint32_t)(x >> 32), ((double)of_key((uint32_t)x) - (double)top) / (double)set.T - log_total);
         }
     }
 }
@@ -523,58 +579,326 @@ __device__ void draw_shared(Row<T> &r, const SampleArgs &a, int row, const Setti
 }
 
 template <class T>
-__global__ void __launch_bounds__(kThreads) k_sample(SampleArgs a) {
+__global__ void __launch_bounds__(kThreads) k_draw_cut(SampleArgs a) {
     extern __shared__ float4 mem[];
     __shared__ Shared sh;
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    const int row = blockIdx.x / a.ctas, rank = blockIdx.x - row * a.ctas;
+    Settings set;
+    if (settings_of(a, row, set) != kCut) return;
     begun_arrive(a.ctas);
-    const int row = blockIdx.x / a.ctas;
-    Settings set = {a.temperature, a.top_p, a.min_p, a.top_k};
-    if (a.temperature_r) set.T = a.temperature_r[row];
-    if (a.top_p_r) set.p = a.top_p_r[row];
-    if (a.min_p_r) set.m = a.min_p_r[row];
-    if (a.top_k_r) set.k = a.top_k_r[row];
-    const int rank = blockIdx.x - row * a.ctas;
-    const bool valid = set.T >= 0.f && set.T < CUDART_INF_F && set.p > 0.f && set.m >= 0.f && set.m <= 1.f;
     const T *at = static_cast<const T *>(a.logits) + (int64_t)row * a.stride;
-    Row<T> r = {share<T>(at, a.V, rank, a.per), mem, sh, a.ctas, rank, a.V, 0, 0, 0.f, 0.f, 0.f};
+    Row<T> r = {share<T>(at, a.V, rank, a.per), mem, sh, reinterpret_cast<uint64_t *>(mem + a.words), a.list_room, a.ctas, rank, a.V, 0, 0, 0.f, 0.f, 0.f};
     Mass::fill(sh.table);
-    if (!valid) begun_wait(a.ctas);
-    if (!valid || !bring<T>(r, at, mem, a.status)) {
+    if (!bring<T>(r, at, mem, a.status)) {
         if (rank == 0)
-            for (int d = threadIdx.x; d < a.draws; d += kThreads) no_draw(a, row, d, valid ? 0 : DSBD_DEV_BAD_PARAM);
-        return;
-    }
-    if (set.T == 0.f) {
-        uint32_t first = 0x7fffffffu;
-        each<T>(r.s, r.mem, [&](int t, float z) { if (z == r.top) first = min(first, (uint32_t)t); });
-        auto least = [](uint32_t x, uint32_t y) { return min(x, y); };
-        first = over_cta(first, least, reinterpret_cast<uint32_t *>(sh.scratch));
-        const Note *all = r.tell_all({0.0, 0.f, 0.f, first, 0});
-        for (int c = 0; c < a.ctas; ++c) first = min(first, all[c].a);
-        if (rank == 0)
-            for (int d = threadIdx.x; d < a.draws; d += kThreads) {
-                const float u = a.uniform[(int64_t)row * a.draws + d];
-                if (u >= 0.f && u <= 1.f) put_draw(a, row, d, (int)first, 0.0);
-                else no_draw(a, row, d, DSBD_DEV_BAD_PARAM);
-            }
+            for (int d = threadIdx.x; d < a.draws; d += kThreads) no_draw(a, row, d, 0);
         return;
     }
     const Mass mass(set.T, r.top, sh.table);
-    Cut cut = {kKeyMasked, -1};                    // everything above -inf
-    const bool by_rank = set.k > 0 && set.k < a.V;
-    if (by_rank && set.k <= kTop) {
-        const int n = list_top(r, set.k);
-        if (n >= 0) {
-            if (rank == 0) draw_listed(r, a, row, set, n, mass);
-            return;
-        }
+    double whole_mass = 0.0;
+    int n = -1;
+    if (set.k == 0) n = list_mass(r, set.p, set.m, set.T, mass, &whole_mass);
+    else if (set.k <= kTop) n = list_top(r, set.k);
+    if (n >= 0) {
+        if (rank == 0)
+            draw_listed<kThreads, kList>(r.list, r.tmp(), sh.sums, sh.hist[0].count, reinterpret_cast<uint32_t *>(sh.scan), a, row, set, set.k ? min(n, set.k) : n, whole_mass, mass, r.top);
+        return;
     }
+    Cut cut = {kKeyMasked, -1};                    // everything above -inf
     const Whole whole = {mass, (double)(1ull << (30 + __clz(a.V - 1 | 1)))};
-    if (by_rank) cut = cut_at<false>(r, cut, (uint32_t)set.k, 0.0, whole, 2.f * (r.top - r.low));
+    if (set.k) cut = cut_at<false>(r, cut, (uint32_t)set.k, 0.0, whole, 2.f * (r.top - r.low));
     if (set.p < 1.f) cut = cut_at<true>(r, cut, 0, (double)set.p, whole, 64.f * 0.6931472f * set.T);
     draw_shared(r, a, row, set, cut, mass);
+}
+
+// ------------------------------------------------------------------------------------ rows of one pass
+constexpr int kOnce = 256;                         // threads
+constexpr int kOnceResident = 3;                   // CTAs of an SM
+constexpr int kOnceTop = 512;                      // top-k, at most
+constexpr int kShareTop = 128;                     // the same where rows have their own, and CTAs of a row are not chosen by it
+constexpr int kBatches = DSBD_MAX_ROW_BYTES / 2 / 1024 + 16;           // of 1024 tokens, of the longest row (bf16)
+using DrawList = TopList<kOnce, 4, 2048, 1536>;
+
+struct Report {
+    double mass;
+    float top;
+    uint32_t listed;                               // ~0: a NaN or +inf
+};
+
+struct Batches {
+    double upto[kBatches];
+    float top[kBatches];
+};
+
+struct DrawShared {
+    double table[64];
+    Told<Report> told;
+    union {
+        DrawList list;
+        Batches batch;
+    };
+    double sums[kOnce / 32];
+};
+
+// Draws of a row without cuts: each CTA those of its share.
+template <class T>
+__device__ void draw_plain(DrawShared &sh, const SampleArgs &a, int row, int rank, const T *at, const Settings &set) {
+    constexpr int P = kPer<T>, D = kDeep<T>, kBatch = D * kOnce;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x / 32;
+    const Share s = share<T>(at, a.V, rank, a.per);
+    Batches &batch = sh.batch;
+    Mass mass(set.T, 0.f, sh.table);
+    // a warp's batch: its mass and largest logit.  Batches are in the tokens' order: number w0 / kBatch * warps + warp.
+    bool good = true;
+    int batches = 0;
+    for (int w0 = 0; w0 < s.words; w0 += kBatch, batches += kOnce / 32) {
+        float4 raw[D];
+        load_batch<T, kOnce>(raw, at, s, w0);
+        float top = -CUDART_INF_F;
+#pragma unroll
+        for (int u = 0; u < D; ++u) {
+            float x[P];
+            unpack(raw[u], x);
+#pragma unroll
+            for (int e = 0; e < P; ++e) top = max_nan(top, x[e]);
+        }
+        good &= top < CUDART_INF_F;
+        top = warp_most(top < CUDART_INF_F ? top : -CUDART_INF_F);
+        double sum = 0.0;
+        if (top > -CUDART_INF_F) {
+            mass.relative_to(top);
+#pragma unroll
+            for (int u = 0; u < D; ++u) {
+                float x[P];
+                unpack(raw[u], x);
+                double part = 0.0;
+#pragma unroll
+                for (int e = 0; e < P; ++e) part += mass.of(x[e]);
+                sum += part;
+            }
+            sum = warp_sum(sum);
+        }
+        if (lane == 0) {
+            batch.upto[batches + warp] = sum;
+            batch.top[batches + warp] = top;
+        }
+    }
+    good = __syncthreads_and(good);
+    // the share's largest logit, the batches' masses relative to it, and their cumulative sums
+    float top = -CUDART_INF_F;
+    for (int b = lane; b < batches; b += 32) top = fmaxf(top, batch.top[b]);
+    top = warp_most(top);
+    Mass rel = mass;
+    rel.relative_to(top);
+    __syncthreads();
+    for (int b = threadIdx.x; b < batches; b += kOnce) {
+        const double m = batch.upto[b] * rel.of(batch.top[b]);
+        batch.upto[b] = m;
+        if (m == 0.0) batch.top[b] = -CUDART_INF_F;
+    }
+    __syncthreads();
+    if (warp == 0) {
+        const int each = (batches + 31) / 32, b0 = min(lane * each, batches), b1 = min(b0 + each, batches);
+        double sum = 0.0;
+        for (int b = b0; b < b1; ++b) sum += batch.upto[b];
+        double up = sum;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const double x = __shfl_up_sync(kFull, up, o);
+            if (lane >= o) up += x;
+        }
+        sum = __shfl_up_sync(kFull, up, 1);
+        if (lane == 0) sum = 0.0;
+        for (int b = b0; b < b1; ++b) {
+            sum += batch.upto[b];
+            batch.upto[b] = sum;
+        }
+    }
+    __syncthreads();
+    begun_wait(a.ctas);
+    int turn = 0;
+    const double mine = batches ? batch.upto[batches - 1] : 0.0;
+    const Report own = {mine, top, good ? 0u : ~0u};
+    const Report *all = tell(own, sh.told, turn, a.ctas, rank);
+    float most = all[0].top;
+    for (int c = 0; c < a.ctas; ++c) {
+        good &= all[c].listed == 0;
+        most = fmaxf(most, all[c].top);
+    }
+    if (!good || most == -CUDART_INF_F) {
+        if (rank == 0) {
+            for (int d = threadIdx.x; d < a.draws; d += kOnce) no_draw(a, row, d, 0);
+            if (threadIdx.x == 0) report(a.status, good ? DSBD_DEV_EXHAUSTED : DSBD_DEV_BAD_LOGIT);
+        }
+        return;
+    }
+    // where the shares begin and end, by the same roundings in every CTA
+    Mass between = mass;
+    between.relative_to(most);
+    double begin = 0.0, total = 0.0;
+    for (int c = 0; c < a.ctas; ++c) {
+        if (c == rank) begin = total;
+        total = __dadd_rn(total, __dmul_rn(all[c].mass, between.of(all[c].top)));
+    }
+    const double unit = between.of(top), end = __dadd_rn(begin, __dmul_rn(mine, unit));
+    const double log_total = log(total);
+    for (int d = warp; d < a.draws; d += kOnce / 32) {
+        const float u = a.uniform[(int64_t)row * a.draws + d];
+        if (!(u >= 0.f && u <= 1.f)) {
+            if (rank == 0 && lane == 0) no_draw(a, row, d, DSBD_DEV_BAD_PARAM);
+            continue;
+        }
+        const double t = target(u, total);
+        if (!(begin <= t && t < end)) continue;
+        // the first batch that ends beyond t
+        int b = 0;
+        for (int i = lane; i < batches; i += 32) b += __dadd_rn(begin, __dmul_rn(batch.upto[i], unit)) <= t;
+        b = min((int)__reduce_add_sync(kFull, (unsigned)b), batches - 1);
+        if (batch.top[b] == -CUDART_INF_F) {
+            // (t lies within a rounding of the sums before a batch without mass: the last one with some)
+            int before_ = -1, behind = batches;
+            for (int i = lane; i < batches; i += 32)
+                if (batch.top[i] > -CUDART_INF_F) {
+                    if (i < b) before_ = max(before_, i);
+                    else behind = min(behind, i);
+                }
+            before_ = __reduce_max_sync(kFull, before_);
+            behind = __reduce_min_sync(kFull, behind);
+            b = before_ >= 0 ? before_ : behind;
+        }
+        const float from = batch.top[b];
+        mass.relative_to(from);
+        // what is left of t in the batch, relative to its largest logit
+        const double left = ((t - begin) / unit - (b ? batch.upto[b - 1] : 0.0)) / rel.of(from);
+        double done = 0.0;
+        int token = -1;
+        float z = 0.f;
+        const int first = b / (kOnce / 32) * kBatch + b % (kOnce / 32) * D * 32;
+        for (int v = 0; v < D; ++v) {
+            const int w = first + v * 32 + lane;
+            float x[P];
+            unpack(w < s.words ? load_word(at, s, w) : masked_word<T>(), x);
+            double m[P], here = 0.0;
+#pragma unroll
+            for (int e = 0; e < P; ++e) {
+                m[e] = mass.of(x[e]);
+                here += m[e];
+            }
+            double up = here;
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) {
+                const double y = __shfl_up_sync(kFull, up, o);
+                if (lane >= o) up += y;
+            }
+            // the first lane that goes beyond; where rounding lets none, the last one with a mass
+            const unsigned beyond = __ballot_sync(kFull, done + up > left && here > 0.0), some = __ballot_sync(kFull, here > 0.0);
+            if (some) {
+                const int who = beyond ? __ffs(beyond) - 1 : 31 - __clz(some);
+                if (lane == who) {
+                    double c = done + (up - here);
+#pragma unroll
+                    for (int e = 0; e < P; ++e)
+                        if (m[e] != 0.0 && !(c > left)) {
+                            token = s.first + w * P - s.mis + e;
+                            z = x[e];
+                            c += m[e];
+                        }
+                }
+                token = __shfl_sync(kFull, token, who);
+                z = __shfl_sync(kFull, z, who);
+            }
+            if (beyond) break;
+            done += __shfl_sync(kFull, up, 31);
+        }
+        if (lane == 0) put_draw(a, row, d, token, ((double)z - (double)most) / (double)set.T - log_total);
+    }
+}
+
+template <class T>
+__global__ void __launch_bounds__(kOnce, kOnceResident) k_draw(SampleArgs a) {
+    extern __shared__ float4 mem[];
+    DrawShared &sh = *reinterpret_cast<DrawShared *>(mem);
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    const int row = blockIdx.x / a.ctas, rank = blockIdx.x - row * a.ctas;
+    Settings set;
+    const Kind kind = settings_of(a, row, set);
+    if (kind == kCut) return;
+    if (kind == kBad) {
+        if (rank == 0)
+            for (int d = threadIdx.x; d < a.draws; d += kOnce) no_draw(a, row, d, DSBD_DEV_BAD_PARAM);
+        return;
+    }
+    begun_arrive(a.ctas);
+    Mass::fill(sh.table);
+    __syncthreads();
+    const T *at = static_cast<const T *>(a.logits) + (int64_t)row * a.stride;
+    if (kind == kPlain) {
+        draw_plain(sh, a, row, rank, at, set);
+        return;
+    }
+    const uint32_t K = kind == kGreedy ? 1 : (uint32_t)set.k;
+    Rest rest;
+    Sum cleared = {-CUDART_INF_F, 0.0};
+    const bool good = collect<T, false>(sh.list, at, share<T>(at, a.V, rank, a.per), K, a.ctas > 1, 0.f, rest, cleared);
+    begun_wait(a.ctas);
+    int turn = 0;
+    const Report own = {0.0, 0.f, good ? sh.list.listed : ~0u};
+    const Report *all = tell(own, sh.told, turn, a.ctas, rank);
+    bool bad = false;
+    uint64_t n = 0;
+    for (int c = 0; c < a.ctas; ++c) {
+        bad |= all[c].listed == ~0u;
+        n += all[c].listed;
+    }
+    const bool over = n > DrawList::kList;
+    if (rank == 0 && !bad && !over) {
+        uint32_t to = all[0].listed;
+        for (int c = 1; c < a.ctas; ++c) {
+            const uint64_t *from = cg::this_cluster().map_shared_rank(&sh.list.list[0], c);
+            for (uint32_t i = threadIdx.x; i < all[c].listed; i += kOnce) sh.list.list[to + i] = from[i];
+            to += all[c].listed;
+        }
+        if (threadIdx.x == 0) sh.list.listed = to;
+    }
+    cluster_barrier(a.ctas);                       // (rank 0 has the lists)
+    if (rank) return;
+    if (bad || n == 0) {
+        for (int d = threadIdx.x; d < a.draws; d += kOnce) no_draw(a, row, d, 0);
+        if (threadIdx.x == 0) report(a.status, bad ? DSBD_DEV_BAD_LOGIT : DSBD_DEV_EXHAUSTED);
+        return;
+    }
+    if (over) {
+        select_row<T, false>(sh.list, at, a.V, K, 0.f, rest);
+    } else {
+        sh.list.clear<false>(sh.list.entries_bound(K), 0.f, cleared);
+    }
+    sh.list.sort();
+    if (kind == kGreedy) {
+        for (int d = threadIdx.x; d < a.draws; d += kOnce) {
+            const float u = a.uniform[(int64_t)row * a.draws + d];
+            if (u >= 0.f && u <= 1.f) put_draw(a, row, d, token_of(sh.list.list[0]), 0.0);
+            else no_draw(a, row, d, DSBD_DEV_BAD_PARAM);
+        }
+        return;
+    }
+    const float top = logit_of(sh.list.list[0]);
+    const Mass mass(set.T, top, sh.table);
+    draw_listed<kOnce, kOnceTop>(sh.list.list, reinterpret_cast<uint64_t *>(sh.list.hot), sh.sums, sh.list.count, sh.list.scan, a, row, set, min((int)sh.list.listed, set.k), 0.0, mass, top);
+}
+
+// CTAs of a row in k_draw: as many as run at once, none with less than half a batch; lists of up to K entries and a half more from each.
+inline Plan plan_once(const dsbd_rows_t *r, int K) {
+    Plan p;
+    p.ctas = 1;
+    while (p.ctas < kMaxCtas && r->rows * 2 * (int64_t)p.ctas <= 148 * kOnceResident && share_of(r->V, 2 * p.ctas) >= kOnce * 16 &&
+           3 * (int64_t)K * p.ctas <= DrawList::kList)
+        p.ctas *= 2;
+    p.per = share_of(r->V, p.ctas);
+    p.words = 0;
+    return p;
 }
 
 }  // namespace
@@ -588,18 +912,40 @@ extern "C" int dsbd_sample_rows(const dsbd_rows_t *rows, const dsbd_sample_param
     int rc = check_rows(rows);
     if (rc) return rc;
     if (!p || p->draws < 0 || !status) return DSBD_ERR_INVALID_ARG;
-    if (!p->temperature_r && !(p->temperature >= 0.f && p->temperature <= FLT_MAX)) return DSBD_ERR_INVALID_ARG;
+    if (!p->temperature_r && p->temperature != 0.f && !(p->temperature >= kLeastTemperature && p->temperature <= FLT_MAX)) return DSBD_ERR_INVALID_ARG;
     if (!p->top_p_r && !(p->top_p > 0.f)) return DSBD_ERR_INVALID_ARG;
     if (!p->min_p_r && !(p->min_p >= 0.f && p->min_p <= 1.f)) return DSBD_ERR_INVALID_ARG;
     if (rows->rows == 0 || p->draws == 0) return DSBD_OK;
     if (!rows->logits || !uniform || !token) return DSBD_ERR_INVALID_ARG;
-    const Plan plan = plan_for(rows);
     SampleArgs a = {};
-    a.logits = rows->logits; a.stride = rows->row_stride; a.rows = rows->rows; a.V = rows->V; a.draws = p->draws;
-    a.ctas = plan.ctas; a.per = plan.per;
+    a.logits = rows->logits; a.stride = rows->row_stride; a.V = rows->V; a.draws = p->draws;
     a.temperature = p->temperature; a.top_p = p->top_p; a.min_p = p->min_p; a.top_k = p->top_k;
     a.temperature_r = p->temperature_r; a.top_p_r = p->top_p_r; a.min_p_r = p->min_p_r; a.top_k_r = p->top_k_r;
     a.uniform = uniform; a.token = token; a.logp = logp; a.status = status;
-    return rows->dtype == DSBD_DTYPE_F32 ? launch(k_sample<float>, rows->rows, plan, 0, a, stream)
-                                         : launch(k_sample<__nv_bfloat16>, rows->rows, plan, 0, a, stream);
+    a.list_most = p->top_k_r ? kShareTop : kOnceTop;
+    // the kernels that rows of these settings may need; each leaves the other's rows alone
+    const bool k_off = !p->top_k_r && (p->top_k <= 0 || p->top_k >= rows->V), no_cut = p->top_p >= 1.f && p->min_p == 0.f;
+    bool once = true, cut = true;
+    if (!p->temperature_r && p->temperature == 0.f) cut = false;
+    else if (!p->top_k_r && !k_off) (p->top_k <= kOnceTop ? cut : once) = false;
+    else if (k_off && !p->top_p_r && !p->min_p_r) (no_cut ? cut : once) = false;
+    if (!cut || p->temperature_r || p->top_p_r || p->min_p_r) once = true;      // (settings out of range are k_draw's)
+    if (once) {
+        const Plan plan = plan_once(rows, p->top_k_r ? kShareTop : k_off ? 1 : p->top_k < kOnceTop ? p->top_k : kOnceTop);
+        a.ctas = plan.ctas;
+        a.per = plan.per;
+        rc = rows->dtype == DSBD_DTYPE_F32 ? launch<kOnce>(k_draw<float>, rows->rows, plan, sizeof(DrawShared), a, stream)
+                                           : launch<kOnce>(k_draw<__nv_bfloat16>, rows->rows, plan, sizeof(DrawShared), a, stream);
+        if (rc) return rc;
+    }
+    if (!cut) return DSBD_OK;
+    const Plan plan = plan_for(rows);
+    a.ctas = plan.ctas;
+    a.per = plan.per;
+    // the share, where the list is put in order later, and the list; half as long beside the longest shares
+    a.list_room = plan.words <= 160 * 1024 / 16 ? kList : kList / 2;
+    a.words = plan.words > a.list_room / 2 ? plan.words : a.list_room / 2;
+    const size_t bytes = (size_t)a.words * 16 + (size_t)a.list_room * 8;
+    return rows->dtype == DSBD_DTYPE_F32 ? launch(k_draw_cut<float>, rows->rows, plan, bytes, a, stream)
+                                         : launch(k_draw_cut<__nv_bfloat16>, rows->rows, plan, bytes, a, stream);
 }

@@ -90,10 +90,7 @@ __global__ void __launch_bounds__(NT, CTAS) k_top(TopArgs a) {
         select_row<T, true>(sh, at, a.V, (uint32_t)a.K, scale_f, rest);
     } else {
         for (int c = 0; c < a.ctas; ++c) cleared.add(all[c].rest, scale);
-        const float bound = sh.bound((uint32_t)a.K, [&](auto f) {
-            for (int i = threadIdx.x; i < (int)sh.listed; i += NT) f(logit_of(sh.list[i]));
-        });
-        sh.clear(bound, scale_f, cleared);
+        sh.template clear<true>(sh.entries_bound((uint32_t)a.K), scale_f, cleared);
     }
     sh.sort();
     const int kept = min((int)sh.listed, a.K);
@@ -168,6 +165,6 @@ extern "C" int dsbd_top_logits(const dsbd_rows_t *rows, int32_t K, float tempera
     if (K <= 512)
         return rows->dtype == DSBD_DTYPE_F32 ? run_top<float, 256, 4, 2048, 1536, 3>(rows, a, stream)
                                              : run_top<__nv_bfloat16, 256, 4, 2048, 1536, 3>(rows, a, stream);
-    return rows->dtype == DSBD_DTYPE_F32 ? run_top<float, 512, 4, 4096, 3072, 2>(rows, a, stream)
-                                         : run_top<__nv_bfloat16, 512, 4, 4096, 3072, 2>(rows, a, stream);
+    return rows->dtype == DSBD_DTYPE_F32 ? run_top<float, 512, 4, 4096, 2560, 2>(rows, a, stream)
+                                         : run_top<__nv_bfloat16, 512, 4, 4096, 2560, 2>(rows, a, stream);
 }

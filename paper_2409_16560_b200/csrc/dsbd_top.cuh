@@ -38,7 +38,7 @@ struct TopList {
     static constexpr int kWarps_ = NT / 32;
     static constexpr int kEach = LIST / NT;        // entries of a thread
     static constexpr int kTop = NT * G / 2;        // K, at most: half the groups
-    static_assert(kBins % NT == 0 && LIST % NT == 0 && LIST >= 2 * kTop, "");
+    static_assert(kBins % NT == 0 && LIST % NT == 0 && LIST >= 2 * kTop && HOT * sizeof(float4) >= LIST * sizeof(uint64_t), "");
 
     static constexpr int kList = LIST, kHot = HOT;
 
@@ -106,9 +106,17 @@ struct TopList {
         return l;
     }
 
+    // The same of the list's entries.
+    __device__ __forceinline__ float entries_bound(uint32_t K) {
+        return bound(K, [&](auto f) {
+            for (int i = threadIdx.x; i < (int)listed; i += NT) f(logit_of(list[i]));
+        });
+    }
+
     // Clears the list of entries below `least`, whose sum goes to `cleared`, the same in all threads.  The list has its tokens in no order,
     // so the terms are made multiples of 2^-40 of the largest: their sum has no roundings that could depend on one.  All threads,
     // behind a barrier.
+    template <bool REST>
     __device__ __forceinline__ void clear(float least, float scale, Sum &cleared) {
         const uint32_t n = listed, key = key_of(least);
         static_assert(kEach <= 16, "");
@@ -119,7 +127,8 @@ struct TopList {
             e[i] = threadIdx.x + i * NT < n ? list[threadIdx.x + i * NT] : 0;
             if (e[i] && (uint32_t)(e[i] >> 32) < key) h = fmaxf(h, logit_of(e[i]));
         }
-        range(h, l);                               // (barriers)
+        if (REST) range(h, l);                     // (barriers)
+        else __syncthreads();
         if (threadIdx.x == 0) listed = 0;
         __syncthreads();
         double sum = 0.0;
@@ -127,7 +136,11 @@ struct TopList {
         for (int i = 0; i < kEach; ++i) {
             if (e[i] == 0) continue;
             if ((uint32_t)(e[i] >> 32) >= key) list[next_place(&listed)] = e[i];
-            else sum += rint((double)exp2_fast((logit_of(e[i]) - h) * scale) * 0x1p40);
+            else if (REST) sum += rint((double)exp2_fast((logit_of(e[i]) - h) * scale) * 0x1p40);
+        }
+        if (!REST) {
+            __syncthreads();
+            return;
         }
         sum = warp_sum(sum);
         if ((threadIdx.x & 31) == 0) sums[threadIdx.x / 32] = sum;
@@ -139,7 +152,7 @@ struct TopList {
     }
 
     // The kept words' tokens at or above `least` to the list, the others' sum to `cleared` (as in clear).
-    template <class T>
+    template <class T, bool REST>
     __device__ __forceinline__ void flush(float least, float scale, Sum &cleared) {
         constexpr int P = kPer<T>;
         const int n = (int)hots;
@@ -156,6 +169,12 @@ struct TopList {
                     h = fmaxf(h, x[e]);
                 }
             }
+        }
+        if (!REST) {
+            __syncthreads();
+            if (threadIdx.x == 0) hots = 0;
+            __syncthreads();
+            return;
         }
         range(h, l);                               // (barriers)
         const float from = h == -CUDART_INF_F ? 0.f : h;
@@ -190,10 +209,15 @@ struct TopList {
             if (e) list[rank] = e;
             __syncthreads();
         } else {
-            int size = 256;
-            while (size < n) size <<= 1;
-            for (int i = n + threadIdx.x; i < size; i += NT) list[i] = 0;
-            sort_down<NT>(list, size);
+            float h = -CUDART_INF_F, l = CUDART_INF_F;
+            for (int i = threadIdx.x; i < n; i += NT) {
+                const float z = logit_of(list[i]);
+                h = fmaxf(h, z);
+                l = fminf(l, z);
+            }
+            range(h, l);
+            const float scale = bins_over(h - l);
+            order_down<NT, kBins>(list, reinterpret_cast<uint64_t *>(hot), n, count, scan, [&](uint64_t e) { return bin_below(h, logit_of(e), scale); });
         }
     }
 };
@@ -220,8 +244,8 @@ __device__ __forceinline__ bool collect(TopList<NT, G, LIST, HOT> &sh, const T *
             if (threadIdx.x == 0) sh.listed = LIST + 1;
             __syncthreads();
         } else {
-            if (listed > LIST / 2) sh.clear(bound, scale, cleared);
-            sh.template flush<T>(bound, scale, cleared);
+            if (listed > LIST / 2) sh.template clear<REST>(bound, scale, cleared);
+            sh.template flush<T, REST>(bound, scale, cleared);
         }
     };
     int batch = 0, next = 0;
@@ -262,7 +286,7 @@ __device__ __forceinline__ bool collect(TopList<NT, G, LIST, HOT> &sh, const T *
     if (batch > 1) bound = fmaxf(sh.bound(K, groups), -FLT_MAX);
     __syncthreads();
     sort_out();
-    if (trim && sh.listed <= LIST) sh.clear(bound, scale, cleared);
+    if (trim && sh.listed <= LIST) sh.template clear<REST>(bound, scale, cleared);
     bool good = true;
     groups([&](float x) { good &= x < CUDART_INF_F; });
     return __syncthreads_and(good);
