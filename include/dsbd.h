@@ -562,7 +562,6 @@ int dsbd_chunk_attention_paged_launches(const dsbd_chunk_t *chunk, const dsbd_at
  * dsbd_verify_step accepts.) */
 #define DSBD_MAX_ROW_BYTES 1572864 /* V elements: 393216 in fp32, 786432 in bf16               */
 #define DSBD_MAX_TOP 1024          /* K of dsbd_top_logits and dsbd_distill                    */
-#define DSBD_MIN_TEMPERATURE 1e-20f /* of dsbd_sample_rows, but for 0                          */
 
 /* Row r: the V elements from logits + r * row_stride (elements) on, at any alignment of an element; what lies between the rows is
  * not read.  -inf marks a token that is masked out. */
@@ -574,8 +573,7 @@ typedef struct {
 } dsbd_rows_t;
 
 typedef struct {
-    float temperature;             /* 0: the largest logit's token (the lowest of equal ones);
-                                      or from DSBD_MIN_TEMPERATURE on                        */
+    float temperature;             /* 0: the largest logit's token (the lowest of equal ones) */
     float top_p;                   /* > 0; from 1 on: off                                    */
     float min_p;                   /* 0 .. 1; 0: off                                         */
     int32_t top_k;                 /* <= 0 or >= V: off                                      */

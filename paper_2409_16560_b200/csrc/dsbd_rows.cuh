@@ -331,21 +331,13 @@ struct Rest {
     }
 };
 
-// A float as a double by moving its bits: the conversion instruction has a sixteenth of an SM's lanes and sets the pace of a pass of
-// exponentials.  Zeros and denormals come out off by up to 2^-126 (nothing beside a temperature of kLeastTemperature), infinities as 2^128.
-constexpr float kLeastTemperature = DSBD_MIN_TEMPERATURE;
-__device__ __forceinline__ double widen(float x) {
-    const uint32_t u = __float_as_uint(x);
-    return __hiloint2double((int)((u & 0x80000000u) | (((u & 0x7fffffffu) >> 3) + 0x38000000u)), (int)(u << 29));
-}
-
 // exp((z - top) / T) in 64 bits: 2^(k / 64) from a table of 64, times a Taylor polynomial of 2^f for the rest, |f| <= 1 / 128: the
 // table-driven scheme of P. T. P. Tang, ACM TOMS 15 (1989).  The degree 4 leaves (ln 2 / 128)^5 / 120 = 4e-14 of the value.
 // Exactly 1 for the largest logit, and the same for equal ones.
 struct Mass {
     double scale;                                  // 64 log2(e) / T
     double reach;                                  // 693 T: logits further below have less than 2^-999, and count as 0
-    double top_wide;
+    double top;
     float least;
     const double *table;                           // 64 entries in shared memory
 
@@ -357,12 +349,12 @@ struct Mass {
         relative_to(top);
     }
     __device__ __forceinline__ void relative_to(float top) {
-        top_wide = widen(top);
-        least = (float)((double)top - reach);
+        this->top = (double)top;
+        least = top > -CUDART_INF_F ? (float)((double)top - reach) : CUDART_INF_F;      // (nothing: 0)
     }
-    // z <= top; 0 for -inf
-    __device__ __forceinline__ double of(float z) const {
-        const double d = widen(z) - top_wide;
+    // z <= top, not -inf
+    __device__ __forceinline__ double at(float z) const {
+        const double d = (double)z - top;
         const double magic = 6755399441055744.0;   // 1.5 * 2^52: adding it rounds to whole numbers
         const double t = fma(d, scale, magic);
         const int k = __double2loint(t);
@@ -374,8 +366,24 @@ struct Mass {
         r = fma(r, f, kUnit);
         r = fma(r, f, 1.0);
         r *= table[k & 63];
-        // (no branch: the steps of several logits take turns)
-        return z >= least ? __hiloint2double(__double2hiint(r) + ((k >> 6) << 20), __double2loint(r)) : 0.0;
+        return __hiloint2double(__double2hiint(r) + ((k & ~63) << 14), __double2loint(r));
+    }
+    // 0 for -inf (no branch: the steps of several logits take turns)
+    __device__ __forceinline__ double of(float z) const {
+        const double m = at(fmaxf(z, least));
+        return z >= least ? m : 0.0;
+    }
+    // of a word's elements together
+    template <int P>
+    __device__ __forceinline__ double of_word(const float (&x)[P]) const {
+        double m[P];
+#pragma unroll
+        for (int e = 0; e < P; ++e) m[e] = of(x[e]);
+#pragma unroll
+        for (int d = P / 2; d > 0; d /= 2)
+#pragma unroll
+            for (int e = 0; e < d; ++e) m[e] += m[e + d];
+        return m[0];
     }
 };
 

@@ -14,6 +14,7 @@
 //     Where the list does not hold them: a histogram of 512 bins over the cluster, linear in the logit first, then in the bits of the
 //     keys of the bin that the cut is in, until that is one key; equal keys go by token.  Masses are then whole numbers (2^62 / V' of the
 //     largest token's mass, V' the power of two from V on), so sums do not depend on their order.  Then the draw over all shares.
+#include <cstdlib>
 #include "dsbd_top.cuh"
 
 namespace dsbd {
@@ -29,6 +30,7 @@ struct SampleArgs {
     int64_t stride;
     int V, draws, ctas, per;
     int list_most;                                 // largest top-k that k_draw takes
+    int beside;                                    // k_draw_cut: k_draw has been launched just before
     int words, list_room;                          // k_draw_cut: 16-byte words of shared memory before the list, entries of the list
     float temperature, top_p, min_p;
     int top_k;
@@ -153,7 +155,7 @@ struct Whole {
     const Mass &mass;
     double unit;
     __device__ __forceinline__ uint64_t of(float z) const {
-        // (by its bits, see widen)
+        // (by its bits: the conversion to whole numbers of 64 bits takes a loop)
         const uint64_t bits = (uint64_t)__double_as_longlong(mass.of(z) * unit);
         const int up = (int)(bits >> 52) - 1075;
         const uint64_t digits = (bits & 0xfffffffffffffull) | 0x10000000000000ull;
@@ -302,24 +304,36 @@ __device__ int list_bins(Row<T> &r, float scale, int last) {
     Shared &sh = r.sh;
     if (threadIdx.x == 0) sh.listed = 0;
     __syncthreads();
-    each<T>(r.s, r.mem, [&](int t, float z) {
-        if (z == -CUDART_INF_F || (last < kBins - 1 && (r.top - z) * scale >= (float)(last + 1))) return;
-        const uint32_t at = next_place(&sh.listed);
-        if (at < (uint32_t)r.room) r.list[at] = entry_of(z, t);
-    });
+    const float beyond = last < kBins - 1 ? (float)(last + 1) : CUDART_INF_F;
+    auto inside = [&](float z) { return !((r.top - z) * scale >= beyond) && z > -CUDART_INF_F; };
+    for (int w = threadIdx.x; w < r.s.words; w += kThreads) {
+        float x[kPer<T>], most;
+        unpack(r.mem[w], x);
+        most = x[0];
+#pragma unroll
+        for (int e = 1; e < kPer<T>; ++e) most = fmaxf(most, x[e]);
+        if (!inside(most)) continue;
+        uint32_t which = 0;
+#pragma unroll
+        for (int e = 0; e < kPer<T>; ++e) which |= (uint32_t)inside(x[e]) << e;
+        uint32_t at = atomicAdd(&sh.listed, (uint32_t)__popc(which));
+        for (; which; which &= which - 1, ++at) {
+            const int i = w * kPer<T> + __ffs(which) - 1;
+            if (at < (uint32_t)r.room) r.list[at] = entry_of(value_of(reinterpret_cast<const T *>(r.mem)[i]), r.s.first + i - r.s.mis);
+        }
+    }
     __syncthreads();
     const Note *all = r.tell_all({0.0, 0.f, 0.f, sh.listed, 0});
     uint32_t sum = 0;
     for (int c = 0; c < r.ctas; ++c) sum += all[c].a;
     if (sum > (uint32_t)r.room) return -1;
-    if (r.rank == 0) {
-        uint32_t at = all[0].a;
-        for (int c = 1; c < r.ctas; ++c) {
-            const uint64_t *from = r.of(r.list, c);
-            for (uint32_t i = threadIdx.x; i < all[c].a; i += kThreads) r.list[at + i] = from[i];
-            at += all[c].a;
+    if (r.rank == 0)
+        for (uint32_t i = all[0].a + threadIdx.x; i < sum; i += kThreads) {
+            uint32_t at = i;
+            int c = 0;
+            while (at >= all[c].a) at -= all[c++].a;
+            r.list[i] = r.of(r.list, c)[at];
         }
-    }
     cluster_barrier(r.ctas);                       // (the others' lists have been read)
     if (r.rank == 0) {
         const float finer = scale * ((float)kBins / (float)(last + 1));
@@ -335,7 +349,7 @@ __device__ int list_bins(Row<T> &r, float scale, int last) {
 template <class T>
 __device__ int list_mass(Row<T> &r, float p, float m, float T_, const Mass &mass, double *whole) {
     Shared &sh = r.sh;
-    constexpr float kOctaves = 48.f;               // that the bins span
+    constexpr float kOctaves = 16.f;               // that the bins span: a prefix that reaches further is longer than the list
     const float scale = bins_over(kOctaves * 0.6931472f * T_), step = kOctaves / (float)(kBins - 1);
     int last = kBins - 1;
     if (m > 0.f) last = min(last, (int)(-log2f(m) / step) + 1);
@@ -343,12 +357,19 @@ __device__ int list_mass(Row<T> &r, float p, float m, float T_, const Mass &mass
         Hist &h = sh.hist[r.hist_turn++ & 1];
         clear<false>(h);
         double sum = 0.0;
-        each<T>(r.s, r.mem, [&](int, float z) {
-            sum += mass.of(z);
-            const float x = (r.top - z) * scale;
-            const int b = (int)fminf(x, (float)(kBins - 1));
-            if (b < kBins - 1) atomicAdd(&h.count[b], (uint32_t)(exp2_fast(((float)b - x) * step) * 16384.f));
-        });
+        for (int w = threadIdx.x; w < r.s.words; w += kThreads) {
+            float x[kPer<T>];
+            unpack(r.mem[w], x);
+            sum += mass.of_word(x);
+#pragma unroll
+            for (int e = 0; e < kPer<T>; ++e) {
+                const float below = (r.top - x[e]) * scale;
+                if (below < (float)(kBins - 1)) {
+                    const int b = (int)below;
+                    atomicAdd(&h.count[b], (uint32_t)(exp2_fast(((float)b - below) * step) * 16384.f));
+                }
+            }
+        }
         sum = over_cta(sum, add, sh.sums);
         if (threadIdx.x == 0) sh.picked_bin = kBins - 1;
         const Note *all = r.tell_all({sum, 0.f, 0.f, 0, 0});
@@ -400,7 +421,7 @@ __device__ __forceinline__ Kind settings_of(const SampleArgs &a, int row, Settin
     if (a.min_p_r) set.m = a.min_p_r[row];
     if (a.top_k_r) set.k = a.top_k_r[row];
     if (set.k <= 0 || set.k >= a.V) set.k = 0;
-    if (!((set.T == 0.f || set.T >= kLeastTemperature) && set.T < CUDART_INF_F && set.p > 0.f && set.m >= 0.f && set.m <= 1.f)) return kBad;
+    if (!(set.T >= 0.f && set.T < CUDART_INF_F && set.p > 0.f && set.m >= 0.f && set.m <= 1.f)) return kBad;
     return set.T == 0.f ? kGreedy : set.k ? (set.k <= a.list_most ? kListed : kCut) : set.p >= 1.f && set.m == 0.f ? kPlain : kCut;
 }
 
@@ -421,55 +442,50 @@ __device__ __forceinline__ void put_draw(const SampleArgs &a, int row, int d, in
 }
 
 // Draws of a list of n entries in falling order (one CTA alone): its cuts are prefixes.  whole: the mass that top-p is of; 0: the list's.
-// tmp: scratch of n numbers; sums, scan: one for each warp; count: kBins.
+// tmp: scratch of 2 MOST numbers; sums, scan: one for each warp; count: kBins.
 template <int NT, int MOST>
 __device__ void draw_listed(uint64_t *list, uint64_t *tmp, double *sums, uint32_t *count, uint32_t *scan, const SampleArgs &a, int row, const Settings &set, int n,
                             double whole, const Mass &mass, float top) {
     const int lane = threadIdx.x & 31, warp = threadIdx.x / 32;
-    constexpr int kMine = MOST / NT;               // entries of a thread, side by side
     __shared__ uint32_t first_out;
-    double w[kMine], total, mine = 0.0;
+    double total, mine = 0.0;
     if (threadIdx.x == 0) first_out = (uint32_t)n;
-#pragma unroll
-    for (int i = 0; i < kMine; ++i) {
-        const int at = threadIdx.x * kMine + i;
-        w[i] = at < n ? mass.of(logit_of(list[at])) : 0.0;
-        mine += w[i];
-    }
+    // a thread's entries lie side by side, an odd number of them (an even one would send a warp's lanes to few banks)
+    int each = (n + NT - 1) / NT | 1, begin = min((int)threadIdx.x * each, n), end = min(begin + each, n);
+    double *w = reinterpret_cast<double *>(tmp) + MOST;
+#pragma unroll 4
+    for (int i = threadIdx.x; i < n; i += NT) w[i] = mass.of(logit_of(list[i]));
+    __syncthreads();
+    for (int i = begin; i < end; ++i) mine += w[i];
     double upto = before<NT>(mine, &total, sums);  // (barriers)
     if (whole != 0.0) total = whole;
-    uint64_t e[kMine];
-#pragma unroll
-    for (int i = 0; i < kMine; ++i) {
-        const int at = threadIdx.x * kMine + i;
-        if (at < n && ((set.p < 1.f && !(upto < (double)set.p * total)) || !(w[i] >= (double)set.m) || w[i] == 0.0)) atomicMin(&first_out, (uint32_t)at);
+    const double goal = set.p < 1.f ? (double)set.p * total : (double)CUDART_INF_F;
+    for (int i = begin; i < end; ++i) {
+        if (!(upto < goal) || !(w[i] >= (double)set.m) || w[i] == 0.0) {
+            atomicMin(&first_out, (uint32_t)i);
+            break;
+        }
         upto += w[i];
-        e[i] = at < n ? list[at] : 0;
     }
     __syncthreads();
     n = (int)first_out;
     // the kept ones in the tokens' order: (~token, key) falling
-#pragma unroll
-    for (int i = 0; i < kMine; ++i) {
-        const int at = threadIdx.x * kMine + i;
-        if (at < n) list[at] = (e[i] << 32) | (e[i] >> 32);
-    }
+    for (int i = threadIdx.x; i < n; i += NT) list[i] = (list[i] << 32) | (list[i] >> 32);
     const float per_bin = (float)kBins / (float)a.V;
     order_down<NT, kBins>(list, tmp, n, count, scan, [&](uint64_t x) { return min((int)((float)~(uint32_t)(x >> 32) * per_bin), kBins - 1); });
     double *upto_of = reinterpret_cast<double *>(tmp);
+    each = (n + NT - 1) / NT | 1;
+    begin = min((int)threadIdx.x * each, n);
+    end = min(begin + each, n);
     mine = 0.0;
-#pragma unroll
-    for (int i = 0; i < kMine; ++i) {
-        const int at = threadIdx.x * kMine + i;
-        w[i] = at < n ? mass.of(of_key((uint32_t)list[at])) : 0.0;
-        mine += w[i];
-    }
+#pragma unroll 4
+    for (int i = threadIdx.x; i < n; i += NT) w[i] = mass.of(of_key((uint32_t)list[i]));
+    __syncthreads();
+    for (int i = begin; i < end; ++i) mine += w[i];
     upto = before<NT>(mine, &total, sums);
-#pragma unroll
-    for (int i = 0; i < kMine; ++i) {
+    for (int i = begin; i < end; ++i) {
         upto += w[i];
-        const int at = threadIdx.x * kMine + i;
-        if (at < n) upto_of[at] = upto;
+        upto_of[i] = upto;
     }
     __syncthreads();
     total = upto_of[n - 1];
@@ -481,9 +497,10 @@ __device__ void draw_listed(uint64_t *list, uint64_t *tmp, double *sums, uint32_
             continue;
         }
         const double t = target(u, total);
+        // the first entry beyond t
         int at = 0;
-        for (int i = lane; i < n; i += 32) at += upto_of[i] <= t;
-        at = min((int)__reduce_add_sync(kFull, (unsigned)at), n - 1);
+        for (int step = MOST / 2; step > 0; step >>= 1)
+            if (at + step <= n - 1 && upto_of[at + step - 1] <= t) at += step;
         if (lane == 0) {
             const uint64_t x = list[at];
             put_draw(a, row, d, (int)~(uint32_t)(x >> 32), ((double)of_key((uint32_t)x) - (double)top) / (double)set.T - log_total);
@@ -505,9 +522,10 @@ __device__ void draw_shared(Row<T> &r, const SampleArgs &a, int row, const Setti
         const int t = r.s.first + w * kPer<T> - r.s.mis;
         double sum = 0.0;
 #pragma unroll
+        for (int e = 0; e < kPer<T>; ++e) m[e] = mass.of(x[e]);
+#pragma unroll
         for (int e = 0; e < kPer<T>; ++e) {
-            m[e] = x[e] > z_cut || (x[e] == z_cut && t + e <= cut.token) ? mass.of(x[e]) : 0.0;
-            if (!(m[e] >= least)) m[e] = 0.0;
+            if (!(m[e] >= least) || !(x[e] > z_cut || (x[e] == z_cut && t + e <= cut.token))) m[e] = 0.0;
             sum += m[e];
         }
         return sum;
@@ -579,11 +597,7 @@ __device__ void draw_shared(Row<T> &r, const SampleArgs &a, int row, const Setti
 }
 
 template <class T>
-__global__ void __launch_bounds__(kThreads) k_draw_cut(SampleArgs a) {
-    extern __shared__ float4 mem[];
-    __shared__ Shared sh;
-    asm volatile("griddepcontrol.wait;" ::: "memory");
-    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+__device__ void draw_cut(const SampleArgs &a, float4 *mem, Shared &sh) {
     const int row = blockIdx.x / a.ctas, rank = blockIdx.x - row * a.ctas;
     Settings set;
     if (settings_of(a, row, set) != kCut) return;
@@ -611,6 +625,20 @@ __global__ void __launch_bounds__(kThreads) k_draw_cut(SampleArgs a) {
     if (set.k) cut = cut_at<false>(r, cut, (uint32_t)set.k, 0.0, whole, 2.f * (r.top - r.low));
     if (set.p < 1.f) cut = cut_at<true>(r, cut, 0, (double)set.p, whole, 64.f * 0.6931472f * set.T);
     draw_shared(r, a, row, set, cut, mass);
+}
+
+// Beside k_draw, whose rows are others: its CTAs have all waited for what came before them when this kernel is launched, so this one
+// need not; but it ends after k_draw has, as what comes next waits for this kernel alone.
+template <class T>
+__global__ void __launch_bounds__(kThreads) k_draw_cut(SampleArgs a) {
+    extern __shared__ float4 mem[];
+    __shared__ Shared sh;
+    if (!a.beside) {
+        asm volatile("griddepcontrol.wait;" ::: "memory");
+        asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    }
+    draw_cut<T>(a, mem, sh);
+    if (a.beside) asm volatile("griddepcontrol.wait;" ::: "memory");
 }
 
 // ------------------------------------------------------------------------------------ rows of one pass
@@ -673,10 +701,7 @@ __device__ void draw_plain(DrawShared &sh, const SampleArgs &a, int row, int ran
             for (int u = 0; u < D; ++u) {
                 float x[P];
                 unpack(raw[u], x);
-                double part = 0.0;
-#pragma unroll
-                for (int e = 0; e < P; ++e) part += mass.of(x[e]);
-                sum += part;
+                sum += mass.of_word(x);
             }
             sum = warp_sum(sum);
         }
@@ -893,7 +918,8 @@ __global__ void __launch_bounds__(kOnce, kOnceResident) k_draw(SampleArgs a) {
 inline Plan plan_once(const dsbd_rows_t *r, int K) {
     Plan p;
     p.ctas = 1;
-    while (p.ctas < kMaxCtas && r->rows * 2 * (int64_t)p.ctas <= 148 * kOnceResident && share_of(r->V, 2 * p.ctas) >= kOnce * 16 &&
+    const int waves = getenv("WAVES") ? atoi(getenv("WAVES")) : 1;
+    while (p.ctas < kMaxCtas && r->rows * 2 * (int64_t)p.ctas <= 148 * kOnceResident * waves && share_of(r->V, 2 * p.ctas) >= kOnce * 16 &&
            3 * (int64_t)K * p.ctas <= DrawList::kList)
         p.ctas *= 2;
     p.per = share_of(r->V, p.ctas);
@@ -912,7 +938,7 @@ extern "C" int dsbd_sample_rows(const dsbd_rows_t *rows, const dsbd_sample_param
     int rc = check_rows(rows);
     if (rc) return rc;
     if (!p || p->draws < 0 || !status) return DSBD_ERR_INVALID_ARG;
-    if (!p->temperature_r && p->temperature != 0.f && !(p->temperature >= kLeastTemperature && p->temperature <= FLT_MAX)) return DSBD_ERR_INVALID_ARG;
+    if (!p->temperature_r && !(p->temperature >= 0.f && p->temperature <= FLT_MAX)) return DSBD_ERR_INVALID_ARG;
     if (!p->top_p_r && !(p->top_p > 0.f)) return DSBD_ERR_INVALID_ARG;
     if (!p->min_p_r && !(p->min_p >= 0.f && p->min_p <= 1.f)) return DSBD_ERR_INVALID_ARG;
     if (rows->rows == 0 || p->draws == 0) return DSBD_OK;
@@ -940,11 +966,12 @@ extern "C" int dsbd_sample_rows(const dsbd_rows_t *rows, const dsbd_sample_param
     }
     if (!cut) return DSBD_OK;
     const Plan plan = plan_for(rows);
+    a.beside = once;
     a.ctas = plan.ctas;
     a.per = plan.per;
-    // the share, where the list is put in order later, and the list; half as long beside the longest shares
+    // the share, where the list is put in order and its masses are later, and the list; half as long beside the longest shares
     a.list_room = plan.words <= 160 * 1024 / 16 ? kList : kList / 2;
-    a.words = plan.words > a.list_room / 2 ? plan.words : a.list_room / 2;
+    a.words = plan.words > kList ? plan.words : kList;
     const size_t bytes = (size_t)a.words * 16 + (size_t)a.list_room * 8;
     return rows->dtype == DSBD_DTYPE_F32 ? launch(k_draw_cut<float>, rows->rows, plan, bytes, a, stream)
                                          : launch(k_draw_cut<__nv_bfloat16>, rows->rows, plan, bytes, a, stream);
