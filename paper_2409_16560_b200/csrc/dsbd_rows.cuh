@@ -524,6 +524,21 @@ inline Plan plan_for(const dsbd_rows_t *r) {
     return p;
 }
 
+// CTAs of a row for a kernel of which `slots` CTAs run at once: what takes least time, the CTAs in waves of that many, a CTA's time
+// its share and what it does besides, `fixed` elements' worth.  No share below `least` elements.
+inline Plan plan_waves(const dsbd_rows_t *r, int slots, int fixed, int least, int most) {
+    Plan p = {1, 0, 0};
+    int64_t best = INT64_MAX;
+    for (int ctas = 1; ctas <= most && (ctas == 1 || share_of(r->V, ctas) >= least); ctas *= 2) {
+        const int64_t time = (r->rows * (int64_t)ctas + slots - 1) / slots * (share_of(r->V, ctas) + fixed);
+        if (time >= best) continue;
+        best = time;
+        p.ctas = ctas;
+    }
+    p.per = share_of(r->V, p.ctas);
+    return p;
+}
+
 template <int NT = kThreads, class Args>
 int launch(void (*kernel)(Args), int rows, const Plan &p, size_t bytes, const Args &a, dsbd_stream_t stream) {
     if (bytes > 16 * 1024 && cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes) != cudaSuccess) {

@@ -14,7 +14,6 @@
 //     Where the list does not hold them: a histogram of 512 bins over the cluster, linear in the logit first, then in the bits of the
 //     keys of the bin that the cut is in, until that is one key; equal keys go by token.  Masses are then whole numbers (2^62 / V' of the
 //     largest token's mass, V' the power of two from V on), so sums do not depend on their order.  Then the draw over all shares.
-#include <cstdlib>
 #include "dsbd_top.cuh"
 
 namespace dsbd {
@@ -61,7 +60,6 @@ struct Shared {
     uint64_t scan[kWarps];
     uint64_t picked_before;
     uint32_t picked_bin, picked_count;
-    uint32_t listed;
     int found;
 };
 
@@ -297,49 +295,68 @@ __device__ Cut cut_at(Row<T> &r, Cut within, uint32_t k, double p, const Whole &
     }
 }
 
-// The tokens of the bins up to `last` below the row's largest logit, as (key, ~token) in falling order, in the list of rank 0; returns
-// their number there, and -1 everywhere if the list does not hold them.
+// The tokens of the bins up to `last` below the row's largest logit, as (key, ~token) in the tokens' order, in the list of rank 0;
+// returns their number, and -1 if the list does not hold them.
 template <class T>
 __device__ int list_bins(Row<T> &r, float scale, int last) {
     Shared &sh = r.sh;
-    if (threadIdx.x == 0) sh.listed = 0;
-    __syncthreads();
+    const int lane = threadIdx.x & 31, warp = threadIdx.x / 32, each_warp = r.warp_words();
+    const int w0 = warp * each_warp, w1 = min(w0 + each_warp, r.s.words);
     const float beyond = last < kBins - 1 ? (float)(last + 1) : CUDART_INF_F;
     auto inside = [&](float z) { return !((r.top - z) * scale >= beyond) && z > -CUDART_INF_F; };
-    for (int w = threadIdx.x; w < r.s.words; w += kThreads) {
-        float x[kPer<T>], most;
-        unpack(r.mem[w], x);
-        most = x[0];
-#pragma unroll
-        for (int e = 1; e < kPer<T>; ++e) most = fmaxf(most, x[e]);
-        if (!inside(most)) continue;
+    auto marks = [&](int w) {
         uint32_t which = 0;
+        if (w < w1) {
+            float x[kPer<T>];
+            unpack(r.mem[w], x);
 #pragma unroll
-        for (int e = 0; e < kPer<T>; ++e) which |= (uint32_t)inside(x[e]) << e;
-        uint32_t at = atomicAdd(&sh.listed, (uint32_t)__popc(which));
-        for (; which; which &= which - 1, ++at) {
-            const int i = w * kPer<T> + __ffs(which) - 1;
-            if (at < (uint32_t)r.room) r.list[at] = entry_of(value_of(reinterpret_cast<const T *>(r.mem)[i]), r.s.first + i - r.s.mis);
+            for (int e = 0; e < kPer<T>; ++e) which |= (uint32_t)inside(x[e]) << e;
         }
-    }
+        return which;
+    };
+    // how many each warp's words have, then each entry at its place
+    uint32_t mine = 0;
+    for (int w = w0 + lane; w < w1; w += 32) mine += __popc(marks(w));
+    mine = __reduce_add_sync(kFull, mine);
     __syncthreads();
-    const Note *all = r.tell_all({0.0, 0.f, 0.f, sh.listed, 0});
+    if (lane == 0) sh.scan[warp] = mine;
+    __syncthreads();
+    uint32_t at = 0, listed = 0;
+#pragma unroll
+    for (int w = 0; w < kWarps; ++w) {
+        at += w < warp ? (uint32_t)sh.scan[w] : 0;
+        listed += (uint32_t)sh.scan[w];
+    }
+    if (mine && listed <= (uint32_t)r.room)
+        for (int w = w0; w < w1; w += 32) {
+            uint32_t which = marks(w + lane);
+            if (!__any_sync(kFull, which != 0)) continue;
+            const uint32_t here = __popc(which);
+            uint32_t up = here;
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) {
+                const uint32_t x = __shfl_up_sync(kFull, up, o);
+                if (lane >= o) up += x;
+            }
+            for (uint32_t to = at + up - here; which; which &= which - 1, ++to) {
+                const int i = (w + lane) * kPer<T> + __ffs(which) - 1;
+                r.list[to] = entry_of(value_of(reinterpret_cast<const T *>(r.mem)[i]), r.s.first + i - r.s.mis);
+            }
+            at += __shfl_sync(kFull, up, 31);
+        }
+    __syncthreads();
+    const Note *all = r.tell_all({0.0, 0.f, 0.f, listed, 0});
     uint32_t sum = 0;
     for (int c = 0; c < r.ctas; ++c) sum += all[c].a;
     if (sum > (uint32_t)r.room) return -1;
     if (r.rank == 0)
         for (uint32_t i = all[0].a + threadIdx.x; i < sum; i += kThreads) {
-            uint32_t at = i;
+            uint32_t from = i;
             int c = 0;
-            while (at >= all[c].a) at -= all[c++].a;
-            r.list[i] = r.of(r.list, c)[at];
+            while (from >= all[c].a) from -= all[c++].a;
+            r.list[i] = r.of(r.list, c)[from];
         }
     cluster_barrier(r.ctas);                       // (the others' lists have been read)
-    if (r.rank == 0) {
-        const float finer = scale * ((float)kBins / (float)(last + 1));
-        order_down<kThreads, kBins>(r.list, r.tmp(), (int)sum, sh.hist[0].count, reinterpret_cast<uint32_t *>(sh.scan),
-                                    [&](uint64_t e) { return bin_below(r.top, logit_of(e), finer); });
-    }
     return (int)sum;
 }
 
@@ -347,7 +364,7 @@ __device__ int list_bins(Row<T> &r, float scale, int last) {
 // list_bins; *whole: the row's mass (p < 1).  A bin's mass is summed in steps of 2^-14 of its largest, rounded down: what is found to have p of the whole
 // has it, and the list is exact.
 template <class T>
-__device__ int list_mass(Row<T> &r, float p, float m, float T_, const Mass &mass, double *whole) {
+__device__ int list_mass(Row<T> &r, float p, float m, float T_, const Mass &mass, double *whole, float *finer) {
     Shared &sh = r.sh;
     constexpr float kOctaves = 16.f;               // that the bins span: a prefix that reaches further is longer than the list
     const float scale = bins_over(kOctaves * 0.6931472f * T_), step = kOctaves / (float)(kBins - 1);
@@ -384,13 +401,13 @@ __device__ int list_mass(Row<T> &r, float p, float m, float T_, const Mass &mass
         __syncthreads();
         last = min(last, (int)sh.picked_bin);
     }
+    *finer = scale * ((float)kBins / (float)(last + 1));
     return list_bins(r, scale, last);
 }
 
-// The tokens at or above the k-th largest logit, as (key, ~token) in falling order, in the list of rank 0; returns their
-// number there, and -1 everywhere if the list does not hold them.  k <= kTop; fewer than k where the row has fewer above -inf.
+// The tokens at or above the k-th largest logit, listed as in list_bins.  k <= kTop; fewer than k where the row has fewer above -inf.
 template <class T>
-__device__ int list_top(Row<T> &r, int k) {
+__device__ int list_top(Row<T> &r, int k, float *finer) {
     Shared &sh = r.sh;
     const float scale = bins_over(r.top - r.low);
     Hist &h = sh.hist[r.hist_turn++ & 1];
@@ -403,6 +420,7 @@ __device__ int list_top(Row<T> &r, int k) {
     if (excl < (uint64_t)k && excl + n >= (uint64_t)k) sh.picked_bin = threadIdx.x;
     __syncthreads();
     const int last = (int)sh.picked_bin;
+    *finer = scale * ((float)kBins / (float)(last + 1));
     return list_bins(r, scale, last);
 }
 
@@ -441,21 +459,27 @@ __device__ __forceinline__ void put_draw(const SampleArgs &a, int row, int d, in
     if (a.logp) a.logp[(int64_t)row * a.draws + d] = (float)logp;
 }
 
-// Draws of a list of n entries in falling order (one CTA alone): its cuts are prefixes.  whole: the mass that top-p is of; 0: the list's.
-// tmp: scratch of 2 MOST numbers; sums, scan: one for each warp; count: kBins.
+// Draws of a list of n entries in the tokens' order that has the k largest, or all that can be kept (one CTA alone).  whole: the mass that
+// top-p is of; 0: the k largest entries'.  room: 2 MOST numbers; sums, scan: one for each warp; count: kBins; scale: of bins below top that
+// hold the list's logits.
 template <int NT, int MOST>
-__device__ void draw_listed(uint64_t *list, uint64_t *tmp, double *sums, uint32_t *count, uint32_t *scan, const SampleArgs &a, int row, const Settings &set, int n,
-                            double whole, const Mass &mass, float top) {
+__device__ void draw_listed(const uint64_t *list, uint64_t *room, double *sums, uint32_t *count, uint32_t *scan, const SampleArgs &a, int row,
+                            const Settings &set, int n, double whole, const Mass &mass, float top, float scale) {
     const int lane = threadIdx.x & 31, warp = threadIdx.x / 32;
     __shared__ uint32_t first_out;
-    double total, mine = 0.0;
-    if (threadIdx.x == 0) first_out = (uint32_t)n;
-    // a thread's entries lie side by side, an odd number of them (an even one would send a warp's lanes to few banks)
-    int each = (n + NT - 1) / NT | 1, begin = min((int)threadIdx.x * each, n), end = min(begin + each, n);
-    double *w = reinterpret_cast<double *>(tmp) + MOST;
+    uint64_t *down = room, *tmp = room + MOST;
+    // ---- in falling order: what is kept is a prefix, so everything from an entry on
+    for (int i = threadIdx.x; i < n; i += NT) down[i] = list[i];
+    order_down<NT, kBins>(down, tmp, n, count, scan, [&](uint64_t e) { return bin_below(top, logit_of(e), scale); });
+    const int most = set.k ? min(n, set.k) : n;
+    if (threadIdx.x == 0) first_out = (uint32_t)most;
+    double *w = reinterpret_cast<double *>(tmp);
 #pragma unroll 4
-    for (int i = threadIdx.x; i < n; i += NT) w[i] = mass.of(logit_of(list[i]));
+    for (int i = threadIdx.x; i < most; i += NT) w[i] = mass.of(logit_of(down[i]));
     __syncthreads();
+    // a thread's entries lie side by side, an odd number of them (an even one would send a warp's lanes to few banks)
+    int each = (most + NT - 1) / NT | 1, begin = min((int)threadIdx.x * each, most), end = min(begin + each, most);
+    double total, mine = 0.0;
     for (int i = begin; i < end; ++i) mine += w[i];
     double upto = before<NT>(mine, &total, sums);  // (barriers)
     if (whole != 0.0) total = whole;
@@ -468,21 +492,18 @@ __device__ void draw_listed(uint64_t *list, uint64_t *tmp, double *sums, uint32_
         upto += w[i];
     }
     __syncthreads();
-    n = (int)first_out;
-    // the kept ones in the tokens' order: (~token, key) falling
-    for (int i = threadIdx.x; i < n; i += NT) list[i] = (list[i] << 32) | (list[i] >> 32);
-    const float per_bin = (float)kBins / (float)a.V;
-    order_down<NT, kBins>(list, tmp, n, count, scan, [&](uint64_t x) { return min((int)((float)~(uint32_t)(x >> 32) * per_bin), kBins - 1); });
-    double *upto_of = reinterpret_cast<double *>(tmp);
+    const uint64_t least = down[first_out - 1];
+    // ---- in the tokens' order: cumulative masses of what is kept
+#pragma unroll 4
+    for (int i = threadIdx.x; i < n; i += NT) w[i] = list[i] >= least ? mass.of(logit_of(list[i])) : 0.0;
+    __syncthreads();
     each = (n + NT - 1) / NT | 1;
     begin = min((int)threadIdx.x * each, n);
     end = min(begin + each, n);
     mine = 0.0;
-#pragma unroll 4
-    for (int i = threadIdx.x; i < n; i += NT) w[i] = mass.of(of_key((uint32_t)list[i]));
-    __syncthreads();
     for (int i = begin; i < end; ++i) mine += w[i];
     upto = before<NT>(mine, &total, sums);
+    double *upto_of = reinterpret_cast<double *>(room);
     for (int i = begin; i < end; ++i) {
         upto += w[i];
         upto_of[i] = upto;
@@ -497,13 +518,16 @@ __device__ void draw_listed(uint64_t *list, uint64_t *tmp, double *sums, uint32_
             continue;
         }
         const double t = target(u, total);
-        // the first entry beyond t
+        // the first entry beyond t, of those kept
         int at = 0;
         for (int step = MOST / 2; step > 0; step >>= 1)
             if (at + step <= n - 1 && upto_of[at + step - 1] <= t) at += step;
         if (lane == 0) {
-            const uint64_t x = list[at];
-            put_draw(a, row, d, (int)~(uint32_t)(x >> 32), ((double)of_key((uint32_t)x) - (double)top) / (double)set.T - log_total);
+            int back = at;
+            while (back >= 0 && list[back] < least) --back;         // (within a rounding of the sums)
+            while (back < 0 && list[at] < least) ++at;
+            const uint64_t x = list[back >= 0 ? back : at];
+            put_draw(a, row, d, token_of(x), ((double)logit_of(x) - (double)top) / (double)set.T - log_total);
         }
     }
 }
@@ -613,11 +637,13 @@ __device__ void draw_cut(const SampleArgs &a, float4 *mem, Shared &sh) {
     const Mass mass(set.T, r.top, sh.table);
     double whole_mass = 0.0;
     int n = -1;
-    if (set.k == 0) n = list_mass(r, set.p, set.m, set.T, mass, &whole_mass);
-    else if (set.k <= kTop) n = list_top(r, set.k);
+    float finer = 0.f;                             // scale of bins that hold the list's logits alone
+    if (set.k == 0) n = list_mass(r, set.p, set.m, set.T, mass, &whole_mass, &finer);
+    else if (set.k <= kTop) n = list_top(r, set.k, &finer);
     if (n >= 0) {
         if (rank == 0)
-            draw_listed<kThreads, kList>(r.list, r.tmp(), sh.sums, sh.hist[0].count, reinterpret_cast<uint32_t *>(sh.scan), a, row, set, set.k ? min(n, set.k) : n, whole_mass, mass, r.top);
+            draw_listed<kThreads, kList>(r.list, r.tmp(), sh.sums, sh.hist[0].count, reinterpret_cast<uint32_t *>(sh.scan), a, row, set, n,
+                                         whole_mass, mass, r.top, finer);
         return;
     }
     Cut cut = {kKeyMasked, -1};                    // everything above -inf
@@ -841,6 +867,64 @@ __device__ void draw_plain(DrawShared &sh, const SampleArgs &a, int row, int ran
     }
 }
 
+// Draws of a list that has the k largest (in no order), one CTA alone.
+__device__ void draw_few(DrawShared &sh, const SampleArgs &a, int row, const Settings &set) {
+    DrawList &list = sh.list;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x / 32, n = (int)list.listed;
+    list.sort();
+    const float top = logit_of(list.list[0]);
+    const Mass mass(set.T, top, sh.table);
+    if (set.k > 32) {
+        // in the tokens' order, as draw_listed wants them
+        uint64_t *by_token = reinterpret_cast<uint64_t *>(list.hot), *tmp = by_token + kOnceTop;
+        const int kept = min(n, set.k);
+        for (int i = threadIdx.x; i < kept; i += kOnce) by_token[i] = (list.list[i] << 32) | (list.list[i] >> 32);
+        const float per_bin = (float)kBins / (float)a.V, low = logit_of(list.list[kept - 1]);
+        order_down<kOnce, kBins>(by_token, tmp, kept, list.count, list.scan,
+                                 [&](uint64_t x) { return min((int)((float)~(uint32_t)(x >> 32) * per_bin), kBins - 1); });
+        for (int i = threadIdx.x; i < kept; i += kOnce) list.list[i] = (by_token[i] << 32) | (by_token[i] >> 32);
+        draw_listed<kOnce, kOnceTop>(list.list, by_token, sh.sums, list.count, list.scan, a, row, set, kept, 0.0, mass, top, bins_over(top - low));
+        return;
+    }
+    // an entry to a lane; the warps share the draws
+    const int kept = min(n, set.k);
+    const uint64_t mine = lane < kept ? list.list[lane] : 0;
+    double w = lane < kept ? mass.of(logit_of(mine)) : 0.0, upto = w;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const double x = __shfl_up_sync(kFull, upto, o);
+        if (lane >= o) upto += x;
+    }
+    double below = __shfl_up_sync(kFull, upto, 1), total = __shfl_sync(kFull, upto, 31);
+    if (lane == 0) below = 0.0;
+    const bool out = lane >= kept || (set.p < 1.f && !(below < (double)set.p * total)) || !(w >= (double)set.m) || w == 0.0;
+    const unsigned cut = __ballot_sync(kFull, out);
+    const int in = cut ? __ffs(cut) - 1 : 32;
+    if (lane >= in) w = 0.0;
+    const uint32_t token = lane < in ? (uint32_t)token_of(mine) : 0x7fffffffu;
+    // cumulative masses in the tokens' order
+    upto = 0.0;
+    total = 0.0;
+    for (int j = 0; j < in; ++j) {
+        const double x = __shfl_sync(kFull, w, j);
+        upto += __shfl_sync(kFull, token, j) <= token ? x : 0.0;
+        total += x;
+    }
+    // (by another order of additions the last sum may differ from the whole in its last bit)
+    const uint32_t last = __reduce_max_sync(kFull, lane < in ? token : 0u);
+    const double log_total = log(total);
+    for (int d = warp; d < a.draws; d += kOnce / 32) {
+        const float u = a.uniform[(int64_t)row * a.draws + d];
+        if (!(u >= 0.f && u <= 1.f)) {
+            if (lane == 0) no_draw(a, row, d, DSBD_DEV_BAD_PARAM);
+            continue;
+        }
+        const double t = target(u, total);
+        const uint32_t found = __reduce_min_sync(kFull, lane < in && (upto > t || token == last) ? token : 0x7fffffffu);
+        if (lane < in && token == found) put_draw(a, row, d, (int)token, ((double)logit_of(mine) - (double)top) / (double)set.T - log_total);
+    }
+}
+
 template <class T>
 __global__ void __launch_bounds__(kOnce, kOnceResident) k_draw(SampleArgs a) {
     extern __shared__ float4 mem[];
@@ -900,31 +984,31 @@ __global__ void __launch_bounds__(kOnce, kOnceResident) k_draw(SampleArgs a) {
     } else {
         sh.list.clear<false>(sh.list.entries_bound(K), 0.f, cleared);
     }
-    sh.list.sort();
     if (kind == kGreedy) {
-        for (int d = threadIdx.x; d < a.draws; d += kOnce) {
-            const float u = a.uniform[(int64_t)row * a.draws + d];
-            if (u >= 0.f && u <= 1.f) put_draw(a, row, d, token_of(sh.list.list[0]), 0.0);
-            else no_draw(a, row, d, DSBD_DEV_BAD_PARAM);
+        if (threadIdx.x < 32) {
+            uint64_t best = 0;
+            for (int i = threadIdx.x; i < (int)sh.list.listed; i += 32) best = sh.list.list[i] > best ? sh.list.list[i] : best;
+#pragma unroll
+            for (int o = 16; o > 0; o >>= 1) {
+                const uint64_t x = __shfl_xor_sync(kFull, best, o);
+                best = x > best ? x : best;
+            }
+            for (int d = threadIdx.x; d < a.draws; d += 32) {
+                const float u = a.uniform[(int64_t)row * a.draws + d];
+                if (u >= 0.f && u <= 1.f) put_draw(a, row, d, token_of(best), 0.0);
+                else no_draw(a, row, d, DSBD_DEV_BAD_PARAM);
+            }
         }
         return;
     }
-    const float top = logit_of(sh.list.list[0]);
-    const Mass mass(set.T, top, sh.table);
-    draw_listed<kOnce, kOnceTop>(sh.list.list, reinterpret_cast<uint64_t *>(sh.list.hot), sh.sums, sh.list.count, sh.list.scan, a, row, set, min((int)sh.list.listed, set.k), 0.0, mass, top);
+    draw_few(sh, a, row, set);
 }
 
-// CTAs of a row in k_draw: as many as run at once, none with less than half a batch; lists of up to K entries and a half more from each.
+// CTAs of a row in k_draw: lists of up to K entries and a half more from each.
 inline Plan plan_once(const dsbd_rows_t *r, int K) {
-    Plan p;
-    p.ctas = 1;
-    const int waves = getenv("WAVES") ? atoi(getenv("WAVES")) : 1;
-    while (p.ctas < kMaxCtas && r->rows * 2 * (int64_t)p.ctas <= 148 * kOnceResident * waves && share_of(r->V, 2 * p.ctas) >= kOnce * 16 &&
-           3 * (int64_t)K * p.ctas <= DrawList::kList)
-        p.ctas *= 2;
-    p.per = share_of(r->V, p.ctas);
-    p.words = 0;
-    return p;
+    int most = kMaxCtas;
+    while (most > 1 && 3 * (int64_t)K * most > 2 * DrawList::kList) most /= 2;
+    return plan_waves(r, 148 * kOnceResident, 24000, kOnce * 16, most);
 }
 
 }  // namespace
