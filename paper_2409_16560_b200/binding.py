@@ -967,38 +967,42 @@ class DistillParamsT(C.Structure):
 
 def _rows(logits):
     """RowsT of a [rows, V] tensor whose rows are contiguous (a view of a padded buffer's columns will do)."""
-    if logits.dim() != 2 or not logits.is_cuda or logits.dtype not in _DTYPES:
+    if not logits.is_cuda or logits.dim() != 2 or logits.dtype not in _DTYPES:
         raise AssertionError("logits are [rows, V] on the device, fp32 or bf16")
     R, V = logits.shape
-    if V < 1 or (V > 1 and logits.stride(1) != 1):
+    stride, one = logits.stride()
+    if V < 1 or (V > 1 and one != 1):
         raise AssertionError("a row's logits lie side by side")
-    stride = logits.stride(0) if R > 1 else V
-    return RowsT(logits.data_ptr(), stride, R, V, _DTYPES[logits.dtype])
+    return RowsT(logits.data_ptr(), stride if R > 1 else V, R, V, _DTYPES[logits.dtype])
 
 
 def _given(t, shape, dtype, device, what):
-    """Address of a caller's tensor, after a look at it."""
-    if t.shape != shape or t.dtype != dtype or t.device != device or not t.is_contiguous():
+    """Address of a caller's tensor, after a look at it (device: its number)."""
+    if t.shape != shape or t.dtype != dtype or t.get_device() != device or not t.is_contiguous():
         raise AssertionError("%s is %s %s, contiguous, on the logits' device" % (what, dtype, list(shape)))
     return t.data_ptr()
 
 
 def _or_new(t, shape, dtype, device, stream, what):
-    """The caller's output tensor, or a new one."""
+    """The caller's output tensor, or a new one; and its address."""
     if t is None:
-        return _made_on(stream, torch.empty, shape, dtype, device)
-    _given(t, torch.Size(shape), dtype, device, what)
-    return t
+        t = _made_on(stream, torch.empty, shape, dtype, torch.device("cuda", device))
+        return t, t.data_ptr()
+    return t, _given(t, shape, dtype, device, what)
 
 
-def _row_call(logits, status, stream):
-    """Checks that the call runs on the logits' device; its status word."""
-    if (stream.device if stream is not None else torch.device("cuda", torch.cuda.current_device())) != logits.device:
+_current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
+
+
+def _row_call(device, status, stream):
+    """Checks that the call runs on the logits' device; its status word and the address."""
+    if (_current_device() if stream is None else stream.device.index) != device:
         raise AssertionError("the stream is one of the logits' device")
-    status = _status(status, logits.device, stream)
-    if status.device != logits.device:
-        raise AssertionError("the status word is on the logits' device")
-    return status
+    if status is None:
+        status = _made_on(stream, torch.zeros, 1, torch.int32, torch.device("cuda", device))
+    elif status.dtype != torch.int32 or status.numel() < 1 or status.get_device() != device:
+        raise AssertionError("the status word is an int32 on the logits' device")
+    return status, status.data_ptr()
 
 
 def sample_rows(logits, uniform, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, token=None, logp=None, status=None, stream=None):
@@ -1006,23 +1010,21 @@ def sample_rows(logits, uniform, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0,
     [rows, draws] (fp32 in [0, 1]; [rows]: one draw each).  Each setting is a number, or a tensor [rows] (fp32; top_k int32) of the
     rows' own; temperature 0 takes the largest logit, top_k 0, top_p 1 and min_p 0 are off.
     Returns (token int32, logp fp32, status) in the shape of `uniform`."""
-    rows = _rows(logits)
-    R, dev = rows.rows, logits.device
-    if uniform.dim() not in (1, 2) or uniform.shape[0] != R:
+    rows, dev = _rows(logits), logits.get_device()
+    shape, R = uniform.shape, rows.rows
+    if len(shape) not in (1, 2) or shape[0] != R:
         raise AssertionError("uniform is [rows] or [rows, draws]")
-    u = _given(uniform, uniform.shape, torch.float32, dev, "uniform")
-    status = _row_call(logits, status, stream)
-    token = _or_new(token, uniform.shape, torch.int32, dev, stream, "token")
-    logp = _or_new(logp, uniform.shape, torch.float32, dev, stream, "logp")
-    p = SampleParamsT(1.0, 1.0, 0.0, 0, None, None, None, None, uniform.shape[1] if uniform.dim() == 2 else 1)
-    for name, x, dtype in (("temperature", temperature, torch.float32), ("top_p", top_p, torch.float32),
-                           ("min_p", min_p, torch.float32), ("top_k", top_k, torch.int32)):
+    u = _given(uniform, shape, torch.float32, dev, "uniform")
+    status, at_status = _row_call(dev, status, stream)
+    token, at_token = _or_new(token, shape, torch.int32, dev, stream, "token")
+    logp, at_logp = _or_new(logp, shape, torch.float32, dev, stream, "logp")
+    p = SampleParamsT(1.0, 1.0, 0.0, 0, None, None, None, None, shape[1] if len(shape) == 2 else 1)
+    for name, x in (("temperature", temperature), ("top_p", top_p), ("min_p", min_p), ("top_k", top_k)):
         if isinstance(x, torch.Tensor):
-            setattr(p, name + "_r", _given(x, torch.Size((R,)), dtype, dev, name))
+            setattr(p, name + "_r", _given(x, (R,), torch.int32 if name == "top_k" else torch.float32, dev, name))
         else:
             setattr(p, name, x)
-    rc = load().dsbd_sample_rows(C.addressof(rows), C.addressof(p), u, token.data_ptr(), logp.data_ptr(), status.data_ptr(),
-                                 _stream(stream))
+    rc = load().dsbd_sample_rows(C.addressof(rows), C.addressof(p), u, at_token, at_logp, at_status, _stream(stream))
     if rc != OK:
         raise DsbdError("dsbd_sample_rows", rc)
     return token, logp, status
@@ -1031,14 +1033,13 @@ def sample_rows(logits, uniform, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0,
 def top_logits(logits, K, temperature=1.0, value=None, index=None, rest=None, status=None, stream=None):
     """dsbd_top_logits: the K largest logits of each row of logits [rows, V] in falling order, of equal ones the lower token first, and
     the log-sum-exp of the row's other logits / temperature.  Returns (value fp32 [rows, K], index int32 [rows, K], rest fp32 [rows], status)."""
-    rows = _rows(logits)
-    R, dev, K = rows.rows, logits.device, int(K)
-    status = _row_call(logits, status, stream)
-    value = _or_new(value, (R, K), torch.float32, dev, stream, "value")
-    index = _or_new(index, (R, K), torch.int32, dev, stream, "index")
-    rest = _or_new(rest, (R,), torch.float32, dev, stream, "rest")
-    rc = load().dsbd_top_logits(C.addressof(rows), K, temperature, value.data_ptr(), index.data_ptr(), rest.data_ptr(),
-                                status.data_ptr(), _stream(stream))
+    rows, dev, K = _rows(logits), logits.get_device(), int(K)
+    R = rows.rows
+    status, at_status = _row_call(dev, status, stream)
+    value, at_value = _or_new(value, (R, K), torch.float32, dev, stream, "value")
+    index, at_index = _or_new(index, (R, K), torch.int32, dev, stream, "index")
+    rest, at_rest = _or_new(rest, (R,), torch.float32, dev, stream, "rest")
+    rc = load().dsbd_top_logits(C.addressof(rows), K, temperature, at_value, at_index, at_rest, at_status, _stream(stream))
     if rc != OK:
         raise DsbdError("dsbd_top_logits", rc)
     return value, index, rest, status
@@ -1049,28 +1050,31 @@ def distill(logits, value, index, rest=None, weight=None, temperature=1.0, loss=
     the teacher's other tokens together, as top_logits gives them), and the gradient of sum(weight * loss) by the logits.  grad: True for
     a new tensor, a tensor [rows, V] (rows may lie apart; the logits themselves: in place), or None for the losses alone.  Returns (loss
     fp32 [rows], grad or None, status); logits.backward(grad) hands the gradient on to what made the logits."""
-    rows = _rows(logits)
-    R, V, dev = rows.rows, rows.V, logits.device
-    if value.dim() != 2 or value.shape[0] != R:
+    rows, dev = _rows(logits), logits.get_device()
+    R, V = rows.rows, rows.V
+    shape = value.shape
+    if len(shape) != 2 or shape[0] != R:
         raise AssertionError("value is [rows, K]")
-    K = value.shape[1]
-    f32, each = torch.float32, torch.Size((R,))
-    p = DistillParamsT(K, temperature, _given(value, value.shape, f32, dev, "value"), _given(index, value.shape, torch.int32, dev, "index"),
-                       None if rest is None else _given(rest, each, f32, dev, "rest"),
-                       None if weight is None else _given(weight, each, f32, dev, "weight"))
-    status = _row_call(logits, status, stream)
-    loss = _or_new(loss, (R,), f32, dev, stream, "loss")
+    f32 = torch.float32
+    p = DistillParamsT(shape[1], temperature, _given(value, shape, f32, dev, "value"), _given(index, shape, torch.int32, dev, "index"),
+                       None if rest is None else _given(rest, (R,), f32, dev, "rest"),
+                       None if weight is None else _given(weight, (R,), f32, dev, "weight"))
+    status, at_status = _row_call(dev, status, stream)
+    loss, at_loss = _or_new(loss, (R,), f32, dev, stream, "loss")
     if grad is True:
-        grad = _made_on(stream, torch.empty, (R, V), logits.dtype, dev)
+        grad = _made_on(stream, torch.empty, (R, V), logits.dtype, logits.device)
     elif grad is False:
         grad = None
     at, stride = None, 0
     if grad is not None:
-        g = _rows(grad)
-        if (g.rows, g.V, g.dtype) != (R, V, rows.dtype) or grad.device != dev:
-            raise AssertionError("the gradient has the logits' shape, type and device")
-        at, stride = g.logits, g.row_stride
-    rc = load().dsbd_distill(C.addressof(rows), C.addressof(p), loss.data_ptr(), at, stride, status.data_ptr(), _stream(stream))
+        if grad is logits:
+            at, stride = rows.logits, rows.row_stride
+        else:
+            g = _rows(grad)
+            if (g.rows, g.V, g.dtype) != (R, V, rows.dtype) or grad.get_device() != dev:
+                raise AssertionError("the gradient has the logits' shape, type and device")
+            at, stride = g.logits, g.row_stride
+    rc = load().dsbd_distill(C.addressof(rows), C.addressof(p), at_loss, at, stride, at_status, _stream(stream))
     if rc != OK:
         raise DsbdError("dsbd_distill", rc)
     return loss, grad, status

@@ -120,15 +120,14 @@ __global__ void __launch_bounds__(NT, CTAS) k_top(TopArgs a) {
         }
 }
 
-// CTAs of a row: as many as an SM's `resident` allow to run at once, none with less than a batch, and lists that fit into one.
+// CTAs of a row: as many as run at once (resident ones of an SM), none with less than half a batch, and lists that fit into one.  (More CTAs
+// of a row than run at once, to even out the waves, cost what a CTA does for each row: 592 rows of 128256 91 us, in two CTAs each 108.)
 inline Plan plan_top(const dsbd_rows_t *r, int threads, int resident, int list, int K) {
-    Plan p;
-    p.ctas = 1;
+    Plan p = {1, 0, 0};
     while (p.ctas < kMaxCtas && r->rows * 2 * (int64_t)p.ctas <= 148 * resident && share_of(r->V, 2 * p.ctas) >= threads * 16 &&
            3 * (int64_t)K * p.ctas <= list)
         p.ctas *= 2;
     p.per = share_of(r->V, p.ctas);
-    p.words = 0;
     return p;
 }
 
@@ -157,9 +156,9 @@ extern "C" int dsbd_top_logits(const dsbd_rows_t *rows, int32_t K, float tempera
     TopArgs a = {};
     a.logits = rows->logits; a.stride = rows->row_stride; a.V = rows->V; a.K = K; a.temperature = temperature;
     a.value = value; a.index = index; a.rest = rest; a.status = status;
-    // Where there are rows enough, small CTAs: what a CTA does once for each row costs fewer instructions (4608 rows of 128256 467 us,
-    // with 256 threads 496; 592 rows 100 and 90)
-    if (K <= 256 && rows->rows >= 148 * 6)
+    // Where there are rows enough, small CTAs: what a CTA does once for each row costs fewer instructions (4608 rows of 128256 465 us,
+    // with 256 threads 496; 512 rows 85 and 88; 296 rows 57 and 52)
+    if (K <= 256 && rows->rows >= 148 * 3)
         return rows->dtype == DSBD_DTYPE_F32 ? run_top<float, 128, 4, 1024, 1024, 6>(rows, a, stream)
                                              : run_top<__nv_bfloat16, 128, 4, 1024, 1024, 6>(rows, a, stream);
     if (K <= 512)
