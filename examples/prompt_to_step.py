@@ -5,7 +5,10 @@
 The large model reads its prompts in two chunks (dsbd_kv_append_paged, dsbd_chunk_attention_paged), the small model reads them whole
 and then draws drafts: every draft beam is a sequence of its own behind shared prompt pages.  The drafts become a forest,
 whose nodes are rotated at their positions (dsbd_forest_positions, dsbd_rotate_qk) and attend in the large model
-(dsbd_forest_attention_paged); the verification keeps the output beams and the caches follow them.
+(dsbd_forest_attention_paged); the verification keeps the output beams and the caches follow them.  Beside the step: what each
+request would draw without speculating, with settings of its own (dsbd_sample_rows), and what pulls the small model to the large
+one -- the large model's largest logits at the verified nodes (dsbd_top_logits), the small model's losses there and their gradient
+(dsbd_distill), which go on to the weights that made its logits.
 """
 import os
 import sys
@@ -169,8 +172,18 @@ def run(lengths=(150, 65), gamma=3, W_S=4, V=1000, seed=0):
                                out["out_logp"], k_new, v_new, large.k_pool, large.v_pool, table, page_off, prefix_off, poff,
                                dev(free, np.int32), dev([len(large.free)], np.int32), n_slots=int(out_off[-1]), table_capacity=64,
                                status=status)
+
+    # ---- beside the step: plain draws of each request, and what the small model learns from the verified nodes
+    settings = dict(temperature=dev(np.linspace(0.0, 1.0, R), np.float32), top_k=dev([0, 20][:R] + [0] * max(R - 2, 0), np.int32),
+                    top_p=dev(np.full(R, 0.9), np.float32))
+    uniform = torch.rand(R, 3, generator=torch.Generator(device=DEV).manual_seed(seed), device=DEV)
+    plain, plain_logp, _ = dsbd.sample_rows(zp[roots], uniform, status=status, **settings)
+    value, index, rest, _ = dsbd.top_logits(zp, 16, temperature=2.0, status=status)
+    weight = torch.full((forest.N,), 1.0 / forest.N, device=DEV)
+    loss, slope, _ = dsbd.distill(zq_nodes, value, index, rest=rest, weight=weight, temperature=2.0, status=status)
     torch.cuda.synchronize()
-    return dict(large=large, prompts=prompts, forest=forest, tokens=tokens, zp=zp, out=out, commit=res, status=int(status.item()),
+    fit = dict(value=value, index=index, rest=rest, weight=weight, loss=loss, slope=slope)
+    return dict(zq=zq_nodes, roots=roots, plain=plain, plain_logp=plain_logp, uniform=uniform, settings=settings, fit=fit, large=large, prompts=prompts, forest=forest, tokens=tokens, zp=zp, out=out, commit=res, status=int(status.item()),
                 need=need, out_off=out_off)
 
 
@@ -184,6 +197,7 @@ def main():
             i, len(r["prompts"][i]), int(out["l_last"][i]), w, out["out_token"][s].tolist(),
             [int(x) for x in (r["commit"]["new_prefix_off"][1:] - r["commit"]["new_prefix_off"][:-1])[int(r["commit"]["new_req_beam_off"][i]):
                                                                  int(r["commit"]["new_req_beam_off"][i + 1])]]))
+        print("  plain draws %s; nodes' mean loss of the small model %.3f" % (r["plain"][i].tolist(), float(r["fit"]["loss"].mean())))
     print("status", r["status"])
 
 

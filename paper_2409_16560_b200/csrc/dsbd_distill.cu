@@ -158,7 +158,7 @@ __global__ void __launch_bounds__(NT, RESIDENT) k_distill(DistillArgs a) {
     }
     // ---- the student's sums
     const double scale = 1.4426950408889634 * a.inverse;
-    const float scale_f = (float)scale;
+    const float scale_f = fminf((float)scale, FLT_MAX);                 // (0 times it stays 0)
     Rest others;
     for (int w0 = 0; w0 < s.words;) {
         // the warp's 1024 elements of the batch have 32 words of marks

@@ -119,12 +119,6 @@ __device__ __forceinline__ void load_batch(float4 (&raw)[kDeep<T>], const T *row
     }
 }
 
-// A whole word into shared memory, later.
-__device__ __forceinline__ void copy_async(float4 *to, const float4 *from) {
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"((uint32_t)__cvta_generic_to_shared(to)), "l"(from) : "memory");
-}
-__device__ __forceinline__ void copies_here() { asm volatile("cp.async.wait_all;" ::: "memory"); }
-
 // The share into shared memory, 8 words a thread in flight, each also to f(elements) of the thread that brought it.
 template <class T, class F>
 __device__ __forceinline__ void load_share(const T *row, const Share &s, float4 *mem, F f) {

@@ -126,8 +126,8 @@ __device__ __forceinline__ bool bring(Row<T> &r, const T *row, float4 *mem, int3
 
 // The cluster's totals of bin threadIdx.x, after a barrier behind the filling.
 template <class T>
-__device__ __forceinline__ uint32_t bin_count(const Row<T> &r, Hist &h) {
-    uint32_t n = 0;
+__device__ __forceinline__ uint64_t bin_count(const Row<T> &r, Hist &h) {
+    uint64_t n = 0;
     for (int c = 0; c < r.ctas; ++c) n += r.of(&h, c)->count[threadIdx.x];
     return n;
 }
@@ -244,7 +244,7 @@ __device__ Cut cut_at(Row<T> &r, Cut within, uint32_t k, double p, const Whole &
             atomicAdd(&h.count[b], 1u);
         });
         cluster_barrier(r.ctas);
-        const uint32_t n = bin_count(r, h);
+        const uint32_t n = (uint32_t)bin_count(r, h);
         const uint64_t v = BY_MASS ? bin_mass(r, h) : n;
         uint64_t total;
         const uint64_t excl = before(v, &total, sh.scan);

@@ -35,7 +35,7 @@ __global__ void __launch_bounds__(NT, CTAS) k_top(TopArgs a) {
     float *value_out = a.value + (int64_t)row * a.K;
     int32_t *index_out = a.index + (int64_t)row * a.K;
     const double scale = 1.4426950408889634 / (double)a.temperature;
-    const float scale_f = (float)scale;
+    const float scale_f = fminf((float)scale, FLT_MAX);                 // (0 times it stays 0)
     Rest rest;
     Sum cleared = {-CUDART_INF_F, 0.0};
     const bool good = collect<T, true>(sh, at, share<T>(at, a.V, rank, a.per), (uint32_t)a.K, a.ctas > 1, scale_f, rest, cleared);
