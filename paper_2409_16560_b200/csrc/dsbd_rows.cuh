@@ -18,7 +18,6 @@ namespace cg = cooperative_groups;
 constexpr int kThreads = 512;
 constexpr int kWarps = kThreads / 32;
 constexpr int kMaxCtas = 8;                        // the largest portable cluster
-constexpr int kShareBytes = DSBD_MAX_ROW_BYTES / kMaxCtas;       // of a row in one CTA, at most
 
 // ---- elements ------------------------------------------------------------------------------
 template <class T> constexpr int kPer = 16 / (int)sizeof(T);     // elements of a 16-byte word

@@ -10,8 +10,9 @@
 //   k_draw_cut: the other rows.  A cluster of 1 to 8 CTAs brings the row into shared memory once; every later step reads it there.
 //     Larger top-k: each thread has the largest of its words; the k-th largest of those maxima (by bins) is at or below the k-th largest
 //     logit, and little more than k tokens reach it.  Top-p, min-p: a histogram of masses by bins of the logit, rounded down a little, says which
-//     bins certainly hold the prefix.  These tokens go to a list in one CTA, as above.
-//     Where the list does not hold them: a histogram of 512 bins over the cluster, linear in the logit first, then in the bits of the
+//     bins certainly hold the prefix.  These tokens go to a list in one CTA, as above; where they are too many for it, those of the bins
+//     that the cut may lie in do, and all CTAs draw from their shares.
+//     Where the list does not hold these either: a histogram of 512 bins over the cluster, linear in the logit first, then in the bits of the
 //     keys of the bin that the cut is in, until that is one key; equal keys go by token.  Masses are then whole numbers (2^62 / V' of the
 //     largest token's mass, V' the power of two from V on), so sums do not depend on their order.  Then the draw over all shares.
 #include "dsbd_top.cuh"
@@ -295,15 +296,19 @@ __device__ Cut cut_at(Row<T> &r, Cut within, uint32_t k, double p, const Whole &
     }
 }
 
-// The tokens of the bins up to `last` below the row's largest logit, as (key, ~token) in the tokens' order, in the list of rank 0;
-// returns their number, and -1 if the list does not hold them.
+// The tokens of the bins `first` to `last` below the row's largest logit, as (key, ~token) in the tokens' order, in the list of rank 0;
+// returns their number, and -1 if the list does not hold them.  *sum: a CTA's number in, all CTAs' out.
 template <class T>
-__device__ int list_bins(Row<T> &r, float scale, int last) {
+__device__ int list_bins(Row<T> &r, float scale, int first, int last, double *sum = nullptr) {
     Shared &sh = r.sh;
     const int lane = threadIdx.x & 31, warp = threadIdx.x / 32, each_warp = r.warp_words();
     const int w0 = warp * each_warp, w1 = min(w0 + each_warp, r.s.words);
     const float beyond = last < kBins - 1 ? (float)(last + 1) : CUDART_INF_F;
-    auto inside = [&](float z) { return !((r.top - z) * scale >= beyond) && z > -CUDART_INF_F; };
+    const float begins = first ? (float)first : -1.f;
+    auto inside = [&](float z) {
+        const float x = (r.top - z) * scale;
+        return !(x >= beyond) && !(x < begins) && z > -CUDART_INF_F;
+    };
     auto marks = [&](int w) {
         uint32_t which = 0;
         if (w < w1) {
@@ -345,26 +350,30 @@ __device__ int list_bins(Row<T> &r, float scale, int last) {
             at += __shfl_sync(kFull, up, 31);
         }
     __syncthreads();
-    const Note *all = r.tell_all({0.0, 0.f, 0.f, listed, 0});
-    uint32_t sum = 0;
-    for (int c = 0; c < r.ctas; ++c) sum += all[c].a;
-    if (sum > (uint32_t)r.room) return -1;
+    const Note *all = r.tell_all({sum ? *sum : 0.0, 0.f, 0.f, listed, 0});
+    uint32_t found = 0;
+    if (sum) *sum = 0.0;
+    for (int c = 0; c < r.ctas; ++c) {
+        found += all[c].a;
+        if (sum) *sum += all[c].sum;
+    }
+    if (found > (uint32_t)r.room) return -1;
     if (r.rank == 0)
-        for (uint32_t i = all[0].a + threadIdx.x; i < sum; i += kThreads) {
+        for (uint32_t i = all[0].a + threadIdx.x; i < found; i += kThreads) {
             uint32_t from = i;
             int c = 0;
             while (from >= all[c].a) from -= all[c++].a;
             r.list[i] = r.of(r.list, c)[from];
         }
     cluster_barrier(r.ctas);                       // (the others' lists have been read)
-    return (int)sum;
+    return (int)found;
 }
 
 // The tokens that certainly hold the shortest prefix of p of the mass (p < 1), or those of at least m of the largest one's, listed as in
 // list_bins; *whole: the row's mass (p < 1).  A bin's mass is summed in steps of 2^-14 of its largest, rounded down: what is found to have p of the whole
-// has it, and the list is exact.
+// has it, and the list is exact.  *inside: so many bins are certainly part of the prefix.
 template <class T>
-__device__ int list_mass(Row<T> &r, float p, float m, float T_, const Mass &mass, double *whole, float *finer) {
+__device__ int list_mass(Row<T> &r, float p, float m, float T_, const Mass &mass, double *whole, float *scale_out, int *inside, int *last_out) {
     Shared &sh = r.sh;
     constexpr float kOctaves = 16.f;               // that the bins span: a prefix that reaches further is longer than the list
     const float scale = bins_over(kOctaves * 0.6931472f * T_), step = kOctaves / (float)(kBins - 1);
@@ -396,13 +405,68 @@ __device__ int list_mass(Row<T> &r, float p, float m, float T_, const Mass &mass
         const double v = (double)((float)bin_count(r, h) * exp2_fast(-(float)threadIdx.x * step)) * (1.0 / 16384.0);
         double all_bins;
         const double upto = before(v, &all_bins, sh.sums);
-        const double goal = (double)p * sum * (1.0 + 1e-4);
-        if (upto < goal && upto + v >= goal) sh.picked_bin = threadIdx.x;
-        __syncthreads();
+        // (the bins' sums are at most 7e-5 too small)
+        const double goal = (double)p * sum;
+        if (upto < goal * (1.0 + 1e-4) && upto + v >= goal * (1.0 + 1e-4)) sh.picked_bin = threadIdx.x;
+        *inside = __syncthreads_count((upto + v) * (1.0 + 1e-4) < goal);
         last = min(last, (int)sh.picked_bin);
     }
-    *finer = scale * ((float)kBins / (float)(last + 1));
-    return list_bins(r, scale, last);
+    *scale_out = scale;
+    *last_out = last;
+    return list_bins(r, scale, 0, last);
+}
+
+// The cut that keeps the shortest prefix of `goal`, which lies in the bins first to last, where these are few enough for the list; false
+// everywhere if not.  The mass above them is summed, they are put in order.
+template <class T>
+__device__ bool cut_in_bins(Row<T> &r, float scale, int first, int last, double goal, const Mass &mass, Cut *cut) {
+    Shared &sh = r.sh;
+    double above = 0.0;
+    const float begins = (float)first;
+    for (int w = threadIdx.x; w < r.s.words; w += kThreads) {
+        float x[kPer<T>];
+        unpack(r.mem[w], x);
+        double m[kPer<T>];
+#pragma unroll
+        for (int e = 0; e < kPer<T>; ++e) m[e] = mass.of(x[e]);
+#pragma unroll
+        for (int e = 0; e < kPer<T>; ++e) above += (r.top - x[e]) * scale < begins ? m[e] : 0.0;
+    }
+    above = over_cta(above, add, sh.sums);
+    const int n = list_bins(r, scale, first, last, &above);
+    if (n <= 0 || n > r.room / 2) return false;
+    Note note = {0.0, 0.f, 0.f, 0, 0};
+    if (r.rank == 0) {
+        // (in the list's other half, not in the share's place: every CTA still draws from its share)
+        uint64_t *tmp = r.list + r.room / 2;
+        const float finer = scale * ((float)kBins / (float)(last - first + 1)), top = r.top - (float)first / scale;
+        order_down<kThreads, kBins>(r.list, tmp, n, sh.hist[0].count, reinterpret_cast<uint32_t *>(sh.scan),
+                                    [&](uint64_t e) { return min(max(__float2int_rz((top - logit_of(e)) * finer), 0), kBins - 1); });
+        double *w = reinterpret_cast<double *>(tmp), mine = 0.0, total;
+#pragma unroll 4
+        for (int i = threadIdx.x; i < n; i += kThreads) w[i] = mass.of(logit_of(r.list[i]));
+        if (threadIdx.x == 0) sh.picked_count = (uint32_t)n;
+        __syncthreads();
+        const int each = (n + kThreads - 1) / kThreads | 1, begin = min((int)threadIdx.x * each, n), end = min(begin + each, n);
+        for (int i = begin; i < end; ++i) mine += w[i];
+        double upto = above + before(mine, &total, sh.sums);
+        for (int i = begin; i < end; ++i) {
+            if (!(upto < goal)) {
+                atomicMin(&sh.picked_count, (uint32_t)i);
+                break;
+            }
+            upto += w[i];
+        }
+        __syncthreads();
+        // the last entry that is kept (none: what is above the first)
+        const int kept = (int)sh.picked_count;
+        const uint64_t e = r.list[max(kept - 1, 0)];
+        note.a = (uint32_t)(e >> 32);
+        note.b = (uint32_t)token_of(e) - (kept == 0);
+    }
+    const Note got = r.tell_all(note)[0];
+    *cut = {got.a, (int)got.b};
+    return true;
 }
 
 // The tokens at or above the k-th largest logit, listed as in list_bins.  k <= kTop; fewer than k where the row has fewer above -inf.
@@ -421,7 +485,7 @@ __device__ int list_top(Row<T> &r, int k, float *finer) {
     __syncthreads();
     const int last = (int)sh.picked_bin;
     *finer = scale * ((float)kBins / (float)(last + 1));
-    return list_bins(r, scale, last);
+    return list_bins(r, scale, 0, last);
 }
 
 // ------------------------------------------------------------------------------------ draws
@@ -638,8 +702,14 @@ __device__ void draw_cut(const SampleArgs &a, float4 *mem, Shared &sh) {
     double whole_mass = 0.0;
     int n = -1;
     float finer = 0.f;                             // scale of bins that hold the list's logits alone
-    if (set.k == 0) n = list_mass(r, set.p, set.m, set.T, mass, &whole_mass, &finer);
-    else if (set.k <= kTop) n = list_top(r, set.k, &finer);
+    float scale = 0.f;
+    int inside = 0, last = kBins - 1;
+    if (set.k == 0) {
+        n = list_mass(r, set.p, set.m, set.T, mass, &whole_mass, &scale, &inside, &last);
+        finer = scale * ((float)kBins / (float)(last + 1));
+    } else if (set.k <= kTop) {
+        n = list_top(r, set.k, &finer);
+    }
     if (n >= 0) {
         if (rank == 0)
             draw_listed<kThreads, kList>(r.list, r.tmp(), sh.sums, sh.hist[0].count, reinterpret_cast<uint32_t *>(sh.scan), a, row, set, n,
@@ -647,6 +717,13 @@ __device__ void draw_cut(const SampleArgs &a, float4 *mem, Shared &sh) {
         return;
     }
     Cut cut = {kKeyMasked, -1};                    // everything above -inf
+    // a prefix longer than the list: only where it ends is put in order (64 rows of 128256 fp32 with settings of their own: 86 us by
+    // levels of bins, 67 so; where the list holds the prefix, it in order is faster: 512 rows of such, top-p 0.95, 447 us against 720)
+    if (set.k == 0 && set.p < 1.f && inside > 0 && last < kBins - 1 &&
+        cut_in_bins(r, scale, inside, last, (double)set.p * whole_mass, mass, &cut)) {
+        draw_shared(r, a, row, set, cut, mass);
+        return;
+    }
     const Whole whole = {mass, (double)(1ull << (30 + __clz(a.V - 1 | 1)))};
     if (set.k) cut = cut_at<false>(r, cut, (uint32_t)set.k, 0.0, whole, 2.f * (r.top - r.low));
     if (set.p < 1.f) cut = cut_at<true>(r, cut, 0, (double)set.p, whole, 64.f * 0.6931472f * set.T);
@@ -656,7 +733,7 @@ __device__ void draw_cut(const SampleArgs &a, float4 *mem, Shared &sh) {
 // Beside k_draw, whose rows are others: its CTAs have all waited for what came before them when this kernel is launched, so this one
 // need not; but it ends after k_draw has, as what comes next waits for this kernel alone.
 template <class T>
-__global__ void __launch_bounds__(kThreads) k_draw_cut(SampleArgs a) {
+__global__ void __launch_bounds__(kThreads, 2) k_draw_cut(SampleArgs a) {
     extern __shared__ float4 mem[];
     __shared__ Shared sh;
     if (!a.beside) {

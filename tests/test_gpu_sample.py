@@ -74,6 +74,26 @@ def test_top_p_of_any_size(dtype, T, p):
     check(z, uniform(3, 8, 8), T, 0, p)
 
 
+@pytest.mark.parametrize("dtype", [F32, BF])
+@pytest.mark.parametrize("V", [20000, 50257, 151936])
+@pytest.mark.parametrize("spread", [0.05, 0.5, 3.0])
+def test_prefixes_longer_than_a_list(V, dtype, spread):
+    """Flat rows, whose top-p and min-p keep thousands of tokens, among ties (bf16) and without (fp32)."""
+    z = ru.rows_of(3, V, dtype, seed=V + 1, pad=5, start=3, spread=spread, zipf=False)
+    u = uniform(3, 6, V)
+    for T, p, m in [(1.0, 0.5, 0.0), (1.0, 0.9, 0.0), (2.5, 0.97, 0.0), (8.0, 0.3, 0.0), (1.0, 0.9, 0.2), (3.0, 0.999, 0.7), (0.5, 0.8, 1e-3)]:
+        check(z, u, T, 0, p, m)
+
+
+@pytest.mark.parametrize("T", [1e-30, 1e-36, 1e-38, 1e-40])
+def test_temperatures_that_leave_no_scale(T):
+    """Differences of the logits over the temperature: beyond fp32, or of ordinary size where the logits are as small."""
+    z = ru.rows_of(4, 9000, F32, seed=5)
+    z[2:] = (z[2:].double() * T).float()
+    for k, p, m in [(0, 1.0, 0.0), (20, 0.9, 0.0), (0, 0.9, 0.0), (2000, 0.9, 0.1)]:
+        check(z, uniform(4, 5, 6), T, k, p, m)
+
+
 @pytest.mark.parametrize("V", [5, 700, 3000, 40000, 128256])
 @pytest.mark.parametrize("levels", [1, 2, 3])
 def test_equal_logits_go_by_token(V, levels):
