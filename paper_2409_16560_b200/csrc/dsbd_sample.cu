@@ -24,6 +24,7 @@ namespace {
 static_assert(kBins == kThreads, "a thread for each bin");
 constexpr int kTop = DSBD_MAX_TOP;                 // tokens that a cut by list keeps, at most
 constexpr int kList = 4 * kTop;                    // entries of the list
+constexpr int kNear = 256;                         // entries that are compared with one another
 
 struct SampleArgs {
     const void *logits;
@@ -55,7 +56,7 @@ struct Note {
 struct Shared {
     double table[64];
     Told<Note> told;
-    Hist hist[2];
+    alignas(16) Hist hist[2];
     Note scratch[kWarps];
     double sums[kWarps + 1];
     uint64_t scan[kWarps];
@@ -296,30 +297,36 @@ __device__ Cut cut_at(Row<T> &r, Cut within, uint32_t k, double p, const Whole &
     }
 }
 
-// The tokens of the bins `first` to `last` below the row's largest logit, as (key, ~token) in the tokens' order, in the list of rank 0;
-// returns their number, and -1 if the list does not hold them.  *sum: a CTA's number in, all CTAs' out.
+// What bins of width 1 / scale below top hold, by logits alone (one comparison, where a bin takes a subtraction, a product and three).  `from`: at or
+// above it lie all of the bins up to `last`, and what is within a rounding of them.  `above`: at or above it lie bins before `first` alone.
+struct Range {
+    float from, above;
+    __device__ Range(float top, float scale, int first, int last) {
+        const float wide = (float)(last + 1) / scale, near = (float)first / scale;
+        from = last < kBins - 1 && scale > 0.f ? fmaxf(top - wide - 4.8e-7f * (fabsf(top) + wide), -FLT_MAX) : -FLT_MAX;
+        above = first ? top - near + 4.8e-7f * (fabsf(top) + near) : CUDART_INF_F;
+    }
+};
+
+// The tokens with logits in a range, as (key, ~token) in the tokens' order, in the list of rank 0; returns their number, and -1 if the list does
+// not hold them.  *sum: a CTA's number in, all CTAs' out.
 template <class T>
-__device__ int list_bins(Row<T> &r, float scale, int first, int last, double *sum = nullptr) {
+__device__ int list_range(Row<T> &r, const Range range, double *sum = nullptr) {
     Shared &sh = r.sh;
     const int lane = threadIdx.x & 31, warp = threadIdx.x / 32, each_warp = r.warp_words();
     const int w0 = warp * each_warp, w1 = min(w0 + each_warp, r.s.words);
-    const float beyond = last < kBins - 1 ? (float)(last + 1) : CUDART_INF_F;
-    const float begins = first ? (float)first : -1.f;
-    auto inside = [&](float z) {
-        const float x = (r.top - z) * scale;
-        return !(x >= beyond) && !(x < begins) && z > -CUDART_INF_F;
-    };
     auto marks = [&](int w) {
         uint32_t which = 0;
         if (w < w1) {
             float x[kPer<T>];
             unpack(r.mem[w], x);
 #pragma unroll
-            for (int e = 0; e < kPer<T>; ++e) which |= (uint32_t)inside(x[e]) << e;
+            for (int e = 0; e < kPer<T>; ++e) which |= (uint32_t)(x[e] >= range.from && x[e] < range.above) << e;
         }
         return which;
     };
-    // how many each warp's words have, then each entry at its place
+    // how many each warp's words have, then each entry at its place in rank 0's list (entries gathered by rank 0 instead, in reads that
+    // wait for one another: one row of 128256 fp32 with top-p 27 us, so XX)
     uint32_t mine = 0;
     for (int w = w0 + lane; w < w1; w += 32) mine += __popc(marks(w));
     mine = __reduce_add_sync(kFull, mine);
@@ -332,45 +339,37 @@ __device__ int list_bins(Row<T> &r, float scale, int first, int last, double *su
         at += w < warp ? (uint32_t)sh.scan[w] : 0;
         listed += (uint32_t)sh.scan[w];
     }
-    if (mine && listed <= (uint32_t)r.room)
-        for (int w = w0; w < w1; w += 32) {
-            uint32_t which = marks(w + lane);
-            if (!__any_sync(kFull, which != 0)) continue;
-            const uint32_t here = __popc(which);
-            uint32_t up = here;
-#pragma unroll
-            for (int o = 1; o < 32; o <<= 1) {
-                const uint32_t x = __shfl_up_sync(kFull, up, o);
-                if (lane >= o) up += x;
-            }
-            for (uint32_t to = at + up - here; which; which &= which - 1, ++to) {
-                const int i = (w + lane) * kPer<T> + __ffs(which) - 1;
-                r.list[to] = entry_of(value_of(reinterpret_cast<const T *>(r.mem)[i]), r.s.first + i - r.s.mis);
-            }
-            at += __shfl_sync(kFull, up, 31);
-        }
-    __syncthreads();
     const Note *all = r.tell_all({sum ? *sum : 0.0, 0.f, 0.f, listed, 0});
     uint32_t found = 0;
     if (sum) *sum = 0.0;
     for (int c = 0; c < r.ctas; ++c) {
+        at += c < r.rank ? all[c].a : 0;
         found += all[c].a;
         if (sum) *sum += all[c].sum;
     }
     if (found > (uint32_t)r.room) return -1;
-    if (r.rank == 0)
-        for (uint32_t i = all[0].a + threadIdx.x; i < found; i += kThreads) {
-            uint32_t from = i;
-            int c = 0;
-            while (from >= all[c].a) from -= all[c++].a;
-            r.list[i] = r.of(r.list, c)[from];
+    uint64_t *list = r.of(r.list, 0);
+    if (mine)
+        for (int w = w0; w < w1; w += 32) {
+            uint32_t which = marks(w + lane), up = 0, here = 0;
+#pragma unroll
+            for (int e = 0; e < kPer<T>; ++e) {
+                const unsigned b = __ballot_sync(kFull, which >> e & 1);
+                up += __popc(b & ((1u << lane) - 1));
+                here += __popc(b);
+            }
+            for (uint32_t to = at + up; which; which &= which - 1, ++to) {
+                const int i = (w + lane) * kPer<T> + __ffs(which) - 1;
+                list[to] = entry_of(value_of(reinterpret_cast<const T *>(r.mem)[i]), r.s.first + i - r.s.mis);
+            }
+            at += here;
         }
-    cluster_barrier(r.ctas);                       // (the others' lists have been read)
+    cluster_barrier(r.ctas);
     return (int)found;
 }
 
 // The tokens that certainly hold the shortest prefix of p of the mass (p < 1), or those of at least m of the largest one's, listed as in
-// list_bins; *whole: the row's mass (p < 1).  A bin's mass is summed in steps of 2^-14 of its largest, rounded down: what is found to have p of the whole
+// list_range; *whole: the row's mass (p < 1).  A bin's mass is summed in steps of 2^-14 of its largest, rounded down: what is found to have p of the whole
 // has it, and the list is exact.  *inside: so many bins are certainly part of the prefix.
 template <class T>
 __device__ int list_mass(Row<T> &r, float p, float m, float T_, const Mass &mass, double *whole, float *scale_out, int *inside, int *last_out) {
@@ -413,7 +412,7 @@ __device__ int list_mass(Row<T> &r, float p, float m, float T_, const Mass &mass
     }
     *scale_out = scale;
     *last_out = last;
-    return list_bins(r, scale, 0, last);
+    return list_range(r, Range(r.top, scale, 0, last));
 }
 
 // The cut that keeps the shortest prefix of `goal`, which lies in the bins first to last, where these are few enough for the list; false
@@ -422,7 +421,7 @@ template <class T>
 __device__ bool cut_in_bins(Row<T> &r, float scale, int first, int last, double goal, const Mass &mass, Cut *cut) {
     Shared &sh = r.sh;
     double above = 0.0;
-    const float begins = (float)first;
+    const Range range(r.top, scale, first, last);
     for (int w = threadIdx.x; w < r.s.words; w += kThreads) {
         float x[kPer<T>];
         unpack(r.mem[w], x);
@@ -430,10 +429,10 @@ __device__ bool cut_in_bins(Row<T> &r, float scale, int first, int last, double 
 #pragma unroll
         for (int e = 0; e < kPer<T>; ++e) m[e] = mass.of(x[e]);
 #pragma unroll
-        for (int e = 0; e < kPer<T>; ++e) above += (r.top - x[e]) * scale < begins ? m[e] : 0.0;
+        for (int e = 0; e < kPer<T>; ++e) above += x[e] >= range.above ? m[e] : 0.0;
     }
     above = over_cta(above, add, sh.sums);
-    const int n = list_bins(r, scale, first, last, &above);
+    const int n = list_range(r, range, &above);
     if (n <= 0 || n > r.room / 2) return false;
     Note note = {0.0, 0.f, 0.f, 0, 0};
     if (r.rank == 0) {
@@ -469,7 +468,7 @@ __device__ bool cut_in_bins(Row<T> &r, float scale, int first, int last, double 
     return true;
 }
 
-// The tokens at or above the k-th largest logit, listed as in list_bins.  k <= kTop; fewer than k where the row has fewer above -inf.
+// The tokens at or above the k-th largest logit, listed as in list_range.  k <= kTop; fewer than k where the row has fewer above -inf.
 template <class T>
 __device__ int list_top(Row<T> &r, int k, float *finer) {
     Shared &sh = r.sh;
@@ -485,7 +484,7 @@ __device__ int list_top(Row<T> &r, int k, float *finer) {
     __syncthreads();
     const int last = (int)sh.picked_bin;
     *finer = scale * ((float)kBins / (float)(last + 1));
-    return list_bins(r, scale, 0, last);
+    return list_range(r, Range(r.top, scale, 0, last));
 }
 
 // ------------------------------------------------------------------------------------ draws
@@ -523,13 +522,50 @@ __device__ __forceinline__ void put_draw(const SampleArgs &a, int row, int d, in
     if (a.logp) a.logp[(int64_t)row * a.draws + d] = (float)logp;
 }
 
+// Draws of a list of n entries in the tokens' order by their masses w (0: not kept).  upto_of: n numbers; sums: one for each warp.
+template <int NT, int MOST>
+__device__ void draw_kept(const uint64_t *list, const double *w, double *upto_of, double *sums, const SampleArgs &a, int row, const Settings &set,
+                          int n, float top) {
+    const int lane = threadIdx.x & 31, warp = threadIdx.x / 32;
+    __syncthreads();
+    const int each = (n + NT - 1) / NT | 1, begin = min((int)threadIdx.x * each, n), end = min(begin + each, n);
+    double total, mine = 0.0;
+    for (int i = begin; i < end; ++i) mine += w[i];
+    double upto = before<NT>(mine, &total, sums);
+    for (int i = begin; i < end; ++i) {
+        upto += w[i];
+        upto_of[i] = upto;
+    }
+    __syncthreads();
+    total = upto_of[n - 1];
+    const double log_total = log(total);
+    for (int d = warp; d < a.draws; d += NT / 32) {
+        const float u = a.uniform[(int64_t)row * a.draws + d];
+        if (!(u >= 0.f && u <= 1.f)) {
+            if (lane == 0) no_draw(a, row, d, DSBD_DEV_BAD_PARAM);
+            continue;
+        }
+        const double t = target(u, total);
+        // the first entry beyond t, of those kept
+        int at = 0;
+        for (int step = MOST / 2; step > 0; step >>= 1)
+            if (at + step <= n - 1 && upto_of[at + step - 1] <= t) at += step;
+        if (lane == 0) {
+            int back = at;
+            while (back >= 0 && w[back] == 0.0) --back;             // (within a rounding of the sums)
+            while (back < 0 && w[at] == 0.0) ++at;
+            const uint64_t x = list[back >= 0 ? back : at];
+            put_draw(a, row, d, token_of(x), ((double)logit_of(x) - (double)top) / (double)set.T - log_total);
+        }
+    }
+}
+
 // Draws of a list of n entries in the tokens' order that has the k largest, or all that can be kept (one CTA alone).  whole: the mass that
 // top-p is of; 0: the k largest entries'.  room: 2 MOST numbers; sums, scan: one for each warp; count: kBins; scale: of bins below top that
 // hold the list's logits.
 template <int NT, int MOST>
 __device__ void draw_listed(const uint64_t *list, uint64_t *room, double *sums, uint32_t *count, uint32_t *scan, const SampleArgs &a, int row,
                             const Settings &set, int n, double whole, const Mass &mass, float top, float scale) {
-    const int lane = threadIdx.x & 31, warp = threadIdx.x / 32;
     __shared__ uint32_t first_out;
     uint64_t *down = room, *tmp = room + MOST;
     // ---- in falling order: what is kept is a prefix, so everything from an entry on
@@ -560,40 +596,66 @@ __device__ void draw_listed(const uint64_t *list, uint64_t *room, double *sums, 
     // ---- in the tokens' order: cumulative masses of what is kept
 #pragma unroll 4
     for (int i = threadIdx.x; i < n; i += NT) w[i] = list[i] >= least ? mass.of(logit_of(list[i])) : 0.0;
-    __syncthreads();
-    each = (n + NT - 1) / NT | 1;
-    begin = min((int)threadIdx.x * each, n);
-    end = min(begin + each, n);
-    mine = 0.0;
-    for (int i = begin; i < end; ++i) mine += w[i];
-    upto = before<NT>(mine, &total, sums);
-    double *upto_of = reinterpret_cast<double *>(room);
-    for (int i = begin; i < end; ++i) {
-        upto += w[i];
-        upto_of[i] = upto;
+    draw_kept<NT, MOST>(list, w, reinterpret_cast<double *>(room), sums, a, row, set, n, top);
+}
+
+// The same for a prefix of top-p or min-p whose end lies in the bins from `inside` on, of width 1 / scale below top: only these bins'
+// entries are compared with one another.  False if they are more than `most`, up to NT (nothing is drawn then).  near: 2 most numbers.
+template <int NT, int MOST>
+__device__ bool draw_prefix(const uint64_t *list, uint64_t *room, double *sums, uint64_t *near, int most, const SampleArgs &a, int row,
+                            const Settings &set, int n, double whole, const Mass &mass, float top, float scale, int inside) {
+    double *near_mass = reinterpret_cast<double *>(near + most);
+    const int lane = threadIdx.x & 31, warp = threadIdx.x / 32;
+    double *w = reinterpret_cast<double *>(room), *upto_of = w + MOST;
+    const double m = (double)set.m;
+#pragma unroll 4
+    for (int i = threadIdx.x; i < n; i += NT) {
+        const double x = mass.of(logit_of(list[i]));
+        w[i] = x >= m ? x : 0.0;                   // (what is below m has no part in a larger entry's sum)
     }
-    __syncthreads();
-    total = upto_of[n - 1];
-    const double log_total = log(total);
-    for (int d = warp; d < a.draws; d += NT / 32) {
-        const float u = a.uniform[(int64_t)row * a.draws + d];
-        if (!(u >= 0.f && u <= 1.f)) {
-            if (lane == 0) no_draw(a, row, d, DSBD_DEV_BAD_PARAM);
-            continue;
+    if (set.p < 1.f) {
+        const float sure = Range(top, scale, inside, kBins - 1).above;
+        const int each = (n + NT - 1) / NT | 1, begin = min((int)threadIdx.x * each, n), end = min(begin + each, n);
+        double above = 0.0;
+        uint32_t mine = 0, total;
+        __syncthreads();
+        for (int i = begin; i < end; ++i) {
+            const bool in = logit_of(list[i]) >= sure;
+            if (in) above += w[i];
+            mine += !in;
         }
-        const double t = target(u, total);
-        // the first entry beyond t, of those kept
-        int at = 0;
-        for (int step = MOST / 2; step > 0; step >>= 1)
-            if (at + step <= n - 1 && upto_of[at + step - 1] <= t) at += step;
-        if (lane == 0) {
-            int back = at;
-            while (back >= 0 && list[back] < least) --back;         // (within a rounding of the sums)
-            while (back < 0 && list[at] < least) ++at;
-            const uint64_t x = list[back >= 0 ? back : at];
-            put_draw(a, row, d, token_of(x), ((double)logit_of(x) - (double)top) / (double)set.T - log_total);
+        uint32_t at = before<NT>(mine, &total, reinterpret_cast<uint32_t *>(sums));
+        if (total > (uint32_t)most) return false;
+        above = over_cta<NT>(above, add, sums);    // (barriers)
+        for (int i = begin; mine && i < end; ++i)
+            if (logit_of(list[i]) < sure) {
+                near[at] = list[i];
+                near_mass[at++] = w[i];
+            }
+        __syncthreads();
+        // an entry stays while what is larger has less than the goal; the least one that does, or none of these
+        const double goal = (double)set.p * whole;
+        uint64_t e = ~0ull;
+        if (threadIdx.x < total) {
+            const uint64_t own = near[threadIdx.x];
+            double upto = above;
+#pragma unroll 4
+            for (int i = 0; i < (int)total; ++i) upto += near[i] > own ? near_mass[i] : 0.0;
+            if (upto < goal) e = own;
         }
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) e = min(e, (uint64_t)__shfl_xor_sync(kFull, (unsigned long long)e, o));
+        uint64_t *least_of = reinterpret_cast<uint64_t *>(sums);
+        if (lane == 0) least_of[warp] = e;
+        __syncthreads();
+        uint64_t least = ~0ull;
+#pragma unroll
+        for (int v = 0; v < NT / 32; ++v) least = min(least, least_of[v]);
+        for (int i = begin; i < end; ++i)
+            if (list[i] < least && logit_of(list[i]) < sure) w[i] = 0.0;
     }
+    draw_kept<NT, MOST>(list, w, upto_of, sums, a, row, set, n, top);
+    return true;
 }
 
 // Draws of all tokens that the cut keeps and that have at least m of the largest one's mass, each CTA its share's.
@@ -711,7 +773,8 @@ __device__ void draw_cut(const SampleArgs &a, float4 *mem, Shared &sh) {
         n = list_top(r, set.k, &finer);
     }
     if (n >= 0) {
-        if (rank == 0)
+        if (rank == 0 && (set.k || !draw_prefix<kThreads, kList>(r.list, r.tmp(), sh.sums, reinterpret_cast<uint64_t *>(sh.hist), kNear, a, row, set, n,
+                                                                 whole_mass, mass, r.top, scale, inside)))
             draw_listed<kThreads, kList>(r.list, r.tmp(), sh.sums, sh.hist[0].count, reinterpret_cast<uint32_t *>(sh.scan), a, row, set, n,
                                          whole_mass, mass, r.top, finer);
         return;
