@@ -8,7 +8,7 @@
 //     batch that the target falls into is read again.  Top-k up to a few hundred (and with it top-p and min-p), or the largest logit: the k
 //     largest logits come to a list in one CTA, sorted, and all the rest is done there.
 //   k_draw_cut: the other rows.  A cluster of 1 to 8 CTAs brings the row into shared memory once; every later step reads it there.
-//     Larger top-k: each thread has the largest of its words; the k-th largest of those maxima (by bins) is at or below the k-th largest
+//     Larger top-k: the k-th largest of the words' maxima (by bins) is at or below the k-th largest
 //     logit, and little more than k tokens reach it.  Top-p, min-p: a histogram of masses by bins of the logit, rounded down a little, says which
 //     bins certainly hold the prefix.  These tokens go to a list in one CTA, as above; where they are too many for it, those of the bins
 //     that the cut may lie in do, and all CTAs draw from their shares.
@@ -22,8 +22,11 @@ namespace rows {
 namespace {
 
 static_assert(kBins == kThreads, "a thread for each bin");
-constexpr int kTop = DSBD_MAX_TOP;                 // tokens that a cut by list keeps, at most
-constexpr int kList = 4 * kTop;                    // entries of the list
+constexpr int kList = 4096;                        // entries of the list
+// Top-k that a cut by list takes, at most.  Beyond that it is longer than the list often; and in bf16 many logits are equal, which is what
+// putting it in order suffers from (64 rows of 32000, top-k 1500: 40 us, by bins 34; fp32 of 128256, top-k 2000: 53, by bins 76).
+template <class T>
+constexpr int kTop = sizeof(T) == 4 ? 2048 : 1024;
 constexpr int kNear = 256;                         // entries that are compared with one another
 
 struct SampleArgs {
@@ -81,7 +84,6 @@ struct Row {
     int room, ctas, rank, V;
     int note_turn, hist_turn;
     float top, low;                                // the largest logit; the smallest of the threads' finite maxima
-    float mine;                                    // this thread's maximum
 
     // (rank 0, which needs its share no more once the list is whole)
     __device__ __forceinline__ uint64_t *tmp() const { return reinterpret_cast<uint64_t *>(const_cast<float4 *>(mem)); }
@@ -111,7 +113,6 @@ __device__ __forceinline__ bool bring(Row<T> &r, const T *row, float4 *mem, int3
             bad |= !(x[e] < CUDART_INF_F);
         }
     });
-    r.mine = high;
     Note n = {0.0, high, high > -CUDART_INF_F ? high : CUDART_INF_F, bad, 0};
     n = over_cta(n, join_top, r.sh.scratch);
     begun_wait(r.ctas);
@@ -468,7 +469,7 @@ __device__ bool cut_in_bins(Row<T> &r, float scale, int first, int last, double 
     return true;
 }
 
-// The tokens at or above the k-th largest logit, listed as in list_range.  k <= kTop; fewer than k where the row has fewer above -inf.
+// The tokens at or above the k-th largest logit, listed as in list_range.  k <= kTop<T>; fewer than k where the row has fewer above -inf.
 template <class T>
 __device__ int list_top(Row<T> &r, int k, float *finer) {
     Shared &sh = r.sh;
@@ -476,7 +477,15 @@ __device__ int list_top(Row<T> &r, int k, float *finer) {
     Hist &h = sh.hist[r.hist_turn++ & 1];
     clear<false>(h);
     if (threadIdx.x == 0) sh.picked_bin = kBins - 1;
-    if (r.mine > -CUDART_INF_F) atomicAdd(&h.count[bin_below(r.top, r.mine, scale)], 1u);
+    // (a maximum of each thread instead: no faster where the list holds what reaches it, and it mostly does not where the threads are not some
+    // times k: 512 rows of 32000 bf16, one CTA each, top-k 600: 109 us, so 54)
+    for (int w = threadIdx.x; w < r.s.words; w += kThreads) {
+        float x[kPer<T>], most = -CUDART_INF_F;
+        unpack(r.mem[w], x);
+#pragma unroll
+        for (int e = 0; e < kPer<T>; ++e) most = fmaxf(most, x[e]);
+        if (most > -CUDART_INF_F) atomicAdd(&h.count[bin_below(r.top, most, scale)], 1u);
+    }
     cluster_barrier(r.ctas);
     uint64_t total;
     const uint64_t n = bin_count(r, h), excl = before(n, &total, sh.scan);
@@ -753,7 +762,7 @@ __device__ void draw_cut(const SampleArgs &a, float4 *mem, Shared &sh) {
     if (settings_of(a, row, set) != kCut) return;
     begun_arrive(a.ctas);
     const T *at = static_cast<const T *>(a.logits) + (int64_t)row * a.stride;
-    Row<T> r = {share<T>(at, a.V, rank, a.per), mem, sh, reinterpret_cast<uint64_t *>(mem + a.words), a.list_room, a.ctas, rank, a.V, 0, 0, 0.f, 0.f, 0.f};
+    Row<T> r = {share<T>(at, a.V, rank, a.per), mem, sh, reinterpret_cast<uint64_t *>(mem + a.words), a.list_room, a.ctas, rank, a.V, 0, 0, 0.f, 0.f};
     Mass::fill(sh.table);
     if (!bring<T>(r, at, mem, a.status)) {
         if (rank == 0)
@@ -769,7 +778,7 @@ __device__ void draw_cut(const SampleArgs &a, float4 *mem, Shared &sh) {
     if (set.k == 0) {
         n = list_mass(r, set.p, set.m, set.T, mass, &whole_mass, &scale, &inside, &last);
         finer = scale * ((float)kBins / (float)(last + 1));
-    } else if (set.k <= kTop) {
+    } else if (set.k <= kTop<T>) {
         n = list_top(r, set.k, &finer);
     }
     if (n >= 0) {
