@@ -1,7 +1,7 @@
 // Distillation of rows of logits from a teacher's entries, loss and gradient in one pass.
 //
-// A row belongs to a cluster of 1 to 8 CTAs, each of which reads its share for the sums and again for the gradient, the first part from shared
-// memory, the rest while it is still in the L2.
+// A row belongs to a cluster of 1 to 8 CTAs, each of which reads its share for the sums and again for the gradient: the last part from registers, the
+// first from shared memory, the rest while it is still in the L2.
 //
 // The tokens that the teacher names are marked by bits.  The others' softmax has a reference of its own (their largest logit):
 // beside a named token of nearly all the mass their sum would vanish in 32 bits, and with it the loss's last term.  Terms of the
@@ -66,18 +66,19 @@ __device__ __forceinline__ void put_share(T *row, const Share &s, F f) {
     }
 }
 
-// MINE entries of a thread: k = threadIdx.x + i * NT.  RESIDENT CTAs of an SM.
+// MINE entries of a thread: k = threadIdx.x + i * NT.  RESIDENT CTAs of an SM.  GRAD: with the gradient (the losses alone leave the
+// registers of its last batch free: one text for both 1022 us for 4608 rows of 128256 fp32, 19.3 for 517 of 50257 bf16 without, so 999 and 18.4).
 //
-// One reading and one writing of the logits are what it has to do: 4608 rows of 128256 fp32 1069 us, 4.4 TB/s in both directions together, of
-// 723 at the copy rate; 2048 rows in bf16 304 us of 161.  What holds it up is a CTA's chain (some 12000 cycles: the teacher, the first words, two
+// One reading and one writing of the logits are what it has to do: 4608 rows of 128256 fp32 999 us, 4.7 TB/s in both directions together, of
+// 723 at the copy rate; 2048 rows in bf16 267 us of 161.  What holds it up is a CTA's chain (some 12000 cycles: the teacher, the first words, two
 // exchanges, 64-bit sums), which the SM's other CTAs cover in part, and the second reading, from the L2 for what is not held in shared memory.  (Held:
 // all of it leaves one CTA of an SM, less is slower in the L2; rows' loads begun a row ahead, 1 to 8 rows a cluster: no gain; 512 threads: slower.)
-// Without a gradient one reading: 517 rows of 50257 bf16 18.6 us of 8.
+// Without a gradient one reading: 517 rows of 50257 bf16 18.4 us of 8.
 //
 // 64-bit chains are kept short and off the others' way (a dependent step takes some 40 cycles, a logarithm more than a thousand): the teacher's
 // exponentials run while the first words are on their way, the student's sums are joined by lanes side by side, and logarithms are
 // for the loss alone, which one CTA works out behind its share of the gradient.
-template <class T, int MINE, int RESIDENT>
+template <class T, int MINE, int RESIDENT, bool GRAD>
 __global__ void __launch_bounds__(NT, RESIDENT) k_distill(DistillArgs a) {
     constexpr int P = kPer<T>, D = kDeep<T>;
     extern __shared__ float4 mem[];
@@ -89,7 +90,7 @@ __global__ void __launch_bounds__(NT, RESIDENT) k_distill(DistillArgs a) {
     const int row = blockIdx.x / a.ctas, rank = blockIdx.x - row * a.ctas;
     uint32_t *named = reinterpret_cast<uint32_t *>(mem + a.held);      // a bit for each element of the share's words
     const T *z_row = static_cast<const T *>(a.logits) + (int64_t)row * a.stride;
-    T *g_row = a.grad ? static_cast<T *>(a.grad) + (int64_t)row * a.grad_stride : nullptr;
+    T *g_row = GRAD ? static_cast<T *>(a.grad) + (int64_t)row * a.grad_stride : nullptr;
     const Share s = share<T>(z_row, a.V, rank, a.per);
     const float weight = a.weight ? a.weight[row] : 1.f;
     const float *value = a.value + (int64_t)row * a.K;
@@ -104,7 +105,7 @@ __global__ void __launch_bounds__(NT, RESIDENT) k_distill(DistillArgs a) {
         t[i] = k < a.K ? value[k] : -CUDART_INF_F;
     }
     auto no_gradient = [&] {
-        if (g_row) put_share<T>(g_row, s, [](int, float (&g)[P]) {
+        if constexpr (GRAD) put_share<T>(g_row, s, [](int, float (&g)[P]) {
 #pragma unroll
             for (int e = 0; e < P; ++e) g[e] = 0.f;
         });
@@ -258,7 +259,7 @@ __global__ void __launch_bounds__(NT, RESIDENT) k_distill(DistillArgs a) {
     }
     const double per_whole = inverse_of(whole), per_teacher = inverse_of(teacher);
     // ---- the gradient: the others', then the named tokens' over it
-    if (g_row) {
+    if constexpr (GRAD) {
         const double q = others_top * per_whole;
         const float factor_f = rest_sum != 0.0 ? (float)((double)weight * a.temperature * (a.rest ? q - e_rest * per_teacher : q) * inverse_of(rest_sum)) : 0.f;
         if (base == -CUDART_INF_F) base = 0.f;
@@ -274,8 +275,13 @@ __global__ void __launch_bounds__(NT, RESIDENT) k_distill(DistillArgs a) {
         if (((reinterpret_cast<uintptr_t>(g_row) ^ reinterpret_cast<uintptr_t>(z_row)) & 15) == 0) {
             // words of the gradient lie as the logits' do
             float4 *to = reinterpret_cast<float4 *>(g_row + s.first - s.mis);
-            for (int w0 = 0; w0 < s.words; w0 += D * NT) {
-                if (w0 + D * NT <= a.held) {
+            // backwards, from the batch that is still in registers on, so that what was read last is read again first (4608 rows of 128256 fp32: 1069
+            // us, so 1022)
+            const int last = s.words > 0 ? (s.words - 1) / (D * NT) * (D * NT) : -1;
+            for (int w0 = last; w0 >= 0; w0 -= D * NT) {
+                if (w0 == last) {
+                    // (in raw)
+                } else if (w0 + D * NT <= a.held) {
 #pragma unroll
                     for (int u = 0; u < D; ++u) raw[u] = mem[batch_word<D>(w0, u)];
                 } else {
@@ -350,18 +356,21 @@ inline Plan plan_distill(const dsbd_rows_t *r, int resident) {
     return p;
 }
 
-template <class T, int RESIDENT>
+template <class T, int RESIDENT, bool GRAD>
 int run_distill(const dsbd_rows_t *r, DistillArgs &a, dsbd_stream_t stream) {
     constexpr int kBatch = NT * kDeep<T>;
     const Plan p = plan_distill(r, RESIDENT);
     a.ctas = p.ctas;
     a.per = p.per;
-    // whole batches of 32 elements a thread; without a gradient nothing is read twice
-    const int batches = (p.per / kPer<T> + 1 + kBatch - 1) / kBatch;
-    a.held = a.grad ? std::min(batches, 48 * 1024 / 16 / kBatch) * kBatch : 0;
-    const size_t bytes = (size_t)a.held * 16 + (size_t)batches * NT * 4;
-    return a.K <= NT ? launch<NT>(k_distill<T, 1, RESIDENT>, r->rows, p, bytes, a, stream)
-                     : launch<NT>(k_distill<T, DSBD_MAX_TOP / NT, RESIDENT>, r->rows, p, bytes, a, stream);
+    // whole batches of 32 elements a thread, as many as leave room for RESIDENT CTAs in an SM's 228 KB, of which each takes 1 more (2048 rows of 128256 bf16:
+    // three batches and three CTAs 306 us, two and four
+    // 280), but the last, which stays in registers; without a gradient nothing is read twice
+    const int batches = (p.per / kPer<T> + 1 + kBatch - 1) / kBatch, marks = batches * NT * 4;
+    const int room = 228 * 1024 / RESIDENT - 1024 - (int)sizeof(Shared) - marks;
+    a.held = GRAD ? std::min(batches - 1, std::min(room, 48 * 1024) / 16 / kBatch) * kBatch : 0;
+    const size_t bytes = (size_t)a.held * 16 + (size_t)marks;
+    return a.K <= NT ? launch<NT>(k_distill<T, 1, RESIDENT, GRAD>, r->rows, p, bytes, a, stream)
+                     : launch<NT>(k_distill<T, DSBD_MAX_TOP / NT, RESIDENT, GRAD>, r->rows, p, bytes, a, stream);
 }
 
 }  // namespace
@@ -388,6 +397,7 @@ extern "C" int dsbd_distill(const dsbd_rows_t *rows, const dsbd_distill_params_t
     a.loss = loss; a.grad = grad; a.grad_stride = grad_stride; a.status = status;
     // Four CTAs of an SM where their registers last (517 rows of 50257 bf16 without gradients 18.2 us, with three 23.1); with gradients in fp32
     // three (20 rows of 32000 6.1 us, with four and what they spill 7.2; 4608 of 128256 1060 and 1066).
-    if (rows->dtype == DSBD_DTYPE_BF16) return run_distill<__nv_bfloat16, 4>(rows, a, stream);
-    return grad ? run_distill<float, 3>(rows, a, stream) : run_distill<float, 4>(rows, a, stream);
+    if (rows->dtype == DSBD_DTYPE_BF16)
+        return grad ? run_distill<__nv_bfloat16, 4, true>(rows, a, stream) : run_distill<__nv_bfloat16, 4, false>(rows, a, stream);
+    return grad ? run_distill<float, 3, true>(rows, a, stream) : run_distill<float, 4, false>(rows, a, stream);
 }
