@@ -343,7 +343,8 @@ __global__ void __launch_bounds__(NT, RESIDENT) k_distill(DistillArgs a) {
 }
 
 // CTAs of a row: shares of up to 128 KB (a CTA's fixed chain, some 12000 cycles, counts for less than with smaller ones; with larger
-// ones the rows under way outgrow the L2, from which what is not held is read again), and more where the SMs would stand idle.
+// ones the rows under way outgrow the L2, from which what is not held is read again: 2048 rows of 128256 bf16, two CTAs each 267 us, one
+// 306), and more where the SMs would stand idle.
 inline Plan plan_distill(const dsbd_rows_t *r, int resident) {
     const int size = r->dtype == DSBD_DTYPE_F32 ? 4 : 2;
     Plan p;
@@ -395,8 +396,8 @@ extern "C" int dsbd_distill(const dsbd_rows_t *rows, const dsbd_distill_params_t
     a.inverse = 1.0 / (double)p->temperature;
     a.value = p->value; a.index = p->index; a.rest = p->rest; a.weight = p->weight;
     a.loss = loss; a.grad = grad; a.grad_stride = grad_stride; a.status = status;
-    // Four CTAs of an SM where their registers last (517 rows of 50257 bf16 without gradients 18.2 us, with three 23.1); with gradients in fp32
-    // three (20 rows of 32000 6.1 us, with four and what they spill 7.2; 4608 of 128256 1060 and 1066).
+    // Four CTAs of an SM where their registers last (517 rows of 50257 bf16 without gradients 18.2 us, with three 23.1; 2048 of 128256 with gradients
+    // 267 and 284); with gradients in fp32 three (20 rows of 32000 6.5 us, with four and what they spill 7.7; 4608 of 128256 999 and 1001).
     if (rows->dtype == DSBD_DTYPE_BF16)
         return grad ? run_distill<__nv_bfloat16, 4, true>(rows, a, stream) : run_distill<__nv_bfloat16, 4, false>(rows, a, stream);
     return grad ? run_distill<float, 3, true>(rows, a, stream) : run_distill<float, 4, false>(rows, a, stream);
