@@ -597,7 +597,8 @@ int dsbd_sample_rows(const dsbd_rows_t *rows, const dsbd_sample_params_t *params
 
 /* The K largest logits of each row in falling order, of equal ones the lower token first: value [rows, K] fp32, index [rows, K];
  * rest [rows] or NULL: log of the sum of exp(z / temperature) over the row's other tokens (-inf where there are none, or all of them
- * are masked).  Where fewer than K tokens are above -inf the first ones at -inf follow.  1 <= K <= min(V, DSBD_MAX_TOP), temperature > 0.
+ * are masked).  Where fewer than K tokens are above -inf the first ones at -inf follow.  1 <= K <= min(V, DSBD_MAX_TOP).  temperature: normal
+ * (2^-126 or more), at most 2^100.
  * *status: DSBD_DEV_BAD_LOGIT, DSBD_DEV_EXHAUSTED as above; such a row gets index -1, value and rest NaN. */
 int dsbd_top_logits(const dsbd_rows_t *rows, int32_t K, float temperature, float *value, int32_t *index, float *rest,
                     int32_t *status, dsbd_stream_t stream);
@@ -616,7 +617,7 @@ int dsbd_top_logits(const dsbd_rows_t *rows, int32_t K, float temperature, float
  * entries, are nothing but -inf or not there: its loss and gradient are 0. */
 typedef struct {
     int32_t K;
-    float temperature;             /* > 0                                                    */
+    float temperature;             /* 2^-126 .. 2^100                                        */
     const float *value;
     const int32_t *index;
     const float *rest;             /* [rows] or NULL                                         */

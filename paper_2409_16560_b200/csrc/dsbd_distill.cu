@@ -165,7 +165,7 @@ __global__ void __launch_bounds__(NT, RESIDENT) k_distill(DistillArgs a) {
     }
     // ---- the student's sums
     const double scale = 1.4426950408889634 * a.inverse;
-    const float scale_f = fminf((float)scale, FLT_MAX);                 // (0 times it stays 0)
+    const float scale_f = (float)scale;
     Rest others;
     for (int w0 = 0; w0 < s.words;) {
         // the warp's 1024 elements of the batch have 32 words of marks
@@ -384,7 +384,7 @@ extern "C" int dsbd_distill(const dsbd_rows_t *rows, const dsbd_distill_params_t
                             int32_t *status, dsbd_stream_t stream) {
     int rc = check_rows(rows);
     if (rc) return rc;
-    if (!p || p->K <= 0 || p->K > rows->V || !(p->temperature > 0.f && p->temperature <= FLT_MAX) || !status) return DSBD_ERR_INVALID_ARG;
+    if (!p || p->K <= 0 || p->K > rows->V || !scales(p->temperature) || !status) return DSBD_ERR_INVALID_ARG;
     if (grad && rows->rows > 1 && grad_stride < rows->V) return DSBD_ERR_INVALID_ARG;
     const int size = rows->dtype == DSBD_DTYPE_F32 ? 4 : 2;
     if (p->K > DSBD_MAX_TOP || (reinterpret_cast<uintptr_t>(grad) & (size - 1))) return DSBD_ERR_UNSUPPORTED;

@@ -343,7 +343,8 @@ struct Mass {
     }
     __device__ __forceinline__ void relative_to(float top) {
         this->top = (double)top;
-        least = top > -CUDART_INF_F ? (float)((double)top - reach) : CUDART_INF_F;      // (nothing: 0)
+        // (nothing: 0; -inf at no temperature)
+        least = top > -CUDART_INF_F ? fmaxf((float)((double)top - reach), -FLT_MAX) : CUDART_INF_F;
     }
     // z <= top, not -inf
     __device__ __forceinline__ double at(float z) const {
@@ -500,6 +501,9 @@ inline int check_rows(const dsbd_rows_t *r) {
     if ((reinterpret_cast<uintptr_t>(r->logits) & (size - 1)) || (int64_t)r->V * size > DSBD_MAX_ROW_BYTES) return DSBD_ERR_UNSUPPORTED;
     return r->rows > INT_MAX / kMaxCtas ? DSBD_ERR_UNSUPPORTED : DSBD_OK;
 }
+
+// Temperatures for sums in 32 bits: below, 1 / T overflows; above, a difference of two logits may overflow that is still worth something.
+inline bool scales(float T) { return T >= FLT_MIN && T <= 0x1p100f; }
 
 // CTAs of a row and their shares, in elements.
 struct Plan {

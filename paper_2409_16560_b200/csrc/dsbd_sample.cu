@@ -305,7 +305,7 @@ struct Range {
     __device__ Range(float top, float scale, int first, int last) {
         const float wide = (float)(last + 1) / scale, near = (float)first / scale;
         from = last < kBins - 1 && scale > 0.f ? fmaxf(top - wide - 4.8e-7f * (fabsf(top) + wide), -FLT_MAX) : -FLT_MAX;
-        above = first ? top - near + 4.8e-7f * (fabsf(top) + near) : CUDART_INF_F;
+        above = first ? fmaxf(top - near, -FLT_MAX) + 4.8e-7f * (fabsf(top) + near) : CUDART_INF_F;
     }
 };
 

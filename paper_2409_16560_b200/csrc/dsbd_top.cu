@@ -40,7 +40,7 @@ __global__ void __launch_bounds__(NT, CTAS) k_top(TopArgs a) {
     float *value_out = a.value + (int64_t)row * a.K;
     int32_t *index_out = a.index + (int64_t)row * a.K;
     const double scale = 1.4426950408889634 / (double)a.temperature;
-    const float scale_f = fminf((float)scale, FLT_MAX);                 // (0 times it stays 0)
+    const float scale_f = (float)scale;
     Rest rest;
     Sum cleared = {-CUDART_INF_F, 0.0};
     const bool good = collect<T, true>(sh, at, share<T>(at, a.V, rank, a.per), (uint32_t)a.K, a.ctas > 1, scale_f, rest, cleared);
@@ -154,7 +154,7 @@ extern "C" int dsbd_top_logits(const dsbd_rows_t *rows, int32_t K, float tempera
                                int32_t *status, dsbd_stream_t stream) {
     int rc = check_rows(rows);
     if (rc) return rc;
-    if (K <= 0 || K > rows->V || !(temperature > 0.f && temperature <= FLT_MAX) || !status) return DSBD_ERR_INVALID_ARG;
+    if (K <= 0 || K > rows->V || !scales(temperature) || !status) return DSBD_ERR_INVALID_ARG;
     if (K > DSBD_MAX_TOP) return DSBD_ERR_UNSUPPORTED;
     if (rows->rows == 0) return DSBD_OK;
     if (!rows->logits || !value || !index) return DSBD_ERR_INVALID_ARG;

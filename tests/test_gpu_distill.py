@@ -89,6 +89,16 @@ def test_temperatures(T, rest):
     check(q, T, grad=False)
 
 
+@pytest.mark.parametrize("T", [2.0 ** -40, 2.0 ** 40])
+@pytest.mark.parametrize("dtype", [F32, BF])
+def test_logits_of_the_temperature_s_size(T, dtype):
+    """Powers of two scale everything but the rest: p and q are those of a temperature of 1, the loss T^2 and the gradient T times theirs."""
+    q = problem(3, 9000, 50, dtype, seed=6)
+    loss, g = check(q)
+    scaled = dsbd.distill(q["z"] * T, q["value"] * T, q["index"], rest=q["rest"], weight=q["weight"], temperature=T)
+    assert torch.equal(scaled[0], loss * T * T) and torch.equal(scaled[1], g * T)
+
+
 @pytest.mark.parametrize("V,dtype", [(262144, F32), (393216, F32), (786432, BF)])
 def test_long_rows(V, dtype):
     check(problem(2, V, 100, dtype, seed=V, start=1))

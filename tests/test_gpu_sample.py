@@ -85,6 +85,27 @@ def test_prefixes_longer_than_a_list(V, dtype, spread):
         check(z, u, T, 0, p, m)
 
 
+@pytest.mark.parametrize("dtype", [F32, BF])
+@pytest.mark.parametrize("k,p,m", [(600, 1.0, 0.0), (1000, 0.9, 0.0), (1500, 0.95, 0.0), (2500, 1.0, 0.01), (0, 0.9, 0.0), (0, 0.99, 0.3), (0, 1.0, 0.05)])
+def test_many_short_rows(dtype, k, p, m):
+    """Rows of one CTA each, with fewer threads than a top-k has tokens, some of them masked to less than that."""
+    z = ru.rows_of(160, 9001, dtype, seed=k + 3, pad=2, zipf=False)
+    z[::7, 300:] = -math.inf
+    z[1::7, 1::2] = -math.inf
+    check(z, uniform(160, 2, 4), 1.2, k, p, m)
+
+
+@pytest.mark.parametrize("T", [1e36, 3e37, 1e38])
+def test_temperatures_of_the_largest_logits_size(T):
+    z = ru.rows_of(4, 9000, F32, seed=8, spread=1.0)
+    z[1] *= 1e37
+    z[2] = z[2] * 1e37 - 3e38
+    z[3, ::3] = torch.finfo(F32).min
+    z = z.clamp(torch.finfo(F32).min)
+    for k, p, m in [(0, 1.0, 0.0), (20, 0.9, 0.0), (0, 0.9, 0.0), (0, 0.3, 0.9), (2000, 0.9, 0.1)]:
+        check(z, uniform(4, 5, 6), T, k, p, m)
+
+
 @pytest.mark.parametrize("T", [1e-30, 1e-36, 1e-38, 1e-40])
 def test_temperatures_that_leave_no_scale(T):
     """Differences of the logits over the temperature: beyond fp32, or of ordinary size where the logits are as small."""

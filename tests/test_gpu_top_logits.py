@@ -55,6 +55,15 @@ def test_temperatures(T):
     check(ru.rows_of(3, 20000, F32, seed=2), 64, T)
 
 
+@pytest.mark.parametrize("T", [2.0 ** -126, 1e-30, 1e20, 2.0 ** 100])
+def test_temperatures_of_every_size(T):
+    """Ordinary logits where T is large, with a mask of the type's lowest value, and logits of T's size."""
+    z = ru.rows_of(4, 5000, F32, seed=4)
+    z[2:] = (z[2:].double() * T).float()
+    z[1, ::2] = torch.finfo(F32).min
+    check(z if T > 1 else z[2:], 20, T)
+
+
 @pytest.mark.parametrize("V,dtype", [(262144, F32), (393216, F32), (786432, BF)])
 def test_long_rows(V, dtype):
     check(ru.rows_of(2, V, dtype, seed=V, start=3), 200)

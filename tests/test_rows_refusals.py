@@ -64,3 +64,10 @@ def test_distill_settings():
         assert distill(rows(), **bad) == INVALID, bad
     assert distill(rows(V=5000, stride=5000), K=1025, stride=5000) == UNSUPPORTED
     assert distill(rows(), grad=AT + 2) == UNSUPPORTED and distill(rows(dtype=DTYPE_BF16), grad=AT + 1) == UNSUPPORTED
+
+
+def test_temperatures_that_sums_in_32_bits_do_not_reach():
+    for T in (2.0 ** -127, 1e-40, 2.0 ** 101, 3e38):
+        assert top(rows(), T=T) == INVALID and distill(rows(), temperature=T) == INVALID
+    for T in (2.0 ** -126, 2.0 ** 100):
+        assert top(rows(n=0), T=T) == OK and distill(rows(n=0), temperature=T) == OK
