@@ -408,7 +408,8 @@ __device__ int list_mass(Row<T> &r, float p, float m, float T_, const Mass &mass
         // (the bins' sums are at most 7e-5 too small)
         const double goal = (double)p * sum;
         if (upto < goal * (1.0 + 1e-4) && upto + v >= goal * (1.0 + 1e-4)) sh.picked_bin = threadIdx.x;
-        *inside = __syncthreads_count((upto + v) * (1.0 + 1e-4) < goal);
+        // (the last bin has no masses: what lies there, and further down, is never certain)
+        *inside = __syncthreads_count(threadIdx.x < kBins - 1 && (upto + v) * (1.0 + 1e-4) < goal);
         last = min(last, (int)sh.picked_bin);
     }
     *scale_out = scale;
