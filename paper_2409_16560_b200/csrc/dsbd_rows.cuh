@@ -343,8 +343,9 @@ struct Mass {
     }
     __device__ __forceinline__ void relative_to(float top) {
         this->top = (double)top;
-        // (nothing: 0; -inf at no temperature)
-        least = top > -CUDART_INF_F ? fmaxf((float)((double)top - reach), -FLT_MAX) : CUDART_INF_F;
+        // (nothing: 0; -inf at no temperature.  Rounded up: where logits lie further apart than reach, the number below it would let one through
+        // whose exponent leaves the range)
+        least = top > -CUDART_INF_F ? fmaxf(__double2float_ru((double)top - reach), -FLT_MAX) : CUDART_INF_F;
     }
     // z <= top, not -inf
     __device__ __forceinline__ double at(float z) const {
