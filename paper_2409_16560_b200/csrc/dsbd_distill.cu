@@ -359,7 +359,8 @@ inline Plan plan_distill(const dsbd_rows_t *r, int resident) {
 
 template <class T, int RESIDENT, bool GRAD>
 int run_distill(const dsbd_rows_t *r, DistillArgs &a, dsbd_stream_t stream) {
-    constexpr int kBatch = NT * kDeep<T>;
+    constexpr int kBatch = NT * kDeep<T>, kHeld = 48 * 1024;
+    constexpr int kMost = kHeld + (kLongestShare + kBatch - 1) / kBatch * NT * 4;
     const Plan p = plan_distill(r, RESIDENT);
     a.ctas = p.ctas;
     a.per = p.per;
@@ -368,10 +369,10 @@ int run_distill(const dsbd_rows_t *r, DistillArgs &a, dsbd_stream_t stream) {
     // 280), but the last, which stays in registers; without a gradient nothing is read twice
     const int batches = (p.per / kPer<T> + 1 + kBatch - 1) / kBatch, marks = batches * NT * 4;
     const int room = 228 * 1024 / RESIDENT - 1024 - (int)sizeof(Shared) - marks;
-    a.held = GRAD ? std::min(batches - 1, std::min(room, 48 * 1024) / 16 / kBatch) * kBatch : 0;
+    a.held = GRAD ? std::min(batches - 1, std::min(room, kHeld) / 16 / kBatch) * kBatch : 0;
     const size_t bytes = (size_t)a.held * 16 + (size_t)marks;
-    return a.K <= NT ? launch<NT>(k_distill<T, 1, RESIDENT, GRAD>, r->rows, p, bytes, a, stream)
-                     : launch<NT>(k_distill<T, DSBD_MAX_TOP / NT, RESIDENT, GRAD>, r->rows, p, bytes, a, stream);
+    return a.K <= NT ? launch<kMost, NT>(k_distill<T, 1, RESIDENT, GRAD>, r->rows, p, bytes, a, stream)
+                     : launch<kMost, NT>(k_distill<T, DSBD_MAX_TOP / NT, RESIDENT, GRAD>, r->rows, p, bytes, a, stream);
 }
 
 }  // namespace

@@ -537,9 +537,15 @@ inline Plan plan_waves(const dsbd_rows_t *r, int slots, int fixed, int least, in
     return p;
 }
 
-template <int NT = kThreads, class Args>
+// 16-byte words of the longest share, of a row of DSBD_MAX_ROW_BYTES in kMaxCtas CTAs.
+constexpr int kLongestShare = DSBD_MAX_ROW_BYTES / kMaxCtas / 16 + 1;
+
+// MOST: the most that any call asks of the kernel's dynamic shared memory.  The limit is the whole process's, so it is this for every call: between
+// one thread's setting and its launch another thread may set it for a row of its own.
+template <int MOST, int NT = kThreads, class Args>
 int launch(void (*kernel)(Args), int rows, const Plan &p, size_t bytes, const Args &a, dsbd_stream_t stream) {
-    if (bytes > 16 * 1024 && cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes) != cudaSuccess) {
+    if (bytes > (size_t)MOST ||
+        (bytes > 16 * 1024 && cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, MOST) != cudaSuccess)) {
         cudaGetLastError();
         return DSBD_ERR_CUDA;
     }

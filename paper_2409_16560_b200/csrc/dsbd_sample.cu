@@ -15,6 +15,8 @@
 //     Where the list does not hold these either: a histogram of 512 bins over the cluster, linear in the logit first, then in the bits of the
 //     keys of the bin that the cut is in, until that is one key; equal keys go by token.  Masses are then whole numbers (2^62 / V' of the
 //     largest token's mass, V' the power of two from V on), so sums do not depend on their order.  Then the draw over all shares.
+#include <algorithm>
+
 #include "dsbd_top.cuh"
 
 namespace dsbd {
@@ -1161,6 +1163,11 @@ __global__ void __launch_bounds__(kOnce, kOnceResident) k_draw(SampleArgs a) {
     draw_few(sh, a, row, set);
 }
 
+// k_draw_cut: the longest share with a whole list beside it, in 16-byte words; the most shared memory of a CTA.
+constexpr int kWholeList = 160 * 1024 / 16;
+constexpr int kCutBytes = std::max(kWholeList * 16 + kList * 8, kLongestShare * 16 + kList / 2 * 8);
+static_assert(kWholeList >= kList && kCutBytes + sizeof(Shared) <= 227 * 1024, "");
+
 // CTAs of a row in k_draw: lists of up to K entries and a half more from each.
 inline Plan plan_once(const dsbd_rows_t *r, int K) {
     int most = kMaxCtas;
@@ -1201,8 +1208,8 @@ extern "C" int dsbd_sample_rows(const dsbd_rows_t *rows, const dsbd_sample_param
         const Plan plan = plan_once(rows, p->top_k_r ? kShareTop : k_off ? 1 : p->top_k < kOnceTop ? p->top_k : kOnceTop);
         a.ctas = plan.ctas;
         a.per = plan.per;
-        rc = rows->dtype == DSBD_DTYPE_F32 ? launch<kOnce>(k_draw<float>, rows->rows, plan, sizeof(DrawShared), a, stream)
-                                           : launch<kOnce>(k_draw<__nv_bfloat16>, rows->rows, plan, sizeof(DrawShared), a, stream);
+        rc = rows->dtype == DSBD_DTYPE_F32 ? launch<sizeof(DrawShared), kOnce>(k_draw<float>, rows->rows, plan, sizeof(DrawShared), a, stream)
+                                           : launch<sizeof(DrawShared), kOnce>(k_draw<__nv_bfloat16>, rows->rows, plan, sizeof(DrawShared), a, stream);
         if (rc) return rc;
     }
     if (!cut) return DSBD_OK;
@@ -1211,9 +1218,9 @@ extern "C" int dsbd_sample_rows(const dsbd_rows_t *rows, const dsbd_sample_param
     a.ctas = plan.ctas;
     a.per = plan.per;
     // the share, where the list is put in order and its masses are later, and the list; half as long beside the longest shares
-    a.list_room = plan.words <= 160 * 1024 / 16 ? kList : kList / 2;
+    a.list_room = plan.words <= kWholeList ? kList : kList / 2;
     a.words = plan.words > kList ? plan.words : kList;
     const size_t bytes = (size_t)a.words * 16 + (size_t)a.list_room * 8;
-    return rows->dtype == DSBD_DTYPE_F32 ? launch(k_draw_cut<float>, rows->rows, plan, bytes, a, stream)
-                                         : launch(k_draw_cut<__nv_bfloat16>, rows->rows, plan, bytes, a, stream);
+    return rows->dtype == DSBD_DTYPE_F32 ? launch<kCutBytes>(k_draw_cut<float>, rows->rows, plan, bytes, a, stream)
+                                         : launch<kCutBytes>(k_draw_cut<__nv_bfloat16>, rows->rows, plan, bytes, a, stream);
 }

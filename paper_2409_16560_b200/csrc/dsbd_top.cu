@@ -141,7 +141,7 @@ int run_top(const dsbd_rows_t *r, TopArgs &a, dsbd_stream_t stream) {
     const Plan p = plan_top(r, NT, CTAS, LIST, a.K);
     a.ctas = p.ctas;
     a.per = p.per;
-    return launch<NT>(k_top<T, NT, G, LIST, HOT, CTAS>, r->rows, p, sizeof(TopList<NT, G, LIST, HOT>), a, stream);
+    return launch<sizeof(TopList<NT, G, LIST, HOT>), NT>(k_top<T, NT, G, LIST, HOT, CTAS>, r->rows, p, sizeof(TopList<NT, G, LIST, HOT>), a, stream);
 }
 
 }  // namespace
