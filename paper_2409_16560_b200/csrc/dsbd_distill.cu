@@ -207,7 +207,8 @@ __global__ void __launch_bounds__(NT, RESIDENT) k_distill(DistillArgs a) {
         // (in 64 bits: the loss takes these tokens' log q from their logits themselves, so an error of their sum would stay in it)
 #pragma unroll
         for (int i = 0; i < MINE; ++i) {
-            if (stands[i] && z[i] != -CUDART_INF_F) sum_named += rescale(z[i], most.y, scale);
+            // (+inf: no softmax, so NaN, as x - most gives it where such a logit is not named)
+            if (stands[i] && z[i] != -CUDART_INF_F) sum_named += z[i] < CUDART_INF_F ? rescale(z[i], most.y, scale) : (double)CUDART_NAN_F;
             sum_entries += e[i];
         }
         sum_named = warp_total(sum_named);
@@ -261,7 +262,8 @@ __global__ void __launch_bounds__(NT, RESIDENT) k_distill(DistillArgs a) {
     // ---- the gradient: the others', then the named tokens' over it
     if constexpr (GRAD) {
         const double q = others_top * per_whole;
-        const float factor_f = rest_sum != 0.0 ? (float)((double)weight * a.temperature * (a.rest ? q - e_rest * per_teacher : q) * inverse_of(rest_sum)) : 0.f;
+        const float factor_f = rest_sum != 0.0 ? (float)((double)weight * a.temperature * (a.rest ? q - e_rest * per_teacher : q) * inverse_of(rest_sum))
+                                                : whole == whole ? 0.f : CUDART_NAN_F;
         if (base == -CUDART_INF_F) base = 0.f;
         const float2 base2 = {-base, -base}, scale2 = {scale_f, scale_f}, factor2 = {factor_f, factor_f};
         auto slope = [&](float (&x)[P]) {
