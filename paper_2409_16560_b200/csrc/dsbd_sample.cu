@@ -13,8 +13,8 @@
 //     bins certainly hold the prefix.  These tokens go to a list in one CTA, as above; where they are too many for it, those of the bins
 //     that the cut may lie in do, and all CTAs draw from their shares.
 //     Where the list does not hold these either: a histogram of 512 bins over the cluster, linear in the logit first, then in the bits of the
-//     keys of the bin that the cut is in, until that is one key; equal keys go by token.  Masses are then whole numbers (2^62 / V' of the
-//     largest token's mass, V' the power of two from V on), so sums do not depend on their order.  Then the draw over all shares.
+//     keys of the bin that the cut is in, until that is one key; equal keys go by token.  Masses are then whole numbers (Whole), so sums do not
+//     depend on their order.  Then the draw over all shares.
 #include <algorithm>
 
 #include "dsbd_top.cuh"
@@ -65,7 +65,7 @@ struct Shared {
     Note scratch[kWarps];
     double sums[kWarps + 1];
     uint64_t scan[kWarps];
-    uint64_t picked_before;
+    uint64_t picked_goal;
     uint32_t picked_bin, picked_count;
     int found;
 };
@@ -153,18 +153,51 @@ __device__ __forceinline__ void clear(Hist &h) {
     __syncthreads();
 }
 
-// Mass as a whole number.
+// Mass as a whole number, in units of 2^-more / unit of the largest one's.  unit is 2^62 / V', V' the power of two from V on, and a token in bin b of the
+// 64 octaves has at most 2^-(b / 8): with more_of(b) units, masses keep 2^-41 of themselves or better down to 2^-38 of the largest, and a bin's
+// sum stays below 2^62.  (Units of one size leave a tail of masses of 2^-30 few digits: V 262144, top-p 0.9999, 4 of 115309 tokens lost.)
+constexpr int kMore = 38;
+__device__ __forceinline__ int more_of(int bin) { return min(bin / 8, kMore); }
+
 struct Whole {
     const Mass &mass;
     double unit;
-    __device__ __forceinline__ uint64_t of(float z) const {
+    __device__ __forceinline__ uint64_t of(float z, int more) const {
         // (by its bits: the conversion to whole numbers of 64 bits takes a loop)
         const uint64_t bits = (uint64_t)__double_as_longlong(mass.of(z) * unit);
-        const int up = (int)(bits >> 52) - 1075;
+        const int up = (int)(bits >> 52) - 1075 + more;
         const uint64_t digits = (bits & 0xfffffffffffffull) | 0x10000000000000ull;
         return up >= 0 ? digits << up : up > -53 ? digits >> -up : 0;
     }
 };
+
+// Sums over bins of different units: up to 2^100.
+struct Wide {
+    uint64_t low, high;
+    __device__ __forceinline__ Wide(uint64_t low = 0, uint64_t high = 0) : low(low), high(high) {}
+    __device__ __forceinline__ Wide &operator+=(const Wide &o) {
+        low += o.low;
+        high += o.high + (low < o.low);
+        return *this;
+    }
+    __device__ __forceinline__ Wide operator+(const Wide &o) const { return Wide(*this) += o; }
+    __device__ __forceinline__ Wide operator-(const Wide &o) const { return {low - o.low, high - o.high - (low < o.low)}; }
+    __device__ __forceinline__ bool operator<(const Wide &o) const { return high < o.high || (high == o.high && low < o.low); }
+    // by 1 to 127
+    __device__ __forceinline__ Wide up(int n) const { return n < 64 ? Wide(low << n, high << n | low >> (64 - n)) : Wide(0, low << (n - 64)); }
+    __device__ __forceinline__ Wide down(int n) const { return n < 64 ? Wide(low >> n | high << (64 - n), high >> n) : Wide(high >> (n - 64), 0); }
+    // x / 2^n, rounded up
+    __device__ __forceinline__ Wide part(int n) const { return (*this + (Wide(1).up(n) - Wide(1))).down(n); }
+};
+
+// p of a sum, rounded up: what a prefix that has p of it reaches.  0 < p < 1.
+__device__ __forceinline__ Wide goal_of(const Wide &sum, float p) {
+    const uint32_t bits = __float_as_uint(p), digits = bits & 0x7fffffu;
+    const uint64_t m = bits >> 23 ? digits | 0x800000u : digits;
+    const int down = bits >> 23 ? 150 - (int)(bits >> 23) : 149;
+    // (sum m is below 2^124)
+    return down < 124 ? Wide(sum.low * m, sum.high * m + __umul64hi(sum.low, m)).part(down) : Wide(1);
+}
 
 // The token of rank `rank` (from 0) among those of the share that `is` holds for, of all CTAs, in the tokens' order.
 template <class T, class F>
@@ -223,13 +256,13 @@ __device__ int nth_token(Row<T> &r, uint32_t rank, F is) {
     return sh.found;
 }
 
-// The cut within `within` that keeps the k largest tokens (BY_MASS false), or the shortest prefix of at least p of the mass.
+// The cut within `within` that keeps the k largest tokens (BY_MASS false), or the shortest prefix of at least p of the mass (bins of 64 octaves then).
 template <bool BY_MASS, class T>
-__device__ Cut cut_at(Row<T> &r, Cut within, uint32_t k, double p, const Whole &whole, float width) {
+__device__ Cut cut_at(Row<T> &r, Cut within, uint32_t k, float p, const Whole &whole, float width) {
     Shared &sh = r.sh;
     const float scale = bins_over(width);
-    uint64_t above = 0;
-    double goal = (double)k;
+    uint64_t goal = k;                             // of what is looked at: where in it the last kept token lies
+    int more = 0;
     uint32_t lo = 0, hi = 0xffffffffu;
     int shift = 32;
     for (bool first = true;; first = false) {
@@ -240,7 +273,7 @@ __device__ Cut cut_at(Row<T> &r, Cut within, uint32_t k, double p, const Whole &
             if (!within.keeps(key, t) || (!first && (key < lo || key > hi))) return;
             const int b = first ? bin_below(r.top, z, scale) : (int)((hi - key) >> shift);
             if (BY_MASS) {
-                const uint64_t m = whole.of(z);
+                const uint64_t m = whole.of(z, first ? more_of(b) : more);
                 if (m == 0) return;
                 const uint32_t low = (uint32_t)m, was = atomicAdd(&h.low[b], low);
                 const uint32_t high = (uint32_t)(m >> 32) + (was + low < low);
@@ -251,24 +284,38 @@ __device__ Cut cut_at(Row<T> &r, Cut within, uint32_t k, double p, const Whole &
         cluster_barrier(r.ctas);
         const uint32_t n = (uint32_t)bin_count(r, h);
         const uint64_t v = BY_MASS ? bin_mass(r, h) : n;
-        uint64_t total;
-        const uint64_t excl = before(v, &total, sh.scan);
-        if (BY_MASS && first) goal = p * (double)total;
-        if (!BY_MASS && first && total <= k) return within;          // (masked rows may have fewer than k)
-        if (v && (double)(above + excl) < goal && (double)(above + excl + v) >= goal) {
-            sh.picked_bin = threadIdx.x;
-            sh.picked_count = n;
-            sh.picked_before = excl;
+        if (BY_MASS && first) {
+            const int up = kMore - more_of(threadIdx.x);
+            const Wide w = up ? Wide(v).up(up) : Wide(v);
+            Wide total;
+            static_assert(sizeof(Note) >= sizeof(Wide) && alignof(Note) >= alignof(Wide), "");
+            const Wide excl = before(w, &total, reinterpret_cast<Wide *>(sh.scratch)), end = goal_of(total, p);
+            if (v && excl < end && !(excl + w < end)) {
+                const Wide left = end - excl;
+                sh.picked_bin = threadIdx.x;
+                sh.picked_count = n;
+                sh.picked_goal = up ? left.part(up).low : left.low;
+            }
+        } else {
+            uint64_t total;
+            const uint64_t excl = before(v, &total, sh.scan);
+            if (!BY_MASS && first && total <= k) return within;      // (masked rows may have fewer than k)
+            if (v && excl < goal && excl + v >= goal) {
+                sh.picked_bin = threadIdx.x;
+                sh.picked_count = n;
+                sh.picked_goal = goal - excl;
+            }
         }
         __syncthreads();
         const uint32_t bin = sh.picked_bin, count = sh.picked_count;
-        above += sh.picked_before;
+        goal = sh.picked_goal;
         if (first) {
+            more = more_of(bin);
             // (the keys of a linear bin: by looking at them)
             uint32_t least = 0xffffffffu, most = 0;
             each<T>(r.s, r.mem, [&](int t, float z) {
                 const uint32_t key = key_of(z);
-                if (!within.keeps(key, t) || bin_below(r.top, z, scale) != (int)bin || (BY_MASS && whole.of(z) == 0)) return;
+                if (!within.keeps(key, t) || bin_below(r.top, z, scale) != (int)bin || (BY_MASS && whole.of(z, more) == 0)) return;
                 least = min(least, key);
                 most = max(most, key);
             });
@@ -284,12 +331,12 @@ __device__ Cut cut_at(Row<T> &r, Cut within, uint32_t k, double p, const Whole &
             if ((uint64_t)hi - lo >= 1ull << shift) lo = hi - ((1u << shift) - 1);
         }
         // everything of the bin is kept: its only token, or the last one of the k
-        if (count == 1 || (!BY_MASS && above + count == k)) return lo > within.key ? Cut{lo, 0x7fffffff} : Cut{max(lo, within.key), within.token};
+        if (count == 1 || (!BY_MASS && goal == count)) return lo > within.key ? Cut{lo, 0x7fffffff} : Cut{max(lo, within.key), within.token};
         if (lo == hi) {
-            uint32_t keep = (uint32_t)(k - above);
+            uint32_t keep = (uint32_t)goal;
             if (BY_MASS) {
-                const double m = (double)whole.of(of_key(lo));
-                keep = (uint32_t)fmin(fmax(ceil((goal - (double)above) / m), 1.0), (double)count);
+                const uint64_t m = whole.of(of_key(lo), more);
+                keep = (uint32_t)min((goal + m - 1) / m, (uint64_t)count);
             }
             const Cut tied = {lo, lo == within.key ? within.token : 0x7fffffff};
             if (keep >= count) return tied;
@@ -800,8 +847,8 @@ __device__ void draw_cut(const SampleArgs &a, float4 *mem, Shared &sh) {
         return;
     }
     const Whole whole = {mass, (double)(1ull << (30 + __clz(a.V - 1 | 1)))};
-    if (set.k) cut = cut_at<false>(r, cut, (uint32_t)set.k, 0.0, whole, 2.f * (r.top - r.low));
-    if (set.p < 1.f) cut = cut_at<true>(r, cut, 0, (double)set.p, whole, 64.f * 0.6931472f * set.T);
+    if (set.k) cut = cut_at<false>(r, cut, (uint32_t)set.k, 0.f, whole, 2.f * (r.top - r.low));
+    if (set.p < 1.f) cut = cut_at<true>(r, cut, 0, set.p, whole, 64.f * 0.6931472f * set.T);
     draw_shared(r, a, row, set, cut, mass);
 }
 
