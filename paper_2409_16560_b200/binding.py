@@ -1049,7 +1049,8 @@ def distill(logits, value, index, rest=None, weight=None, temperature=1.0, loss=
     """dsbd_distill: losses of the student's rows logits [rows, V] against a teacher's entries value, index [rows, K] (and rest [rows],
     the teacher's other tokens together, as top_logits gives them), and the gradient of sum(weight * loss) by the logits.  grad: True for
     a new tensor, a tensor [rows, V] (rows may lie apart; the logits themselves: in place), or None for the losses alone.  Returns (loss
-    fp32 [rows], grad or None, status); logits.backward(grad) hands the gradient on to what made the logits."""
+    fp32 [rows], grad or None, status); logits.backward(grad) hands the gradient on to what made the logits.  In place counts as a change of the
+    logits: what made them must not need them again (a product does not, a soft cap does, and raises)."""
     rows, dev = _rows(logits), logits.get_device()
     R, V = rows.rows, rows.V
     shape = value.shape
@@ -1077,4 +1078,6 @@ def distill(logits, value, index, rest=None, weight=None, temperature=1.0, loss=
     rc = load().dsbd_distill(C.addressof(rows), C.addressof(p), at_loss, at, stride, at_status, _stream(stream))
     if rc != OK:
         raise DsbdError("dsbd_distill", rc)
+    if at == rows.logits and R:
+        torch.autograd.graph.increment_version(grad)    # an operation that saved the logits refuses to go back through them
     return loss, grad, status
