@@ -5,6 +5,7 @@ device pointers of the C ABI declared in ``include/dsbd.h`` and checks return co
 no CPU fallback: without the built library, or without a CUDA device, calls raise.
 """
 import ctypes as C
+import operator
 import os
 
 import numpy as np
@@ -13,6 +14,7 @@ import torch
 from . import build as _build
 
 OK = 0
+ERR_UNSUPPORTED = -2
 DTYPE_BF16, DTYPE_F32 = 0, 1
 NODE_UNREACHED, NODE_ACCEPTED, NODE_REJECTED, NODE_CUT, NODE_PRUNED = 0, 1, 2, 3, 4
 SRC_DRAFT, SRC_RESIDUAL, SRC_FILL, SRC_EXTRA = 0, 1, 2, 3
@@ -950,6 +952,14 @@ def chunk_attention_paged(chunk, Hq, Hkv, d, scale, q, k_pool, v_pool, out=None,
 
 # ---------------------------------------------------------------- rows of logits: draws, largest logits, distillation
 MAX_TOP = 1024               # DSBD_MAX_TOP
+_INT32_MAX = 0x7fffffff
+
+
+def _count(n, where):
+    """A number of rows, tokens, draws or entries, which the C ABI takes in 32 bits (ctypes would cut it to them)."""
+    if n > _INT32_MAX:
+        raise DsbdError(where, ERR_UNSUPPORTED)
+    return n
 
 
 class RowsT(C.Structure):
@@ -973,7 +983,7 @@ def _rows(logits):
     stride, one = logits.stride()
     if V < 1 or (V > 1 and one != 1):
         raise AssertionError("a row's logits lie side by side")
-    return RowsT(logits.data_ptr(), stride if R > 1 else V, R, V, _DTYPES[logits.dtype])
+    return RowsT(logits.data_ptr(), stride if R > 1 else V, _count(R, "rows"), _count(V, "tokens"), _DTYPES[logits.dtype])
 
 
 def _given(t, shape, dtype, device, what):
@@ -1014,14 +1024,17 @@ def sample_rows(logits, uniform, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0,
     shape, R = uniform.shape, rows.rows
     if len(shape) not in (1, 2) or shape[0] != R:
         raise AssertionError("uniform is [rows] or [rows, draws]")
+    draws = _count(shape[1], "dsbd_sample_rows") if len(shape) == 2 else 1
     u = _given(uniform, shape, torch.float32, dev, "uniform")
     status, at_status = _row_call(dev, status, stream)
     token, at_token = _or_new(token, shape, torch.int32, dev, stream, "token")
     logp, at_logp = _or_new(logp, shape, torch.float32, dev, stream, "logp")
-    p = SampleParamsT(1.0, 1.0, 0.0, 0, None, None, None, None, shape[1] if len(shape) == 2 else 1)
+    p = SampleParamsT(1.0, 1.0, 0.0, 0, None, None, None, None, draws)
     for name, x in (("temperature", temperature), ("top_p", top_p), ("min_p", min_p), ("top_k", top_k)):
         if isinstance(x, torch.Tensor):
             setattr(p, name + "_r", _given(x, (R,), torch.int32 if name == "top_k" else torch.float32, dev, name))
+        elif name == "top_k":
+            p.top_k = max(0, min(operator.index(x), _INT32_MAX))        # (below 1 and from V on: off)
         else:
             setattr(p, name, x)
     rc = load().dsbd_sample_rows(C.addressof(rows), C.addressof(p), u, at_token, at_logp, at_status, _stream(stream))
@@ -1033,7 +1046,7 @@ def sample_rows(logits, uniform, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0,
 def top_logits(logits, K, temperature=1.0, value=None, index=None, rest=None, status=None, stream=None):
     """dsbd_top_logits: the K largest logits of each row of logits [rows, V] in falling order, of equal ones the lower token first, and
     the log-sum-exp of the row's other logits / temperature.  Returns (value fp32 [rows, K], index int32 [rows, K], rest fp32 [rows], status)."""
-    rows, dev, K = _rows(logits), logits.get_device(), int(K)
+    rows, dev, K = _rows(logits), logits.get_device(), _count(int(K), "dsbd_top_logits")
     R = rows.rows
     status, at_status = _row_call(dev, status, stream)
     value, at_value = _or_new(value, (R, K), torch.float32, dev, stream, "value")
@@ -1057,7 +1070,7 @@ def distill(logits, value, index, rest=None, weight=None, temperature=1.0, loss=
     if len(shape) != 2 or shape[0] != R:
         raise AssertionError("value is [rows, K]")
     f32 = torch.float32
-    p = DistillParamsT(shape[1], temperature, _given(value, shape, f32, dev, "value"), _given(index, shape, torch.int32, dev, "index"),
+    p = DistillParamsT(_count(shape[1], "dsbd_distill"), temperature, _given(value, shape, f32, dev, "value"), _given(index, shape, torch.int32, dev, "index"),
                        None if rest is None else _given(rest, (R,), f32, dev, "rest"),
                        None if weight is None else _given(weight, (R,), f32, dev, "weight"))
     status, at_status = _row_call(dev, status, stream)
