@@ -119,7 +119,7 @@ struct TopList {
     template <bool REST>
     __device__ __forceinline__ void clear(float least, float scale, Sum &cleared) {
         const uint32_t n = listed, key = key_of(least);
-        static_assert(kEach <= 16, "");
+        static_assert(kEach <= 16 && LIST <= 1 << (53 - 40), "");
         uint64_t e[kEach];
         float h = -CUDART_INF_F, l = 0.f;
 #pragma unroll
@@ -151,10 +151,11 @@ struct TopList {
         cleared.add({h, sum * 0x1p-40}, scale);
     }
 
-    // The kept words' tokens at or above `least` to the list, the others' sum to `cleared` (as in clear).
+    // The kept words' tokens at or above `least` to the list, the others' sum to `cleared` (as in clear; of more terms, so in steps of 2^-38).
     template <class T, bool REST>
     __device__ __forceinline__ void flush(float least, float scale, Sum &cleared) {
         constexpr int P = kPer<T>;
+        static_assert((uint64_t)HOT * P <= 1ull << (53 - 38), "sums of whole numbers are exact");
         const int n = (int)hots;
         float h = -CUDART_INF_F, l = 0.f;
         for (int i = threadIdx.x; i < n; i += NT) {
@@ -184,7 +185,7 @@ struct TopList {
             unpack(hot[i], x);
 #pragma unroll
             for (int e = 0; e < P; ++e)
-                if (x[e] < least) sum += rint((double)exp2_fast((x[e] - from) * scale) * 0x1p40);
+                if (x[e] < least) sum += rint((double)exp2_fast((x[e] - from) * scale) * 0x1p38);
         }
         sum = warp_sum(sum);
         if ((threadIdx.x & 31) == 0) sums[threadIdx.x / 32] = sum;
@@ -192,7 +193,7 @@ struct TopList {
         if (threadIdx.x == 0) hots = 0;
         sum = 0.0;
         for (int w = 0; w < kWarps_; ++w) sum += sums[w];
-        cleared.add({h, sum * 0x1p-40}, scale);
+        cleared.add({h, sum * 0x1p-38}, scale);
         __syncthreads();
     }
 
