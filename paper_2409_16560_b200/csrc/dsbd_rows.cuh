@@ -185,7 +185,6 @@ __device__ __forceinline__ uint32_t next_place(uint32_t *n) {
     return was;
 }
 
-__device__ __forceinline__ float larger(float x, float y) { return fmaxf(x, y); }
 __device__ __forceinline__ double add(double x, double y) { return x + y; }
 
 // Over a warp without shuffles, which wait in one queue with the loads and stores of all of an SM's warps: 250 cycles each beside CTAs that

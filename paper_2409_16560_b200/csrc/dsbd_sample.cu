@@ -83,7 +83,7 @@ struct Row {
     const float4 *mem;
     Shared &sh;
     uint64_t *list;                                // of `room` entries
-    int room, ctas, rank, V;
+    int room, ctas, rank;
     int note_turn, hist_turn;
     float top, low;                                // the largest logit; the smallest of the threads' finite maxima
 
@@ -812,7 +812,7 @@ __device__ void draw_cut(const SampleArgs &a, float4 *mem, Shared &sh) {
     if (settings_of(a, row, set) != kCut) return;
     begun_arrive(a.ctas);
     const T *at = static_cast<const T *>(a.logits) + (int64_t)row * a.stride;
-    Row<T> r = {share<T>(at, a.V, rank, a.per), mem, sh, reinterpret_cast<uint64_t *>(mem + a.words), a.list_room, a.ctas, rank, a.V, 0, 0, 0.f, 0.f};
+    Row<T> r = {share<T>(at, a.V, rank, a.per), mem, sh, reinterpret_cast<uint64_t *>(mem + a.words), a.list_room, a.ctas, rank, 0, 0, 0.f, 0.f};
     Mass::fill(sh.table);
     if (!bring<T>(r, at, mem, a.status)) {
         if (rank == 0)

@@ -40,7 +40,7 @@ struct TopList {
     static constexpr int kTop = NT * G / 2;        // K, at most: half the groups
     static_assert(kBins % NT == 0 && LIST % NT == 0 && LIST >= 2 * kTop && HOT * sizeof(float4) >= LIST * sizeof(uint64_t), "");
 
-    static constexpr int kList = LIST, kHot = HOT;
+    static constexpr int kList = LIST;
 
     float4 hot[HOT];
     int hot_token[HOT];                            // of the word's first element
