@@ -67,13 +67,14 @@ __device__ __forceinline__ void put_share(T *row, const Share &s, F f) {
 }
 
 // MINE entries of a thread: k = threadIdx.x + i * NT.  RESIDENT CTAs of an SM.  GRAD: with the gradient (the losses alone leave the
-// registers of its last batch free: one text for both 1022 us for 4608 rows of 128256 fp32, 19.3 for 517 of 50257 bf16 without, so 999 and 18.4).
+// registers of its last batch free: one text for both 2 per cent slower with 4608 rows of 128256 fp32, 5 with 517 of 50257 bf16 without).
 //
-// One reading and one writing of the logits are what it has to do: 4608 rows of 128256 fp32 999 us, 4.7 TB/s in both directions together, of
-// 723 at the copy rate; 2048 rows in bf16 267 us of 161.  What holds it up is a CTA's chain (some 12000 cycles: the teacher, the first words, two
+// One reading and one writing of the logits are what it has to do: 4608 rows of 128256 fp32 998 us, 4.7 TB/s in both directions together, of
+// 723 at the copy rate (from one GPU to another up to 1029); 2048 rows in bf16 273 us of 161.  592 rows of 128256 read 1.11 times the logits from
+// HBM in fp32 and 1.29 times in bf16 (shares of 128 KB under way: 444 and 592).  What holds it up is a CTA's chain (some 12000 cycles: the teacher, the first words, two
 // exchanges, 64-bit sums), which the SM's other CTAs cover in part, and the second reading, from the L2 for what is not held in shared memory.  (Held:
 // all of it leaves one CTA of an SM, less is slower in the L2; rows' loads begun a row ahead, 1 to 8 rows a cluster: no gain; 512 threads: slower.)
-// Without a gradient one reading: 517 rows of 50257 bf16 18.4 us of 8.
+// Without a gradient one reading: 517 rows of 50257 bf16 18.1 us of 8, fp32 28 of 16; 1024 of 128256 fp32 107 of 80.
 //
 // 64-bit chains are kept short and off the others' way (a dependent step takes some 40 cycles, a logarithm more than a thousand): the teacher's
 // exponentials run while the first words are on their way, the student's sums are joined by lanes side by side, and logarithms are
@@ -347,8 +348,8 @@ __global__ void __launch_bounds__(NT, RESIDENT) k_distill(DistillArgs a) {
 }
 
 // CTAs of a row: shares of up to 128 KB (a CTA's fixed chain, some 12000 cycles, counts for less than with smaller ones; with larger
-// ones the rows under way outgrow the L2, from which what is not held is read again: 2048 rows of 128256 bf16, two CTAs each 267 us, one
-// 306), and more where the SMs would stand idle.
+// ones the rows under way outgrow the L2, from which what is not held is read again: 2048 rows of 128256 bf16, two CTAs each 273 us, one
+// 309), and more where the SMs would stand idle.
 inline Plan plan_distill(const dsbd_rows_t *r, int resident) {
     const int size = r->dtype == DSBD_DTYPE_F32 ? 4 : 2;
     Plan p;
@@ -368,9 +369,8 @@ int run_distill(const dsbd_rows_t *r, DistillArgs &a, dsbd_stream_t stream) {
     const Plan p = plan_distill(r, RESIDENT);
     a.ctas = p.ctas;
     a.per = p.per;
-    // whole batches of 32 elements a thread, as many as leave room for RESIDENT CTAs in an SM's 228 KB, of which each takes 1 more (2048 rows of 128256 bf16:
-    // three batches and three CTAs 306 us, two and four
-    // 280), but the last, which stays in registers; without a gradient nothing is read twice
+    // whole batches of 32 elements a thread, as many as leave room for RESIDENT CTAs in an SM's 228 KB, of which each takes 1 more (2048 rows of 128256 bf16,
+    // an earlier form: three batches and three CTAs 306 us, two and four 280), but the last, which stays in registers; without a gradient nothing is read twice
     const int batches = (p.per / kPer<T> + 1 + kBatch - 1) / kBatch, marks = batches * NT * 4;
     const int room = 228 * 1024 / RESIDENT - 1024 - (int)sizeof(Shared) - marks;
     a.held = GRAD ? std::min(batches - 1, std::min(room, kHeld) / 16 / kBatch) * kBatch : 0;
@@ -401,8 +401,8 @@ extern "C" int dsbd_distill(const dsbd_rows_t *rows, const dsbd_distill_params_t
     a.inverse = 1.0 / (double)p->temperature;
     a.value = p->value; a.index = p->index; a.rest = p->rest; a.weight = p->weight;
     a.loss = loss; a.grad = grad; a.grad_stride = grad_stride; a.status = status;
-    // Four CTAs of an SM where their registers last (517 rows of 50257 bf16 without gradients 18.2 us, with three 23.1; 2048 of 128256 with gradients
-    // 267 and 284); with gradients in fp32 three (20 rows of 32000 6.5 us, with four and what they spill 7.7; 4608 of 128256 999 and 1001).
+    // Four CTAs of an SM where their registers last (517 rows of 50257 bf16 without gradients 18.1 us, with three 23.9; 2048 of 128256 with gradients
+    // 273 and 287); with gradients in fp32 three (20 rows of 32000 6.6 us, with four and what they spill 8.0; 4608 of 128256 996 and 1000).
     if (rows->dtype == DSBD_DTYPE_BF16)
         return grad ? run_distill<__nv_bfloat16, 4, true>(rows, a, stream) : run_distill<__nv_bfloat16, 4, false>(rows, a, stream);
     return grad ? run_distill<float, 3, true>(rows, a, stream) : run_distill<float, 4, false>(rows, a, stream);

@@ -852,9 +852,11 @@ __device__ void draw_cut(const SampleArgs &a, float4 *mem, Shared &sh) {
     draw_shared(r, a, row, set, cut, mass);
 }
 
-// Bound by what an SM issues: 512 rows of 128256 fp32 with top-p 0.95 take 392 us (their bytes 40) and 113 warp instructions an element, 17 to bring
-// it, 51 for its mass in 64 bits and its bin, 38 to list; part of each are the exchanges' some hundreds a thread.  A few rows are a chain: one of these 22 us, of which 3 bring it, 6.5 are masses and bins, 5.5 the list, 6.5 its end and the draw.  Shares of 64 KB, so that two CTAs fit an SM and the chains of one
-// cover the other's (64 rows in clusters of 4 and of 8: 63 and 64 us; 512 rows 417 and 392).
+// 512 rows of 128256 fp32 with top-p 0.95 at temperature 0.9 take 392 us (their bytes 40; at temperature 1 prefixes are longer, 561) and 113 warp
+// instructions an element, 17 to bring it, 51 for its mass in 64 bits and its bin, 38 to list; part of each are the exchanges' some hundreds a
+// thread.  No pipe is full (issue slots 56 %, ALU 40 %): phases stand behind one another, with barriers of the cluster between them, and two CTAs
+// of an SM cover each other in part.  A few rows are a chain: one of these 22 us, of which 3 bring it, 6.5 are masses
+// and bins, 5.5 the list, 6.5 its end and the draw.  Shares of 64 KB, so that two CTAs fit an SM (64 rows in clusters of 4 and of 8: 63 and 64 us; 512 rows 417 and 392).
 //
 // Beside k_draw, whose rows are others: its CTAs have all waited for what came before them when this kernel is launched, so this one
 // need not; but it ends after k_draw has, as what comes next waits for this kernel alone.
@@ -1128,9 +1130,12 @@ __device__ void draw_few(DrawShared &sh, const SampleArgs &a, int row, const Set
     }
 }
 
-// Rows without cuts are bound by the 64-bit exponentials of all tokens (30 warp instructions an element, of which 12 on the FP64 pipe: 512 rows of 128256
-// fp32, 8 draws each, 108 us, 2.4 TB/s, of 40 at the copy rate); exponentials in 32 bits would stream, but are off by more than an improbable
-// token's cell.  Rows with a short top-k take what k_top takes: one row of 32000 with top-k 10 and top-p 0.8 10 us, 64 rows of 128256 fp32 19.
+// Rows without cuts take the time of the 64-bit exponentials of all tokens (30 warp instructions an element, of which 12 on the FP64 pipe: 512 rows of
+// 128256, 8 draws each, fp32 110 us of 40 at the copy rate, bf16 102 of 20); exponentials in 32 bits would stream, but are off by more than an
+// improbable token's cell.  No pipe is full (issue 56 %, FP64 40 %): it is the latency of dependent steps, and of loads of which none are in flight
+// while a batch is worked on, with three CTAs of an SM.  Rows with a short top-k and those at temperature 0 take what k_top takes, a chain of words,
+// bounds, exchange and order: one row of 32000 with top-k 10 and top-p 0.8 10 us; 64 rows of 128256 with top-k 50 fp32 25, bf16 23, at temperature 0
+// 17 and 15; 512 rows with top-k 20 fp32 78 (of 40), bf16 71, with top-k 100 98 and 90, at temperature 0 fp32 69.
 template <class T>
 __global__ void __launch_bounds__(kOnce, kOnceResident) k_draw(SampleArgs a) {
     extern __shared__ float4 mem[];

@@ -22,9 +22,9 @@ struct Part {
 };
 
 // A row is one CTA's (a cluster's where there are few): it streams its share once and at the end sorts little more than K entries.  Long
-// rows are bound by HBM (4608 rows of 128256 fp32, K = 64: 462 us, 5.1 TB/s, of 362 at the copy rate); short ones with many entries by the
+// rows are bound by HBM (4608 rows of 128256 fp32, K = 64: 464 us, 5.1 TB/s, of 362 at the copy rate; from one GPU to another up to 485); short ones with many entries by the
 // instructions that a row needs however short it is -- bounds, sorting kept words out, the list's order: 2048 rows of 32000 bf16,
-// K = 256: 124 us for 21 of bytes, 39 thousand warp instructions a row.  Small CTAs, many on an SM, let some rows stream
+// K = 256: 125 us for 21 of bytes, 39 thousand warp instructions a row.  Small CTAs, many on an SM, let some rows stream
 // while others sort (128 threads 124 us, 256 140, 512 192).  A few rows are a chain of load, bounds, exchange and sort: 20 rows of 50257, 15 us.
 template <class T, int NT, int G, int LIST, int HOT, int CTAS>
 __global__ void __launch_bounds__(NT, CTAS) k_top(TopArgs a) {
